@@ -61,6 +61,23 @@ typedef enum {
   RF_ERR_DEVICE_TIMEOUT = 5   /* a bounded device-side wait expired (status word) */
 } rf_status;
 
+/* Element types of the operators that take one (the step core's own are fixed). */
+typedef enum { RF_BF16 = 0, RF_FP16 = 1, RF_FP32 = 2 } rf_dtype;
+
+/* Which elements of a head rotate together (rf_rope). */
+typedef enum {
+  RF_ROPE_INTERLEAVED = 0, /* pair i is elements 2i and 2i + 1 */
+  RF_ROPE_HALF = 1         /* pair i is elements i and i + R/2, R rotated elements in all */
+} rf_rope_pairing;
+
+/* Activations of rf_linear. */
+typedef enum {
+  RF_ACT_NONE = 0,
+  RF_ACT_GELU = 1,      /* x (1 + erf(x / sqrt 2)) / 2 */
+  RF_ACT_GELU_TANH = 2, /* x (1 + tanh(sqrt(2 / pi) (x + 0.044715 x^3))) / 2 */
+  RF_ACT_SILU = 3       /* x / (1 + e^-x) */
+} rf_act;
+
 /* Human-readable name of a status code.  Never NULL; static storage. */
 const char* rf_status_str(int status);
 
@@ -347,6 +364,81 @@ rf_status rf_frame_gram(const float* d_P, int F, int64_t E, int64_t ld, double* 
 rf_status rf_keyframe_select(const double* h_G, int F, int M, double tau, double dtau,
                              double delta_up, double delta_down, uint8_t* h_is_key,
                              int32_t* h_num_keys);
+
+/*
+ * The operators around the attention.  In a block of a video diffusion transformer the step core's
+ * attention stands between projections, rotary positions, attention to an encoder's states and a
+ * feed-forward pair.  rf_rope, rf_cross_attn and rf_linear compute those for the active frames
+ * only, from the same device-side lists as rf_attn, so a step needs no host synchronisation and no
+ * gathered copies.  Common to the three:
+ *   d_active, d_counts  lists from rf_schedule_compact (device), or both NULL: every frame.
+ *               Rows of other frames are neither read for a result nor written.
+ *   dtype       rf_dtype of the inputs, and of the outputs unless said otherwise
+ *   row strides in elements.  Heads of a row are contiguous, d elements each; a slice of a fused
+ *               buffer is given by its base and the buffer's row stride.
+ * Sums, statistics and the epilogue's arithmetic are held in 32 bits and rounded once.
+ */
+
+/*
+ * rf_rope_table -- (cos, sin) of one axis' rotary angles (CPU, 64-bit arithmetic).
+ *
+ *   h_pos    [n] positions on the axis, any finite values (fractional ones stretch a model to
+ *            another size)
+ *   dim      rotated elements of the axis, even, >= 2
+ *   h_table  [n][dim/2][2] fp32 output: cos and sin of h_pos[i] * base^(-2 j / dim)
+ */
+rf_status rf_rope_table(const double* h_pos, int n, int dim, double base, float* h_table);
+
+/*
+ * rf_rope -- rotary positions over time, height and width, queries and keys in one launch.
+ *
+ *   d_Yq, d_Xq  [F*gh*gw] rows of Hq heads of d elements: output and input; may be the same
+ *               buffer (same strides), and may not overlap otherwise
+ *   d_Yk, d_Xk, Hk  the same for the keys; NULL, NULL, 0: queries only
+ *   dtype       RF_BF16, RF_FP16 or RF_FP32
+ *   F, gh, gw   frames, and the grid of tokens of a frame: token t = (f gh + y) gw + x
+ *   d           head dim, 8..256 and % 8; the first R = dim_t + dim_h + dim_w <= d elements
+ *               rotate, the others are copied
+ *   dim_t, dim_h, dim_w  rotated elements per axis, even, 0 = axis not used; the time axis' pairs
+ *               come first, then height's, then width's
+ *   d_table_t, d_table_h, d_table_w  fp32 [F][dim_t/2][2], [gh][dim_h/2][2], [gw][dim_w/2][2] tables
+ *               of rf_rope_table, uploaded; NULL where the axis is not used
+ *   pairing     rf_rope_pairing
+ *   inverse     nonzero: rotate back, which is also the gradient of the rotation
+ * Each pair (x0, x1) of angle a becomes (x0 cos a - x1 sin a, x0 sin a + x1 cos a).  A frame keeps its
+ * positions over the steps, so rotated keys may be cached and projected (rf_project_kv): Eq. 3 of
+ * rotated keys is the rotation of Eq. 3.
+ * Bases and row strides on 16-byte boundaries (RF_ERR_MISALIGNED), tables on 8-byte ones.
+ */
+rf_status rf_rope(void* d_Yq, const void* d_Xq, int64_t yq_row_stride, int64_t xq_row_stride,
+                  int Hq, void* d_Yk, const void* d_Xk, int64_t yk_row_stride,
+                  int64_t xk_row_stride, int Hk, int dtype, int F, int gh, int gw, int d,
+                  int dim_t, int dim_h, int dim_w, const float* d_table_t,
+                  const float* d_table_h, const float* d_table_w, int pairing, int inverse,
+                  const int32_t* d_active, const int32_t* d_counts, rf_stream_t stream);
+
+/*
+ * rf_linear -- matrix product with bias, activation, gate and residual:
+ *     Y[t, n] = R[t, n] + gate[n] * act(sum_k X[t, k] W[n, k] + bias[n])
+ *
+ *   d_Y         [F*N][d_out] output of out_dtype: dtype or RF_FP32
+ *   d_X         [F*N][d_in], d_W [d_out][d_in] of dtype RF_BF16 or RF_FP16
+ *   d_bias      [d_out] of dtype, or NULL
+ *   act         rf_act
+ *   d_gate      fp32, or NULL: frame f's gate is at d_gate + f * gate_frame_stride
+ *               (0: one gate for all frames)
+ *   d_R         [F*N][d_out] of out_dtype, or NULL; may be d_Y itself (same stride)
+ *   d_status    as for rf_attn, or NULL
+ * X and W rows on 16-byte boundaries (RF_ERR_MISALIGNED): d_in itself may be any number, as may
+ * d_out.  Outputs, bias, gate and residual need only their own elements' alignment, and are moved in
+ * vectors where all of them are 16-byte aligned.  Requires an sm_103 device.
+ */
+rf_status rf_linear(void* d_Y, int64_t y_row_stride, int out_dtype, const void* d_X,
+                    int64_t x_row_stride, const void* d_W, int64_t w_row_stride, int dtype, int F,
+                    int N, int d_in, int d_out, const void* d_bias, int act, const float* d_gate,
+                    int64_t gate_frame_stride, const void* d_R, int64_t r_row_stride,
+                    const int32_t* d_active, const int32_t* d_counts, int32_t* d_status,
+                    rf_stream_t stream);
 
 /*
  * rf_pipeline -- the step core fed from pinned host memory: one asynchronous denoising step

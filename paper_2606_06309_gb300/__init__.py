@@ -17,7 +17,7 @@ import numpy as np
 __all__ = ["load", "lib_path", "RFError", "rf_plan_build", "rf_schedule_compact",
            "rf_project", "rf_project_kv", "rf_attn", "rf_attn_block_masked",
            "rf_attn_workspace_bytes", "rf_attn_noalloc", "rf_step", "rf_step_core", "rf_frame_gram",
-           "rf_keyframe_select", "rf_selftest_bounded_wait", "rf_pipeline_create",
+           "rf_keyframe_select", "rf_rope_table", "rf_rope", "rf_linear", "rf_selftest_bounded_wait", "rf_pipeline_create",
            "rf_pipeline_step", "rf_pipeline_sync", "rf_pipeline_bytes", "rf_pipeline_destroy",
            "rf_status_str", "rf_version", "EXPORTS"]
 
@@ -29,6 +29,7 @@ EXPORTS = ("rf_status_str", "rf_version", "rf_last_error", "rf_plan_build",
            "rf_schedule_compact", "rf_project", "rf_project_kv", "rf_attn",
            "rf_attn_block_masked", "rf_attn_workspace_bytes",
            "rf_attn_noalloc", "rf_step", "rf_step_core", "rf_frame_gram", "rf_keyframe_select",
+           "rf_rope_table", "rf_rope", "rf_linear",
            "rf_pipeline_create", "rf_pipeline_step", "rf_pipeline_sync", "rf_pipeline_bytes",
            "rf_pipeline_destroy", "rf_selftest_bounded_wait")
 
@@ -56,6 +57,11 @@ _SIG = {
     "rf_step": ([_vp, _vp, _vp, _vp, _vp, _vp, _i32, _i64, _vp], _i32),
     "rf_step_core": ([_vp] * 5 + [_i32, _i32, _i64, _i32, _i32] + [_vp] * 14 +
                      [_i64, _i64, _i64, _f32, _vp, _i64, _vp, _vp], _i32),
+    "rf_rope_table": ([_vp, _i32, _i32, ctypes.c_double, _vp], _i32),
+    "rf_rope": ([_vp, _vp, _i64, _i64, _i32, _vp, _vp, _i64, _i64] + [_i32] * 9 + [_vp, _vp, _vp] +
+                [_i32, _i32, _vp, _vp, _vp], _i32),
+    "rf_linear": ([_vp, _i64, _i32, _vp, _i64, _vp, _i64] + [_i32] * 5 +
+                  [_vp, _i32, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp], _i32),
     "rf_pipeline_create": ([_i32, _i32, _i32, _i32, _i64, _i32, _vp, _vp, _vp, _vp, _vp, _vp,
                             _vp, _vp, _i32, _vp, _vp, _vp, ctypes.POINTER(_vp)], _i32),
     "rf_pipeline_step": ([_vp, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _f32], _i32),
@@ -238,6 +244,92 @@ def rf_step_core(mask, cur_slot, alpha, beta, dt, F: int, N: int, E: int, H: int
         _ptr(Kc), _ptr(Vc), _ptr(O), _ptr(lse), _ptr(Q), _ptr(K), _ptr(V), qkv_row_stride,
         kv_row_stride, o_row_stride, float(softmax_scale), _ptr(workspace), ws_bytes,
         _ptr(status), _stream(stream)))
+
+
+_DTYPES = {"torch.bfloat16": 0, "torch.float16": 1, "torch.float32": 2}
+_PAIRINGS = {"interleaved": 0, "half": 1}
+_ACTS = {None: 0, "none": 0, "gelu": 1, "gelu_tanh": 2, "silu": 3}
+
+
+def _dtype(fn: str, *tensors) -> int:
+    """rf_dtype shared by the given tensors (None is skipped)."""
+    kinds = {str(t.dtype) for t in tensors if t is not None}
+    if len(kinds) != 1 or not kinds <= _DTYPES.keys():
+        raise ValueError(f"{fn}: tensors of one type out of bf16, fp16 and fp32, got {sorted(kinds)}")
+    return _DTYPES[kinds.pop()]
+
+
+def _rows(fn: str, name: str, t, *shape) -> int:
+    """Row stride of t, whose rows have to be contiguous; its shape is checked."""
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{fn}: {name} has shape {tuple(t.shape)}, not {shape}")
+    n = 1
+    for size, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
+        if size > 1 and stride != n:
+            raise ValueError(f"{fn}: a row of {name} is not contiguous (strides {t.stride()})")
+        n *= size
+    # one row: its stride is free, and torch may report any
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), n)
+
+
+def rf_rope_table(pos, dim: int, base: float = 10000.0):
+    """(cos, sin) table of one axis, a host array fp32 [n, dim/2, 2], for any positions `pos`."""
+    pos = np.ascontiguousarray(np.asarray(pos, dtype=np.float64))
+    out = np.zeros((pos.size, max(dim, 0) // 2, 2), np.float32)
+    _check("rf_rope_table", load().rf_rope_table(_ptr(pos), pos.size, dim, float(base), _ptr(out)))
+    return out
+
+
+def rf_rope(Yq, Xq, Yk, Xk, F: int, gh: int, gw: int, dims, tables, pairing: str = "interleaved",
+            inverse: bool = False, active=None, counts=None, stream=None):
+    """Rotary positions of queries Xq [F*gh*gw, Hq, d] and keys Xk (or None) into Yq and Yk, which
+    may be the inputs themselves.  dims: rotated elements (time, height, width); tables: the three
+    axes' device tables of rf_rope_table, None where dims is 0."""
+    fn, T = "rf_rope", F * gh * gw
+    d = Xq.shape[-1]
+    keys = Xk is not None
+    dt = _dtype(fn, Yq, Xq, *((Yk, Xk) if keys else ()))
+    side = []
+    for y, x, name in ((Yq, Xq, "q"),) + (((Yk, Xk, "k"),) if keys else ()):
+        shape = (T, x.shape[1], d)
+        side += [_ptr(y), _ptr(x), _rows(fn, "Y" + name, y, *shape), _rows(fn, "X" + name, x, *shape),
+                 x.shape[1]]
+    for n, dim, t in zip((F, gh, gw), dims, tables):
+        if t is not None and (tuple(t.shape) != (n, dim // 2, 2) or _dtype(fn, t) != 2
+                              or not t.is_contiguous()):
+            raise ValueError(f"{fn}: a table is not a contiguous fp32 [{n}, {dim // 2}, 2]")
+    _check(fn, load().rf_rope(
+        *side, *(() if keys else (None, None, 0, 0, 0)), dt, F, gh, gw, d, *dims,
+        *(_ptr(t) for t in tables), _PAIRINGS[pairing], int(inverse), _ptr(active), _ptr(counts),
+        _stream(stream)))
+
+
+def rf_linear(Y, X, W, F: int, N: int, bias=None, act=None, gate=None, residual=None, active=None,
+              counts=None, status=None, stream=None):
+    """Y = residual + gate * act(X W^T + bias) for the active frames' rows.
+
+    X [F*N, d_in], W [d_out, d_in] and bias [d_out] in bf16 or fp16; Y and residual [F*N, d_out]
+    in that type or fp32; gate fp32 [d_out], or [F, d_out] for one per frame; act None, "gelu",
+    "gelu_tanh" or "silu".  residual may be Y."""
+    fn = "rf_linear"
+    d_out, d_in = W.shape
+    dt, out = _dtype(fn, X, W, bias), _dtype(fn, Y, residual)
+    if bias is not None and (tuple(bias.shape) != (d_out,) or not bias.is_contiguous()):
+        raise ValueError(f"{fn}: bias is not a contiguous [{d_out}]")
+    gate_stride = 0
+    if gate is not None:
+        if _dtype(fn, gate) != 2:
+            raise ValueError(f"{fn}: gate is not fp32")
+        if gate.dim() == 1:
+            _rows(fn, "gate", gate[None], 1, d_out)
+        else:
+            gate_stride = _rows(fn, "gate", gate, F, d_out)
+    _check(fn, load().rf_linear(
+        _ptr(Y), _rows(fn, "Y", Y, F * N, d_out), out, _ptr(X), _rows(fn, "X", X, F * N, d_in),
+        _ptr(W), _rows(fn, "W", W, d_out, d_in), dt, F, N, d_in, d_out, _ptr(bias), _ACTS[act],
+        _ptr(gate), gate_stride, _ptr(residual),
+        0 if residual is None else _rows(fn, "residual", residual, F * N, d_out), _ptr(active),
+        _ptr(counts), _ptr(status), _stream(stream)))
 
 
 def rf_pipeline_create(F: int, N: int, H: int, d: int, E: int, plan: dict, z2, K0, V0,

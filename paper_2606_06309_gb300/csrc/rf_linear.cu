@@ -1,0 +1,768 @@
+// rf_linear.cu -- matrix product with bias, activation, gate and residual, over the active frames.
+//
+//     Y[t, n] = R[t, n] + g[n] * act(sum_k X[t, k] W[n, k] + b[n])       t: tokens of active frames
+//
+// Products of 16-bit elements are exact in 32 bits and summed there (tcgen05, fp32 accumulators in
+// tensor memory); bias, activation, gate and residual follow in 32 bits on the accumulator as it
+// leaves tensor memory, so Y is rounded once and nothing between them goes to memory.
+//
+// Two kernels, both fed by TMA from 128-byte-swizzled tiles of 64 columns of K:
+//   pair_kernel  many rows: a pair of CTAs on one tile of 256 tokens x BN columns (cta_group::2).
+//   split_kernel few rows: 128 columns of W against all the rows of a launch, W as the tensor
+//                core's M side, and K split over a cluster of CTAs.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "rf_ops.h"
+#include "rf_tc_ptx.cuh"
+
+namespace rf {
+namespace {
+
+constexpr uint32_t kWaitLimitNs = 2000000000u;    // 2 s: no legitimate wait comes close
+constexpr uint64_t kDrainLimitNs = 200000000ull;  // 0.2 s for what is in flight at teardown
+constexpr int kBlockK = 64;                       // columns of K per stage: 128 bytes, one swizzle atom
+constexpr int kMaxBoxes = 8;                      // gathered boxes per lane: 256 rows / 32 lanes
+
+// ---------------------------------------------------------------------------------------
+// Epilogue
+// ---------------------------------------------------------------------------------------
+struct Epilogue {
+  void* Y;
+  const void* R;        // or null; elements of Y's type
+  const void* bias;     // or null; elements of X's type
+  const float* gate;    // or null
+  int64_t y_stride, r_stride, gate_stride;  // elements; gate_stride 0: one row for all frames
+  int act, in_dtype, out_dtype;
+  int n_out;
+  int vec;              // Y and R rows, bias and gate can be moved in 16-byte vectors
+};
+
+__device__ __forceinline__ float ex2_neg_log2e(float x) { return ex2_approx(-1.4426950408889634f * x); }
+// x * sigmoid(s): 1 + e^-s overflows to infinity for very negative s, and the quotient is then 0
+__device__ __forceinline__ float times_sigmoid(float x, float s) {
+  return __fdividef(x, 1.f + ex2_neg_log2e(s));
+}
+template <int N>
+__device__ __forceinline__ void activate(int act, float (&v)[N]) {
+  switch (act) {
+    case RF_ACT_GELU:
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] = 0.5f * v[i] * (1.f + erff(v[i] * 0.70710678118654752f));
+      break;
+    case RF_ACT_GELU_TANH:  // 0.5 (1 + tanh u) = sigmoid(2 u)
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        v[i] = times_sigmoid(v[i], 1.5957691216057308f * (v[i] + 0.044715f * v[i] * v[i] * v[i]));
+      break;
+    case RF_ACT_SILU:
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] = times_sigmoid(v[i], v[i]);
+      break;
+    default:
+      break;
+  }
+}
+
+__device__ __forceinline__ float load_elem(const void* p, int64_t i, int dtype) {
+  if (dtype == RF_FP32) return static_cast<const float*>(p)[i];
+  if (dtype == RF_FP16) return __half2float(static_cast<const __half*>(p)[i]);
+  return __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
+}
+__device__ __forceinline__ void store_elem(void* p, int64_t i, int dtype, float v) {
+  if (dtype == RF_FP32) static_cast<float*>(p)[i] = v;
+  else if (dtype == RF_FP16) static_cast<__half*>(p)[i] = __float2half_rn(v);
+  else static_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(v);
+}
+__device__ __forceinline__ void unpack2(uint32_t w, int dtype, float& lo, float& hi) {
+  if (dtype == RF_FP16) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
+    lo = f.x;
+    hi = f.y;
+  } else {
+    lo = __uint_as_float(w << 16);
+    hi = __uint_as_float(w & 0xFFFF0000u);
+  }
+}
+// 32 consecutive elements from a 16-byte boundary
+__device__ __forceinline__ void load32(const void* p, int64_t i, int dtype, float (&x)[32]) {
+  if (dtype == RF_FP32) {
+    const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(p) + i);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float4 f = q[e];
+      x[4 * e] = f.x;
+      x[4 * e + 1] = f.y;
+      x[4 * e + 2] = f.z;
+      x[4 * e + 3] = f.w;
+    }
+  } else {
+    const uint4* q = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + i);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint4 w = q[e];
+      unpack2(w.x, dtype, x[8 * e], x[8 * e + 1]);
+      unpack2(w.y, dtype, x[8 * e + 2], x[8 * e + 3]);
+      unpack2(w.z, dtype, x[8 * e + 4], x[8 * e + 5]);
+      unpack2(w.w, dtype, x[8 * e + 6], x[8 * e + 7]);
+    }
+  }
+}
+
+// One element of the result from its sum.
+__device__ __forceinline__ void finish_one(const Epilogue& e, int64_t token, int frame, int n,
+                                           float sum) {
+  float v[1] = {sum};
+  if (e.bias) v[0] += load_elem(e.bias, n, e.in_dtype);
+  activate(e.act, v);
+  if (e.gate) v[0] *= e.gate[frame * e.gate_stride + n];
+  if (e.R) v[0] += load_elem(e.R, token * e.r_stride + n, e.out_dtype);
+  store_elem(e.Y, token * e.y_stride + n, e.out_dtype, v[0]);
+}
+
+// Columns n .. n + 31 of a row.
+__device__ __forceinline__ void finish_row(const Epilogue& e, int64_t token, int frame, int n,
+                                           float (&v)[32]) {
+  if (!e.vec || n + 32 > e.n_out) {
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+      if (n + i < e.n_out && e.bias) v[i] += load_elem(e.bias, n + i, e.in_dtype);
+    activate(e.act, v);
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+      if (n + i < e.n_out) {
+        if (e.gate) v[i] *= e.gate[frame * e.gate_stride + n + i];
+        if (e.R) v[i] += load_elem(e.R, token * e.r_stride + n + i, e.out_dtype);
+        store_elem(e.Y, token * e.y_stride + n + i, e.out_dtype, v[i]);
+      }
+    return;
+  }
+  float x[32];
+  if (e.bias) {
+    load32(e.bias, n, e.in_dtype, x);
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] += x[i];
+  }
+  activate(e.act, v);
+  if (e.gate) {
+    load32(e.gate, frame * e.gate_stride + n, RF_FP32, x);
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] *= x[i];
+  }
+  if (e.R) {
+    load32(e.R, token * e.r_stride + n, e.out_dtype, x);
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] += x[i];
+  }
+  if (e.out_dtype == RF_FP32) {
+    float4* y = reinterpret_cast<float4*>(static_cast<float*>(e.Y) + token * e.y_stride + n);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      y[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+  } else {
+    uint4* y = reinterpret_cast<uint4*>(static_cast<uint16_t*>(e.Y) + token * e.y_stride + n);
+    uint32_t w[16];
+    if (e.out_dtype == RF_FP16) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) w[i] = pack_f16x2(v[2 * i], v[2 * i + 1]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) w[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+  }
+}
+
+struct LinearParams {
+  RowMap rows;
+  Epilogue epi;
+  int N;  // tokens per frame, for the gate's row (rows.N where there is no list is all tokens)
+  int kblocks, n_tiles, fp16;
+  int32_t* status;
+  // split_kernel
+  int tile_tokens, cluster, stages;
+};
+
+__device__ __forceinline__ void flag_error(const LinearParams& p, int where) {
+  if (p.status) atomicOr(p.status, RF_ERR_DEVICE_TIMEOUT | (1 << (8 + where)));
+}
+
+// Token and frame of row r (r < rows of the launch); token -1 in a frame's padding.
+__device__ __forceinline__ int row_token(const LinearParams& p, int r, int& frame) {
+  const int a = r / p.rows.Np, q = r - a * p.rows.Np;
+  const int f = p.rows.frame(a);
+  const int token = f * p.rows.N + q;
+  frame = token / p.N;
+  return q < p.rows.N ? token : -1;
+}
+
+// How the n rows from row r0 are loaded: one box if they lie in one frame, else boxes of
+// rows.box rows, box lane + 32 i by its first token.
+struct RowTile {
+  bool whole;
+  int tok[kMaxBoxes];
+};
+__device__ __forceinline__ RowTile find_rows(const RowMap& m, int R, int r0, int n) {
+  RowTile t;
+  const int a0 = r0 / m.Np;
+  t.whole = r0 >= R || a0 == (min(r0 + n, R) - 1) / m.Np;
+  if (t.whole) {
+    // (rows past the frame read the following tokens, past the last one zeros: never stored)
+    t.tok[0] = r0 >= R ? m.T : m.frame(a0) * m.N + (r0 - a0 * m.Np);
+    return t;
+  }
+#pragma unroll
+  for (int i = 0; i < kMaxBoxes; ++i) {
+    const int r = r0 + ((threadIdx.x & 31) + 32 * i) * m.box;
+    const int a = r / m.Np;
+    t.tok[i] = r < R ? m.frame(a) * m.N + (r - a * m.Np) : m.T;
+  }
+  return t;
+}
+// Issue the copies of one k block of the tile into dst (all lanes; the bytes are announced before).
+template <bool PAIR>
+__device__ __forceinline__ void load_rows(const RowTile& t, const CUtensorMap* whole,
+                                          const CUtensorMap* boxes, int box, int n, uint32_t dst,
+                                          uint32_t bar, int k0, bool lead) {
+  if (t.whole) {
+    if (lead) {
+      if (PAIR) tma_load_2d_pair(dst, whole, bar, k0, t.tok[0]);
+      else tma_load_2d(dst, whole, bar, k0, t.tok[0]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < kMaxBoxes; ++i) {
+      const int b = (threadIdx.x & 31) + 32 * i;
+      if (b * box < n) {
+        if (PAIR) tma_load_2d_pair(dst + b * box * 128, boxes, bar, k0, t.tok[i]);
+        else tma_load_2d(dst + b * box * 128, boxes, bar, k0, t.tok[i]);
+      }
+    }
+  }
+  __syncwarp();
+}
+
+// ---------------------------------------------------------------------------------------
+// Many rows: pairs of CTAs
+// ---------------------------------------------------------------------------------------
+// A pair's tile is 256 tokens x BN columns: each CTA holds 128 token rows of X, half of the tile's
+// rows of W, and the accumulators of its 128 rows; the tensor cores of both read both halves of W.
+// That is what the pair is for: a CTA alone on 128 x 256 would have to bring 48 KB into shared
+// memory per 64 columns of K, in a pair it brings 32 KB.
+// Two accumulators in tensor memory: the epilogue of a tile runs during the products of the next.
+constexpr int kPairThreads = 384;  // warp 0 TMA, 1 MMA (first CTA), 2 tensor memory, 4-11 epilogue
+constexpr int kEpiWarps = 8;
+
+template <int BN>
+struct PairCfg {
+  static constexpr int kABytes = 128 * 128, kBBytes = BN / 2 * 128;
+  static constexpr int kStageBytes = kABytes + kBBytes;
+  static constexpr int kStages = 196608 / kStageBytes;
+  static constexpr int kBarFull = 0, kBarEmpty = kStages, kBarAccFull = 2 * kStages,
+                       kBarAccEmpty = kBarAccFull + 2, kBars = kBarAccEmpty + 2;
+  static constexpr int kOffBar = kStages * kStageBytes;
+  static constexpr int kOffMisc = kOffBar + kBars * 8;
+  static constexpr int kSmem = kOffMisc + 16 + 1024;
+  static constexpr uint32_t kTmemCols = 2 * BN;
+};
+
+// Tiles in groups of eight rows of tiles, column by column within a group, so that the pairs at
+// work share rows of X and of W in L2.
+constexpr int kGroupM = 8;
+__device__ __forceinline__ void tile_at(int t, int m_tiles, int n_tiles, int& m, int& n) {
+  const int per_group = kGroupM * n_tiles;
+  const int g = t / per_group, i = t - g * per_group;
+  const int width = min(kGroupM, m_tiles - g * kGroupM);
+  n = i / width;
+  m = g * kGroupM + (i - n * width);
+}
+
+template <int BN>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
+    pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmBox,
+                const __grid_constant__ CUtensorMap tmW, const LinearParams p) {
+  using C = PairCfg<BN>;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw);
+  const uint32_t sbase = (raw + 1023u) & ~1023u;
+  uint8_t* smem = smem_raw + (sbase - raw);
+  const uint32_t bar0 = sbase + C::kOffBar;
+  auto bar = [&](int i) { return bar0 + 8u * i; };
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::kOffMisc);
+  volatile int* abort = reinterpret_cast<volatile int*>(smem + C::kOffMisc + 4);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_rank();
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < C::kStages; ++s) {
+      mbar_init(bar(C::kBarFull + s), 1);
+      mbar_init(bar(C::kBarEmpty + s), 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(bar(C::kBarAccFull + b), 1);
+      mbar_init(bar(C::kBarAccEmpty + b), 2 * kEpiWarps);
+    }
+    *abort = 0;
+    fence_mbar_init();
+    tma_prefetch_desc(&tmX);
+    tma_prefetch_desc(&tmW);
+  }
+  if (warp == 2) {
+    tmem_alloc_pair(smem_u32(tmem_slot), C::kTmemCols);
+    tmem_relinquish_pair();
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_arrive();  // the other CTA's barriers are initialised, its tensor memory allocated
+  cluster_wait();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+
+  const int R = p.rows.frames() * p.rows.Np;
+  const int m_tiles = (R + 255) / 256;
+  const int tiles = m_tiles * p.n_tiles;
+  const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+
+  if (warp == 0) {
+    const bool lead = elect_one();
+    int it = 0;
+    bool ok = true;
+    for (int t = pair; ok && t < tiles; t += pairs) {
+      int m, n;
+      tile_at(t, m_tiles, p.n_tiles, m, n);
+      const RowTile rt = find_rows(p.rows, R, m * 256 + rank * 128, 128);
+      const int w0 = n * BN + rank * (BN / 2);
+      for (int kb = 0; kb < p.kblocks; ++kb, ++it) {
+        const int s = it % C::kStages;
+        if (!__all_sync(0xffffffffu,
+                        mbar_wait_cluster(bar(C::kBarEmpty + s), ((it / C::kStages) & 1) ^ 1, abort,
+                                          kWaitLimitNs))) {
+          if (lead) flag_error(p, 0);
+          ok = false;
+          break;
+        }
+        // the first CTA's barrier counts the bytes of both
+        const uint32_t full = map_to_rank(bar(C::kBarFull + s), 0);
+        const uint32_t dst = sbase + s * C::kStageBytes;
+        if (lead && rank == 0) mbar_arrive_expect_tx(bar(C::kBarFull + s), 2 * C::kStageBytes);
+        if (lead) tma_load_2d_pair(dst + C::kABytes, &tmW, full, kb * kBlockK, w0);
+        __syncwarp();
+        load_rows<true>(rt, &tmX, &tmBox, p.rows.box, 128, dst, full, kb * kBlockK, lead);
+      }
+    }
+    // every stage that was filled has been given back (so no arrival from the other CTA is still
+    // to come) before this CTA may leave; after a wait that gave up, the copies in flight get time
+    for (int s = 0; s < C::kStages; ++s)
+      if (it > s)
+        mbar_drain(bar(C::kBarEmpty + s), ((it - 1 - s) / C::kStages) & 1, kDrainLimitNs);
+  } else if (warp == 1) {
+    if (rank == 0) {
+      const bool lead = elect_one();
+      const uint32_t idesc = idesc_f16(p.fp16, 256, BN, 0);
+      int it = 0, n_acc = 0;
+      bool ok = true;
+      for (int t = pair; ok && t < tiles; t += pairs, ++n_acc) {
+        const int b = n_acc & 1;
+        if (!__all_sync(0xffffffffu,
+                        mbar_wait_cluster(bar(C::kBarAccEmpty + b), ((n_acc >> 1) & 1) ^ 1, abort,
+                                          kWaitLimitNs))) {
+          if (lead) flag_error(p, 1);
+          break;
+        }
+        tc_fence_after();
+        const uint32_t acc = tmem + b * BN;
+        for (int kb = 0; kb < p.kblocks; ++kb, ++it) {
+          const int s = it % C::kStages;
+          if (!__all_sync(0xffffffffu,
+                          mbar_wait_cluster(bar(C::kBarFull + s), (it / C::kStages) & 1, abort,
+                                            kWaitLimitNs))) {
+            if (lead) flag_error(p, 2);
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          if (lead) {
+            const uint32_t sA = sbase + s * C::kStageBytes;
+            const uint64_t dA = smem_desc_sw128(sA, 16, 1024);
+            const uint64_t dB = smem_desc_sw128(sA + C::kABytes, 16, 1024);
+#pragma unroll
+            for (int k = 0; k < kBlockK / 16; ++k)
+              tc_mma_ss_pair(acc, dA + k * 2, dB + k * 2, idesc, (kb | k) != 0);
+            tc_commit_pair(bar(C::kBarEmpty + s));
+            if (kb == p.kblocks - 1) tc_commit_pair(bar(C::kBarAccFull + b));
+          }
+          __syncwarp();
+        }
+      }
+    }
+  } else if (warp >= 4) {
+    const int quarter = warp & 3, part = (warp - 4) >> 2;  // lanes of tensor memory; half of BN
+    const uint32_t lane_base = static_cast<uint32_t>(quarter * 32) << 16;
+    int n_acc = 0;
+    for (int t = pair; t < tiles; t += pairs, ++n_acc) {
+      int m, n;
+      tile_at(t, m_tiles, p.n_tiles, m, n);
+      const int b = n_acc & 1;
+      const int r = m * 256 + rank * 128 + quarter * 32 + lane;
+      int frame = 0;
+      const int token = r < R ? row_token(p, r, frame) : -1;
+      if (!__all_sync(0xffffffffu, mbar_wait_cluster(bar(C::kBarAccFull + b), (n_acc >> 1) & 1,
+                                                     abort, kWaitLimitNs))) {
+        if (lane == 0) flag_error(p, 3);
+        break;
+      }
+      tc_fence_after();
+#pragma unroll 1
+      for (int c = 0; c < BN / 64; ++c) {
+        const int col = part * (BN / 2) + c * 32;
+        uint32_t v[32];
+        tmem_ld32(tmem + lane_base + b * BN + col, v);
+        tmem_wait_ld();
+        if (c == BN / 64 - 1) {  // the accumulator is read: it may be written again
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_remote(map_to_rank(bar(C::kBarAccEmpty + b), 0));
+        }
+        const int n0 = n * BN + col;
+        if (token >= 0 && n0 < p.epi.n_out)
+          finish_row(p.epi, token, frame, n0, *reinterpret_cast<float(*)[32]>(&v));
+      }
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  cluster_arrive();  // nothing of the other CTA's refers to this CTA's memory any more
+  cluster_wait();
+  if (warp == 2) {
+    tc_fence_after();
+    tmem_dealloc_pair(tmem, C::kTmemCols);
+  }
+}
+
+// ---------------------------------------------------------------------------------------
+// Few rows: W as the M side, K split over a cluster
+// ---------------------------------------------------------------------------------------
+// A tile is 128 columns of the result (rows of W: the tensor core's M side) x tile_tokens tokens
+// (its N side, 16 to 256), so that one token costs a sixteenth of a tile and not all of it.  The
+// CTAs of a cluster take equal ranges of K; each leaves its sums in shared memory, and each
+// finishes its share of the tile's tokens from all of them, in the order of the ranges.
+constexpr int kSplitThreads = 256;  // warp 0 TMA, 1 MMA, 2 tensor memory, 4-7 read the accumulator
+constexpr int kSplitMaxStages = 12;
+constexpr int kSplitRing = 212992;  // bytes for stages; the sums of a split take their place
+constexpr int kSplitBarFull = 0, kSplitBarEmpty = kSplitMaxStages,
+              kSplitBarAcc = 2 * kSplitMaxStages, kSplitBars = kSplitBarAcc + 1;
+constexpr int kSplitOffBar = kSplitRing, kSplitOffMisc = kSplitOffBar + kSplitBars * 8,
+              kSplitSmem = kSplitOffMisc + 16 + 1024;
+
+__global__ void __launch_bounds__(kSplitThreads, 1)
+    split_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmBox,
+                 const __grid_constant__ CUtensorMap tmW, const LinearParams p) {
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw);
+  const uint32_t sbase = (raw + 1023u) & ~1023u;
+  uint8_t* smem = smem_raw + (sbase - raw);
+  const uint32_t bar0 = sbase + kSplitOffBar;
+  auto bar = [&](int i) { return bar0 + 8u * i; };
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + kSplitOffMisc);
+  volatile int* abort = reinterpret_cast<volatile int*>(smem + kSplitOffMisc + 4);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int BT = p.tile_tokens, C = p.cluster;
+  const int rank = C > 1 ? static_cast<int>(cluster_rank()) : 0;
+  const int tile = blockIdx.x / C;
+  const int m = tile / p.n_tiles, n = tile - m * p.n_tiles;
+  const int R = p.rows.frames() * p.rows.Np;
+  const int r0 = m * BT;
+  if (r0 >= R) return;  // the whole cluster
+  const int stage_bytes = 16384 + BT * 128;
+  const uint32_t tmem_cols = BT < 32 ? 32 : BT;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < p.stages; ++s) {
+      mbar_init(bar(kSplitBarFull + s), 1);
+      mbar_init(bar(kSplitBarEmpty + s), 1);
+    }
+    mbar_init(bar(kSplitBarAcc), 1);
+    *abort = 0;
+    fence_mbar_init();
+    tma_prefetch_desc(&tmX);
+    tma_prefetch_desc(&tmW);
+  }
+  if (warp == 2) {
+    tmem_alloc(smem_u32(tmem_slot), tmem_cols);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  const int kb0 = p.kblocks * rank / C, kb1 = p.kblocks * (rank + 1) / C;
+
+  if (warp == 0) {
+    const bool lead = elect_one();
+    const RowTile rt = find_rows(p.rows, R, r0, BT);
+    int it = 0;
+    for (int kb = kb0; kb < kb1; ++kb, ++it) {
+      const int s = it % p.stages;
+      if (!__all_sync(0xffffffffu, mbar_wait(bar(kSplitBarEmpty + s), ((it / p.stages) & 1) ^ 1,
+                                             abort, kWaitLimitNs))) {
+        if (lead) flag_error(p, 0);
+        break;
+      }
+      const uint32_t dst = sbase + s * stage_bytes;
+      if (lead) {
+        mbar_arrive_expect_tx(bar(kSplitBarFull + s), stage_bytes);
+        tma_load_2d(dst, &tmW, bar(kSplitBarFull + s), kb * kBlockK, n * 128);
+      }
+      __syncwarp();
+      load_rows<false>(rt, &tmX, &tmBox, p.rows.box, BT, dst + 16384, bar(kSplitBarFull + s),
+                       kb * kBlockK, lead);
+    }
+    for (int s = 0; s < p.stages; ++s)  // every copy has landed
+      if (it > s) mbar_drain(bar(kSplitBarFull + s), ((it - 1 - s) / p.stages) & 1, kDrainLimitNs);
+  } else if (warp == 1) {
+    const bool lead = elect_one();
+    const uint32_t idesc = idesc_f16(p.fp16, 128, BT, 0);
+    int it = 0;
+    for (int kb = kb0; kb < kb1; ++kb, ++it) {
+      const int s = it % p.stages;
+      if (!__all_sync(0xffffffffu, mbar_wait(bar(kSplitBarFull + s), (it / p.stages) & 1, abort,
+                                             kWaitLimitNs))) {
+        if (lead) flag_error(p, 1);
+        break;
+      }
+      tc_fence_after();
+      if (lead) {
+        const uint32_t sA = sbase + s * stage_bytes;
+        const uint64_t dA = smem_desc_sw128(sA, 16, 1024), dB = smem_desc_sw128(sA + 16384, 16, 1024);
+#pragma unroll
+        for (int k = 0; k < kBlockK / 16; ++k)
+          tc_mma_ss(tmem, dA + k * 2, dB + k * 2, idesc, (it | k) != 0);
+        tc_commit(bar(kSplitBarEmpty + s));
+      }
+      __syncwarp();
+    }
+    // all MMAs issued are done (also after a wait that gave up: tensor memory is freed below)
+    if (lead) tc_commit(bar(kSplitBarAcc));
+    __syncwarp();
+    mbar_drain(bar(kSplitBarAcc), 0, kDrainLimitNs);
+  }
+  float* sums = reinterpret_cast<float*>(smem);  // [BT][128]
+  if (warp >= 4) {
+    const int quarter = warp & 3;
+    const int col = n * 128 + quarter * 32 + lane;
+    const bool ok = __all_sync(0xffffffffu, mbar_wait(bar(kSplitBarAcc), 0, abort, kWaitLimitNs));
+    if (!ok && lane == 0) flag_error(p, 2);
+    tc_fence_after();
+#pragma unroll 1
+    for (int c = 0; ok && c < BT; c += 32) {
+      uint32_t v[32];
+      tmem_ld32(tmem + (static_cast<uint32_t>(quarter * 32) << 16) + c, v);
+      tmem_wait_ld();
+      if (C > 1) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+          if (c + i < BT) sums[(c + i) * 128 + quarter * 32 + lane] = __uint_as_float(v[i]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+          const int r = r0 + c + i;
+          if (c + i >= BT || r >= R) break;
+          int frame;
+          const int token = row_token(p, r, frame);
+          if (token >= 0 && col < p.epi.n_out)
+            finish_one(p.epi, token, frame, col, __uint_as_float(v[i]));
+        }
+      }
+    }
+  }
+  __syncwarp();
+  if (C > 1) {
+    cluster_arrive();
+    cluster_wait();
+    // two tokens at a time (half of the threads each), every C-th pair of them
+    const int col = threadIdx.x & 127;
+    if (n * 128 + col < p.epi.n_out) {
+      for (int j = 2 * rank + (threadIdx.x >> 7); j < BT; j += 2 * C) {
+        const int r = r0 + j;
+        if (r >= R) break;
+        int frame;
+        const int token = row_token(p, r, frame);
+        if (token < 0) continue;
+        const uint32_t at = sbase + (j * 128 + col) * 4;
+        float part[8];
+#pragma unroll
+        for (int c = 0; c < 8; ++c) part[c] = c < C ? ld_cluster_f(map_to_rank(at, c)) : 0.f;
+        float sum = part[0];
+#pragma unroll
+        for (int c = 1; c < 8; ++c) sum += part[c];
+        finish_one(p.epi, token, frame, n * 128 + col, sum);
+      }
+    }
+    __syncwarp();
+    cluster_arrive();  // every CTA has read the others' sums
+    cluster_wait();
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 2) {
+    tc_fence_after();
+    tmem_dealloc(tmem, tmem_cols);
+  }
+}
+
+// ---------------------------------------------------------------------------------------
+// Host side
+// ---------------------------------------------------------------------------------------
+template <typename K>
+rf_status set_smem(K kernel, int bytes, const DeviceInfo& di, bool (&done)[64]) {
+  if (bytes > di.max_smem_optin) return fail(RF_ERR_UNSUPPORTED, "rf_linear: shared memory");
+  if (!done[di.device]) {
+    if (cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                             bytes))
+      return fail(RF_ERR_CUDA, "cudaFuncSetAttribute(rf_linear)", e);
+    done[di.device] = true;
+  }
+  return RF_OK;
+}
+
+rf_status map_2d(CUtensorMap* m, int dtype, const void* base, int cols, int64_t rows,
+                 int64_t row_stride, int box_rows) {
+  const uint64_t dims[2] = {static_cast<uint64_t>(cols), static_cast<uint64_t>(rows)};
+  const uint64_t strides[1] = {static_cast<uint64_t>(row_stride) * 2};
+  const uint32_t box[2] = {kBlockK, static_cast<uint32_t>(box_rows)};
+  return make_tensor_map(m, dtype, base, 2, dims, strides, box);
+}
+
+// CTAs per cluster of a split launch: as many ranges of K as fill the SMs, of at least two blocks.
+int split_ranges(int64_t tiles, int kblocks, int sms) {
+  int c = 1;
+  while (c < 8 && tiles * c * 2 <= sms && kblocks >= c * 4) c *= 2;
+  return c;
+}
+
+template <int BN>
+rf_status launch_pair(const CUtensorMap& x, const CUtensorMap& box, const CUtensorMap& w,
+                      const LinearParams& p, int64_t tiles, const DeviceInfo& di, cudaStream_t s) {
+  static bool done[64] = {};
+  if (rf_status st = set_smem(pair_kernel<BN>, PairCfg<BN>::kSmem, di, done)) return st;
+  const int64_t pairs = std::min<int64_t>(tiles, di.sm_count / 2);
+  pair_kernel<BN><<<static_cast<unsigned>(2 * pairs), kPairThreads, PairCfg<BN>::kSmem, s>>>(
+      x, box, w, p);
+  return launch_status("rf_linear pair_kernel launch");
+}
+
+rf_status launch_split(const CUtensorMap& x, const CUtensorMap& box, const CUtensorMap& w,
+                       const LinearParams& p, int64_t tiles, const DeviceInfo& di, cudaStream_t s) {
+  static bool done[64] = {};
+  if (rf_status st = set_smem(split_kernel, kSplitSmem, di, done)) return st;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(static_cast<unsigned>(tiles * p.cluster));
+  cfg.blockDim = dim3(kSplitThreads);
+  cfg.dynamicSmemBytes = kSplitSmem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = static_cast<unsigned>(p.cluster);
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = p.cluster > 1 ? 1 : 0;
+  if (cudaError_t e = cudaLaunchKernelEx(&cfg, split_kernel, x, box, w, p)) {
+    cudaGetLastError();
+    return fail(RF_ERR_CUDA, "rf_linear split_kernel launch", e);
+  }
+  return RF_OK;
+}
+
+}  // namespace
+}  // namespace rf
+
+using namespace rf;
+
+extern "C" rf_status rf_linear(void* d_Y, int64_t y_row_stride, int out_dtype, const void* d_X,
+                               int64_t x_row_stride, const void* d_W, int64_t w_row_stride,
+                               int dtype, int F, int N, int d_in, int d_out, const void* d_bias,
+                               int act, const float* d_gate, int64_t gate_frame_stride,
+                               const void* d_R, int64_t r_row_stride, const int32_t* d_active,
+                               const int32_t* d_counts, int32_t* d_status, rf_stream_t stream) {
+  if (!d_Y || !d_X || !d_W) return fail(RF_ERR_INVALID_ARG, "rf_linear: null pointer");
+  if (dtype != RF_BF16 && dtype != RF_FP16) return fail(RF_ERR_UNSUPPORTED, "rf_linear: dtype");
+  if (out_dtype != dtype && out_dtype != RF_FP32)
+    return fail(RF_ERR_UNSUPPORTED, "rf_linear: output in the inputs' type or fp32");
+  if (F < 1 || N < 1 || d_in < 1 || d_out < 1)
+    return fail(RF_ERR_INVALID_ARG, "rf_linear: sizes >= 1");
+  if (act < RF_ACT_NONE || act > RF_ACT_SILU) return fail(RF_ERR_INVALID_ARG, "rf_linear: act");
+  if (x_row_stride < d_in || w_row_stride < d_in || y_row_stride < d_out ||
+      (d_R && r_row_stride < d_out) || (d_gate && gate_frame_stride != 0 && gate_frame_stride < d_out))
+    return fail(RF_ERR_INVALID_ARG, "rf_linear: row stride below the row's length");
+  if ((d_active == nullptr) != (d_counts == nullptr))
+    return fail(RF_ERR_INVALID_ARG, "rf_linear: active list and counts come together");
+  if (!aligned16(d_X) || !aligned16(d_W) || x_row_stride % 8 || w_row_stride % 8)
+    return fail(RF_ERR_MISALIGNED, "rf_linear: X and W rows on 16-byte boundaries");
+  const int es_out = dtype_bytes(out_dtype);
+  if (reinterpret_cast<uintptr_t>(d_Y) % es_out || reinterpret_cast<uintptr_t>(d_R) % es_out ||
+      reinterpret_cast<uintptr_t>(d_bias) % 2 || reinterpret_cast<uintptr_t>(d_gate) % 4)
+    return fail(RF_ERR_MISALIGNED, "rf_linear: pointer not on its elements' boundary");
+  // without a list the tokens are one frame, with nothing between them
+  const int64_t T = static_cast<int64_t>(F) * N;
+  const int64_t Fr = d_active ? F : 1, Nr = d_active ? N : T;
+  const int box = Nr < 8 ? 1 : 8;
+  const int64_t Np = (Nr + box - 1) / box * box;
+  if (T > 0x7FFFFFFF - 65536 || Fr * Np > 0x7FFFFFFF - 65536 || d_out > 0x7FFFFFFF - 65536 ||
+      d_in > 0x7FFFFFFF - 65536)
+    return fail(RF_ERR_INVALID_ARG, "rf_linear: too many tokens or columns");
+  DeviceInfo di;
+  if (rf_status st = current_device_info(&di)) return st;
+  if (di.cc_major != 10 || di.cc_minor != 3) return fail(RF_ERR_UNSUPPORTED, "needs sm_103");
+
+  LinearParams p{};
+  p.rows = {d_active, d_counts, static_cast<int>(Fr), static_cast<int>(Nr), static_cast<int>(Np), box,
+            static_cast<int>(T)};
+  Epilogue& e = p.epi;
+  e.Y = d_Y;
+  e.R = d_R;
+  e.bias = d_bias;
+  e.gate = d_gate;
+  e.y_stride = y_row_stride;
+  e.r_stride = r_row_stride;
+  e.gate_stride = gate_frame_stride;
+  e.act = act;
+  e.in_dtype = dtype;
+  e.out_dtype = out_dtype;
+  e.n_out = d_out;
+  e.vec = aligned16(d_Y) && y_row_stride * es_out % 16 == 0 &&
+          (!d_R || (aligned16(d_R) && r_row_stride * es_out % 16 == 0)) && aligned16(d_bias) &&
+          (!d_gate || (aligned16(d_gate) && gate_frame_stride % 4 == 0));
+  p.N = N;
+  p.kblocks = (d_in + kBlockK - 1) / kBlockK;
+  p.fp16 = dtype == RF_FP16;
+  p.status = d_status;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+
+  const int64_t rows = Fr * Np;  // at most: the active count is known on the device only
+  const int64_t n256 = (d_out + 255) / 256, n128 = (d_out + 127) / 128;
+  const int64_t pair_tiles = (rows + 255) / 256 * n256;
+  CUtensorMap mx, mbox, mw;
+  if (rf_status st = map_2d(&mbox, dtype, d_X, d_in, T, x_row_stride, box)) return st;
+  if (rows > 256 && pair_tiles >= di.sm_count / 4) {
+    p.n_tiles = static_cast<int>(n256);
+    if (rf_status st = map_2d(&mx, dtype, d_X, d_in, T, x_row_stride, 128)) return st;
+    if (rf_status st = map_2d(&mw, dtype, d_W, d_in, d_out, w_row_stride, 128)) return st;
+    return launch_pair<256>(mx, mbox, mw, p, pair_tiles, di, s);
+  }
+  int BT = 16;
+  while (BT < 256 && BT < rows) BT *= 2;
+  const int64_t tiles = (rows + BT - 1) / BT * n128;
+  p.n_tiles = static_cast<int>(n128);
+  p.tile_tokens = BT;
+  p.cluster = split_ranges(tiles, p.kblocks, di.sm_count);
+  p.stages = std::min(kSplitMaxStages, kSplitRing / (16384 + BT * 128));
+  if (rf_status st = map_2d(&mx, dtype, d_X, d_in, T, x_row_stride, BT)) return st;
+  if (rf_status st = map_2d(&mw, dtype, d_W, d_in, d_out, w_row_stride, 128)) return st;
+  return launch_split(mx, mbox, mw, p, tiles, di, s);
+}
