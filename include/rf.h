@@ -418,6 +418,34 @@ rf_status rf_rope(void* d_Yq, const void* d_Xq, int64_t yq_row_stride, int64_t x
                   const int32_t* d_active, const int32_t* d_counts, rf_stream_t stream);
 
 /*
+ * rf_cross_attn -- attention of the active frames' tokens to an encoder's states (the text of a
+ * prompt, an image's patches, the audio around a frame) of another length:
+ *     O[f*N+p, h] = sum_j softmax_j(scale * q.k_j) v_j    over the keys j that frame f may see
+ *
+ *   d_O         [F*N] rows of H heads of d; only rows of active frames are written
+ *   d_lse       fp32 [H][F*N] natural-log sum-exp per row, or NULL
+ *   d_Q         [F*N] rows of H heads; d_K, d_V [L] rows of Hkv heads, Hkv dividing H: query head h
+ *               reads key head h / (H / Hkv)
+ *   dtype       RF_BF16 or RF_FP16; d in {64, 128}
+ *   L           encoder states, >= 0 (0: no key; d_K and d_V may be NULL)
+ *   d_kv_range  [F][2] int32: frame f sees states [begin, end), clamped to [0, L]; ranges may
+ *               overlap, be empty, or leave states out.  NULL: every frame sees all L
+ *   d_key_mask  [L] bytes, zero = state j is seen by no row (padding); NULL: none masked.  What
+ *               masked states hold does not matter, infinities and NaN included
+ *   d_status    as for rf_attn, or NULL
+ * A row that sees no key gets O = 0 and LSE = -inf.  Arithmetic as in rf_attn: products of 16-bit
+ * elements, fp32 accumulation and softmax, probabilities rounded to dtype for the product with V.
+ * Bases and row strides on 16-byte boundaries (RF_ERR_MISALIGNED), ranges on 8-byte ones.  No
+ * workspace.  Requires an sm_103 device.
+ */
+rf_status rf_cross_attn(void* d_O, float* d_lse, const void* d_Q, const void* d_K, const void* d_V,
+                        int64_t o_row_stride, int64_t q_row_stride, int64_t k_row_stride,
+                        int64_t v_row_stride, int dtype, int F, int N, int H, int Hkv, int d, int L,
+                        const int32_t* d_kv_range, const uint8_t* d_key_mask,
+                        const int32_t* d_active, const int32_t* d_counts, float softmax_scale,
+                        int32_t* d_status, rf_stream_t stream);
+
+/*
  * rf_linear -- matrix product with bias, activation, gate and residual:
  *     Y[t, n] = R[t, n] + gate[n] * act(sum_k X[t, k] W[n, k] + bias[n])
  *

@@ -17,7 +17,8 @@ import numpy as np
 __all__ = ["load", "lib_path", "RFError", "rf_plan_build", "rf_schedule_compact",
            "rf_project", "rf_project_kv", "rf_attn", "rf_attn_block_masked",
            "rf_attn_workspace_bytes", "rf_attn_noalloc", "rf_step", "rf_step_core", "rf_frame_gram",
-           "rf_keyframe_select", "rf_rope_table", "rf_rope", "rf_linear", "rf_selftest_bounded_wait", "rf_pipeline_create",
+           "rf_keyframe_select", "rf_rope_table", "rf_rope",
+           "rf_cross_attn", "rf_linear", "rf_selftest_bounded_wait", "rf_pipeline_create",
            "rf_pipeline_step", "rf_pipeline_sync", "rf_pipeline_bytes", "rf_pipeline_destroy",
            "rf_status_str", "rf_version", "EXPORTS"]
 
@@ -29,7 +30,7 @@ EXPORTS = ("rf_status_str", "rf_version", "rf_last_error", "rf_plan_build",
            "rf_schedule_compact", "rf_project", "rf_project_kv", "rf_attn",
            "rf_attn_block_masked", "rf_attn_workspace_bytes",
            "rf_attn_noalloc", "rf_step", "rf_step_core", "rf_frame_gram", "rf_keyframe_select",
-           "rf_rope_table", "rf_rope", "rf_linear",
+           "rf_rope_table", "rf_rope", "rf_cross_attn", "rf_linear",
            "rf_pipeline_create", "rf_pipeline_step", "rf_pipeline_sync", "rf_pipeline_bytes",
            "rf_pipeline_destroy", "rf_selftest_bounded_wait")
 
@@ -60,6 +61,7 @@ _SIG = {
     "rf_rope_table": ([_vp, _i32, _i32, ctypes.c_double, _vp], _i32),
     "rf_rope": ([_vp, _vp, _i64, _i64, _i32, _vp, _vp, _i64, _i64] + [_i32] * 9 + [_vp, _vp, _vp] +
                 [_i32, _i32, _vp, _vp, _vp], _i32),
+    "rf_cross_attn": ([_vp] * 5 + [_i64] * 4 + [_i32] * 7 + [_vp] * 4 + [_f32, _vp, _vp], _i32),
     "rf_linear": ([_vp, _i64, _i32, _vp, _i64, _vp, _i64] + [_i32] * 5 +
                   [_vp, _i32, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp], _i32),
     "rf_pipeline_create": ([_i32, _i32, _i32, _i32, _i64, _i32, _vp, _vp, _vp, _vp, _vp, _vp,
@@ -302,6 +304,29 @@ def rf_rope(Yq, Xq, Yk, Xk, F: int, gh: int, gw: int, dims, tables, pairing: str
         *side, *(() if keys else (None, None, 0, 0, 0)), dt, F, gh, gw, d, *dims,
         *(_ptr(t) for t in tables), _PAIRINGS[pairing], int(inverse), _ptr(active), _ptr(counts),
         _stream(stream)))
+
+
+def rf_cross_attn(O, lse, Q, K, V, F: int, N: int, softmax_scale: float, kv_range=None,
+                  key_mask=None, active=None, counts=None, status=None, stream=None):
+    """Attention of Q [F*N, H, d] to an encoder's states K, V [L, Hkv, d], bf16 or fp16.
+
+    kv_range int32 [F, 2]: the states [begin, end) each frame sees; key_mask uint8 or bool [L],
+    zero = not seen; lse fp32 [H, F*N] or None."""
+    fn = "rf_cross_attn"
+    H, d = Q.shape[1:]
+    L, Hkv = K.shape[:2]
+    dt = _dtype(fn, O, Q, K, V)
+    for name, t, shape, kinds in (("lse", lse, (H, F * N), ("torch.float32",)),
+                                  ("kv_range", kv_range, (F, 2), ("torch.int32",)),
+                                  ("key_mask", key_mask, (L,), ("torch.uint8", "torch.bool"))):
+        if t is not None and (tuple(t.shape) != shape or str(t.dtype) not in kinds
+                              or not t.is_contiguous()):
+            raise ValueError(f"{fn}: {name} is not a contiguous {shape} of {' or '.join(kinds)}")
+    _check(fn, load().rf_cross_attn(
+        _ptr(O), _ptr(lse), _ptr(Q), _ptr(K), _ptr(V), _rows(fn, "O", O, F * N, H, d),
+        _rows(fn, "Q", Q, F * N, H, d), _rows(fn, "K", K, L, Hkv, d), _rows(fn, "V", V, L, Hkv, d),
+        dt, F, N, H, Hkv, d, L, _ptr(kv_range), _ptr(key_mask), _ptr(active), _ptr(counts),
+        float(softmax_scale), _ptr(status), _stream(stream)))
 
 
 def rf_linear(Y, X, W, F: int, N: int, bias=None, act=None, gate=None, residual=None, active=None,

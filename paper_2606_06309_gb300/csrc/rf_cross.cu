@@ -1,0 +1,948 @@
+// rf_cross.cu -- attention of the active frames' tokens to an encoder's states (tcgen05 / TMEM / TMA).
+//
+//     O[t, h] = sum_j p_j v_j,   p = softmax_j(scale q_{t,h} . k_j)      h: query head, kv head h / g
+//
+// over the keys j of the token's frame: all L states, or the frame's own range of them, without the
+// masked ones.  A row that sees no key gets O = 0 and LSE = -inf.
+//
+// One CTA per SM, 384 threads, in the roles of the step core's attention: warp 0 brings query
+// tiles and K/V tiles of 128 keys by TMA, warps 1 and 2 issue the products of query tile A and B
+// (S = Q K^T, O += P V, P over S in tensor memory), warpgroups 1 and 2 hold the running maximum and
+// sum of their tile's rows in registers, fp32, and rescale O only when a row's maximum grows by more
+// than 2^8.  Encoder states are few: an item (a pair of query tiles over one frame's keys) is often
+// only four K/V tiles long, so the next item's queries and keys are loaded, and its first product
+// issued, while the softmax warps still write the last one's rows.
+//
+// What masked keys hold must not matter, and 0 * NaN is NaN in a product: their scores are
+// replaced by -inf before anything is computed with them, and warp 3 sets their rows of V to zero
+// in shared memory before P V reads them (launches with ranges or a mask; past the last state TMA
+// fills in zeros by itself).
+//
+// Query rows.  Without ranges the active tokens are one list of rows (a frame padded to a multiple
+// of 8, so that a tile across frames is gathered in boxes of 8 rows); with ranges a tile stays in
+// its frame.  Where a frame's tokens times the query heads of a key head fit a tile, they are its
+// rows together (`packed`): K and V are then read once for all of these heads, which is what a launch
+// of few rows costs.
+//
+// Few items: the K/V tiles of an item are dealt to a cluster of up to 8 CTAs.  Each leaves its
+// unnormalised rows, maxima and sums in its shared memory, and each joins a share of the columns
+// from all of them, in the order of the ranges.
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "rf_ops.h"
+#include "rf_tc_ptx.cuh"
+
+namespace rf {
+namespace {
+
+constexpr int kBM = 128, kBN = 128;  // rows of a query tile, keys of a K/V tile
+constexpr int kThreads = 384;        // three warpgroups
+// Registers after setmaxnreg: 128 * 104 + 256 * 200 = 64512 = 384 * 168, what the launch holds.
+constexpr int kRegsLaunch = 168, kRegsControl = 104, kRegsSoftmax = 200;
+static_assert(128 * kRegsControl + 256 * kRegsSoftmax <= kThreads * kRegsLaunch, "register split");
+constexpr uint32_t kTmemCols = 512;  // S_A, S_B at 0, 128; O_A, O_B at 256, 384
+constexpr uint32_t kWaitLimitNs = 2000000000u;    // 2 s: no legitimate wait comes close
+constexpr uint64_t kDrainLimitNs = 200000000ull;  // 0.2 s for what is in flight at teardown
+constexpr float kRescaleLog2 = 8.0f;
+// P goes to the tile's MMA warp in two parts of 64 keys, and the two MMA warps take turns, over
+// hardware named barriers.  Those have no time limit: who waits on one is always released, by the
+// arrivals of the normal path or, after a bounded wait elsewhere gave up, by release_mma.
+constexpr int kPThreads = 128 + 32;
+__device__ __forceinline__ int p_barrier(int X, int part) { return 1 + 2 * X + part; }
+__device__ __forceinline__ int turn_barrier(int X) { return 5 + X; }
+
+template <int D>
+struct Cfg {
+  static constexpr int kHalves = D / 64;           // 128-byte swizzle atoms across the head dim
+  static constexpr int kTileBytes = 128 * D * 2;   // one tile of Q, K or V
+  static constexpr int kHalfBytes = 128 * 128;
+  static constexpr int kSlots = D == 128 ? 4 : 8;  // K in even slots, V in odd ones
+  static constexpr int kOffKV = 2 * kTileBytes;
+  static constexpr int kOffBar = kOffKV + kSlots * kTileBytes;
+  static constexpr int kQFull = 0, kQEmpty = 2, kKVFull = 4, kKVEmpty = 4 + kSlots,
+                       kVClean = 4 + 2 * kSlots, kSFull = 4 + 3 * kSlots, kODone = kSFull + 2,
+                       kDrain = kODone + 2, kBars = kDrain + 2;
+  static constexpr int kOffMisc = kOffBar + kBars * 8;  // tensor memory address, abort, MMA done [2]
+  static constexpr int kSmem = kOffMisc + 32 + 1024;    // + slack to align the base
+  // A split item's rows: [tile][D / 4][128] float4 over the K/V ring, {max, sum} [tile][128] over
+  // the queries
+  static_assert(2 * 128 * D * 4 <= kSlots * kTileBytes, "partial rows fit the ring");
+};
+
+struct CrossParams {
+  uint16_t* O;
+  float* lse;
+  const int2* kv_range;     // [F] or null
+  const uint8_t* key_mask;  // [L] or null
+  int32_t* status;
+  RowMap rows;
+  int64_t o_row_stride;
+  int L, g;            // g: query heads per key head
+  int units;           // heads an item is of: query heads, or key heads where packed
+  int packed;          // rows of a tile are (frame, token, query head of the key head)
+  int frame_rows;      // packed: rows of a frame, N * g
+  int tile_frames;     // packed: frames of a tile
+  int cluster;
+  float scale_log2;
+};
+
+__device__ __forceinline__ void flag_error(const CrossParams& p, int where) {
+  if (p.status) atomicOr(p.status, RF_ERR_DEVICE_TIMEOUT | (1 << (8 + where)));
+}
+__device__ __forceinline__ bool all_wait(uint32_t bar, uint32_t parity, volatile int* abort) {
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort, kWaitLimitNs));
+}
+
+// The work of a launch, from the active count on the device.
+struct Work {
+  int A, groups, tiles, pairs, items;  // groups of tiles with keys of their own (frames, or one)
+};
+__device__ __forceinline__ Work make_work(const CrossParams& p) {
+  Work w;
+  w.A = p.rows.frames();
+  w.groups = p.kv_range ? w.A : 1;
+  if (p.packed)
+    w.tiles = p.kv_range ? 1 : (w.A + p.tile_frames - 1) / p.tile_frames;
+  else
+    w.tiles = ((p.kv_range ? p.rows.N : w.A * p.rows.Np) + kBM - 1) / kBM;
+  w.pairs = (w.tiles + 1) / 2;
+  w.items = p.units * w.groups * w.pairs;
+  return w;
+}
+
+// One item, or a cluster CTA's share of it: a pair of query tiles of a head over key rows
+// [begin + 128 j0, ...) of the range [begin, end).
+struct Item {
+  int unit, group, pair;
+  int begin, end, j0, j1;
+};
+__device__ __forceinline__ Item get_item(const CrossParams& p, const Work& w, int i, int rank) {
+  Item t;
+  const int gp = i / w.pairs;
+  t.pair = i - gp * w.pairs;
+  t.unit = gp / w.groups;
+  t.group = gp - t.unit * w.groups;
+  t.begin = 0;
+  t.end = p.L;
+  if (p.kv_range) {
+    const int2 r = p.kv_range[p.rows.frame(t.group)];
+    t.begin = min(max(r.x, 0), p.L);
+    t.end = min(max(r.y, t.begin), p.L);
+  }
+  const int nt = (t.end - t.begin + kBN - 1) / kBN;
+  t.j0 = static_cast<int>(static_cast<int64_t>(nt) * rank / p.cluster);
+  t.j1 = static_cast<int>(static_cast<int64_t>(nt) * (rank + 1) / p.cluster);
+  return t;
+}
+
+// Token and query head of a tile's row; token -1 where the row is none.
+__device__ __forceinline__ int row_of(const CrossParams& p, const Work& w, const Item& t, int tile,
+                                      int row, int& head) {
+  head = t.unit;
+  if (p.packed) {
+    const int al = row / p.frame_rows, rem = row - al * p.frame_rows;
+    const int a = p.kv_range ? t.group : tile * p.tile_frames + al;
+    if (al >= p.tile_frames || a >= w.A) return -1;
+    const int q = rem / p.g;
+    head = t.unit * p.g + (rem - q * p.g);
+    return p.rows.frame(a) * p.rows.N + q;
+  }
+  const int r = tile * kBM + row;
+  if (p.kv_range) return r < p.rows.N ? p.rows.frame(t.group) * p.rows.N + r : -1;
+  if (r >= w.A * p.rows.Np) return -1;
+  const int a = r / p.rows.Np, q = r - a * p.rows.Np;
+  return q < p.rows.N ? p.rows.frame(a) * p.rows.N + q : -1;
+}
+
+// Which keys of tile j a row may see: bit c of word c / 32.  Warp-collective.
+struct KeyBits {
+  uint32_t w[4];
+  __device__ __forceinline__ bool all() const {
+    return (w[0] & w[1] & w[2] & w[3]) == 0xFFFFFFFFu;
+  }
+};
+__device__ __forceinline__ KeyBits key_bits(const CrossParams& p, const Item& t, int j) {
+  KeyBits b;
+  const int k0 = t.begin + j * kBN + (threadIdx.x & 31);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int k = k0 + 32 * i;
+    b.w[i] = __ballot_sync(0xffffffffu, k < t.end && (!p.key_mask || p.key_mask[k] != 0));
+  }
+  return b;
+}
+
+// ---------------------------------------------------------------------------------------
+// TMA producer
+// ---------------------------------------------------------------------------------------
+template <int D>
+__device__ __forceinline__ void load_queries(const CUtensorMap* tmQ, const CUtensorMap* tmBox,
+                                             const CrossParams& p, const Work& w, const Item& t,
+                                             int tile, uint32_t dst, uint32_t bar, bool lead) {
+  using C = Cfg<D>;
+  const int lane = threadIdx.x & 31;
+  if (p.packed) {
+    // one box per frame: its tokens, and for each the query heads of the key head
+    const int a0 = p.kv_range ? t.group : tile * p.tile_frames;
+    const int n = min(p.tile_frames, w.A - a0);
+    if (lead) mbar_arrive_expect_tx(bar, n * p.frame_rows * 128 * C::kHalves);
+    __syncwarp();
+    for (int i = lane; i < n; i += 32)
+#pragma unroll
+      for (int hb = 0; hb < C::kHalves; ++hb)
+        tma_load_3d(dst + hb * C::kHalfBytes + i * p.frame_rows * 128, tmBox, bar, hb * 64,
+                    t.unit * p.g, p.rows.frame(a0 + i) * p.rows.N);
+    __syncwarp();
+    return;
+  }
+  const int r0 = tile * kBM;
+  int whole = -1;  // first token, where the tile's rows are consecutive tokens
+  if (p.kv_range) {
+    whole = p.rows.frame(t.group) * p.rows.N + r0;
+  } else {
+    const int a0 = r0 / p.rows.Np;
+    if (a0 == (min(r0 + kBM, w.A * p.rows.Np) - 1) / p.rows.Np)
+      whole = p.rows.frame(a0) * p.rows.N + (r0 - a0 * p.rows.Np);
+  }
+  if (lead) {
+    mbar_arrive_expect_tx(bar, C::kTileBytes);
+    if (whole >= 0)
+#pragma unroll
+      for (int hb = 0; hb < C::kHalves; ++hb)
+        tma_load_3d(dst + hb * C::kHalfBytes, tmQ, bar, hb * 64, t.unit, whole);
+  }
+  __syncwarp();
+  if (whole < 0) {
+    for (int b = lane; b * p.rows.box < kBM; b += 32) {
+      const int r = r0 + b * p.rows.box;
+      const int a = r / p.rows.Np;
+      // past the active rows: out of bounds, zeros
+      const int tok = a < w.A ? p.rows.frame(a) * p.rows.N + (r - a * p.rows.Np) : p.rows.T;
+#pragma unroll
+      for (int hb = 0; hb < C::kHalves; ++hb)
+        tma_load_3d(dst + hb * C::kHalfBytes + b * p.rows.box * 128, tmBox, bar, hb * 64, t.unit,
+                    tok);
+    }
+    __syncwarp();
+  }
+}
+
+template <int D>
+__device__ __forceinline__ void producer(const CUtensorMap* tmQ, const CUtensorMap* tmBox,
+                                         const CUtensorMap* tmK, const CUtensorMap* tmV,
+                                         const CrossParams& p, const Work& w, int rank,
+                                         uint32_t sQ0, uint32_t sKV0, uint32_t bar0,
+                                         volatile int* abort) {
+  using C = Cfg<D>;
+  auto bar = [&](int i) { return bar0 + 8u * i; };
+  const bool lead = elect_one();
+  int q_cnt[2] = {0, 0};
+  int it = 0;
+  bool ok = true;
+  for (int i = blockIdx.x / p.cluster; ok && i < w.items; i += gridDim.x / p.cluster) {
+    const Item t = get_item(p, w, i, rank);
+    if (t.j0 >= t.j1) continue;
+    const int hk = p.packed ? t.unit : t.unit / p.g;
+    for (int X = 0; ok && X < 2; ++X) {
+      const int tile = 2 * t.pair + X;
+      if (tile >= w.tiles) break;
+      ok = all_wait(bar(C::kQEmpty + X), (q_cnt[X] & 1) ^ 1, abort);
+      if (!ok) break;
+      load_queries<D>(tmQ, tmBox, p, w, t, tile, sQ0 + X * C::kTileBytes, bar(C::kQFull + X), lead);
+      ++q_cnt[X];
+    }
+    for (int j = t.j0; ok && j < t.j1; ++j)
+      for (int kv = 0; kv < 2; ++kv) {
+        const int s = it % C::kSlots;
+        ok = all_wait(bar(C::kKVEmpty + s), ((it / C::kSlots) & 1) ^ 1, abort);
+        if (!ok) break;
+        if (lead) {
+          mbar_arrive_expect_tx(bar(C::kKVFull + s), C::kTileBytes);
+#pragma unroll
+          for (int hb = 0; hb < C::kHalves; ++hb)
+            tma_load_3d(sKV0 + s * C::kTileBytes + hb * C::kHalfBytes, kv ? tmV : tmK,
+                        bar(C::kKVFull + s), hb * 64, hk, t.begin + j * kBN);
+        }
+        __syncwarp();
+        ++it;
+      }
+  }
+  if (!ok && lead) flag_error(p, 0);
+  // every copy has landed
+  for (int s = 0; s < C::kSlots; ++s)
+    if (it > s) mbar_drain(bar(C::kKVFull + s), ((it - 1 - s) / C::kSlots) & 1, kDrainLimitNs);
+  for (int X = 0; X < 2; ++X)
+    if (q_cnt[X] > 0) mbar_drain(bar(C::kQFull + X), (q_cnt[X] - 1) & 1, kDrainLimitNs);
+}
+
+// ---------------------------------------------------------------------------------------
+// V rows of keys that may not be seen (CLEAN; warp 3)
+// ---------------------------------------------------------------------------------------
+template <int D>
+__device__ __forceinline__ void cleaner(const CrossParams& p, const Work& w, int rank, uint32_t sKV0,
+                                        uint8_t* kv, uint32_t bar0, volatile int* abort) {
+  using C = Cfg<D>;
+  auto bar = [&](int i) { return bar0 + 8u * i; };
+  const int lane = threadIdx.x & 31;
+  int it = 1;  // V follows K in the ring
+  for (int i = blockIdx.x / p.cluster; i < w.items; i += gridDim.x / p.cluster) {
+    const Item t = get_item(p, w, i, rank);
+    for (int j = t.j0; j < t.j1; ++j, it += 2) {
+      const KeyBits b = key_bits(p, t, j);
+      const int s = it % C::kSlots;
+      if (!all_wait(bar(C::kKVFull + s), (it / C::kSlots) & 1, abort)) {
+        if (lane == 0) flag_error(p, 1);
+        return;
+      }
+      if (!b.all()) {
+        // a row is 128 bytes in each half: the swizzle moves 16-byte pieces within them
+        uint8_t* tile = kv + s * C::kTileBytes;
+        for (int r = lane; r < kBN; r += 32)
+          if (!((b.w[r >> 5] >> lane) & 1u))
+#pragma unroll
+            for (int hb = 0; hb < C::kHalves; ++hb)
+#pragma unroll
+              for (int q = 0; q < 8; ++q)
+                *reinterpret_cast<uint4*>(tile + hb * C::kHalfBytes + r * 128 + q * 16) =
+                    make_uint4(0u, 0u, 0u, 0u);
+        fence_proxy_async();
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(C::kVClean + s));
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------------------
+// MMA issuer of query tile X
+// ---------------------------------------------------------------------------------------
+template <int D, bool F16>
+__device__ __forceinline__ void mma_qk(uint32_t tS, uint64_t dQ, uint64_t dK) {
+  constexpr uint32_t idesc = idesc_f16(F16, kBM, kBN, 0);
+#pragma unroll
+  for (int k = 0; k < D / 16; ++k) {
+    const uint64_t off = ((k >> 2) * (kBM * 128) + (k & 3) * 32) >> 4;
+    tc_mma_ss(tS, dQ + off, dK + off, idesc, k > 0);
+  }
+}
+template <int D, bool F16, int K0, int K1>
+__device__ __forceinline__ void mma_pv(uint32_t tO, uint32_t tP, uint64_t dV, uint32_t acc) {
+  constexpr uint32_t idesc = idesc_f16(F16, kBM, D, 1);
+#pragma unroll
+  for (int k = K0; k < K1; ++k)
+    tc_mma_ts(tO, tP + k * 8, dV + ((k * 2048) >> 4), idesc, (acc | k) != 0);
+}
+
+template <int D, bool F16, bool CLEAN>
+__device__ __forceinline__ bool mma_issuer(const CrossParams& p, const Work& w, int rank, int X,
+                                           uint32_t tmem, uint32_t sQ0, uint32_t sKV0,
+                                           uint32_t bar0, volatile int* abort) {
+  using C = Cfg<D>;
+  const bool lead = elect_one();
+  auto bar = [&](int i) { return bar0 + 8u * i; };
+  const uint32_t tS = tmem + X * 128, tO = tmem + 256 + X * 128;
+  const uint64_t dQ = smem_desc_sw128(sQ0 + X * C::kTileBytes, 16, 1024);
+  auto dK = [&](int s) { return smem_desc_sw128(sKV0 + s * C::kTileBytes, 16, 1024); };
+  auto dV = [&](int s) { return smem_desc_sw128(sKV0 + s * C::kTileBytes, kBN * 128, 1024); };
+  int q_cnt = 0, it = 0;
+  bool my_turn = X == 0;  // the first turn is tile A's
+  auto wait_k = [&](int i) {
+    return all_wait(bar(C::kKVFull + i % C::kSlots), (i / C::kSlots) & 1, abort);
+  };
+  auto wait_v = [&](int i) {  // cleaned, where a launch has keys that may not be seen
+    return all_wait(bar((CLEAN ? C::kVClean : C::kKVFull) + i % C::kSlots), (i / C::kSlots) & 1,
+                    abort);
+  };
+  auto take_turn = [&]() {
+    if (!my_turn) named_sync(turn_barrier(X), 64);
+    my_turn = false;
+  };
+  for (int i = blockIdx.x / p.cluster; i < w.items; i += gridDim.x / p.cluster) {
+    const Item t = get_item(p, w, i, rank);
+    const int nt = t.j1 - t.j0;
+    if (nt <= 0) continue;
+    const bool both = 2 * t.pair + 1 < w.tiles;
+    bool ok = true;
+    if (X == 1 && !both) {  // no such query tile: only give the K/V slots back
+      for (int n = 0; ok && n < 2 * nt; ++n, ++it) {
+        ok = (n & 1) ? wait_v(it) : wait_k(it);
+        if (ok && lead) mbar_arrive(bar(C::kKVEmpty + it % C::kSlots));
+        __syncwarp();
+      }
+      if (!ok) break;
+      continue;
+    }
+    if (!all_wait(bar(C::kQFull + X), q_cnt & 1, abort)) break;
+    ++q_cnt;
+    if (!wait_k(it) || !__all_sync(0xffffffffu, *abort == 0)) break;
+    tc_fence_after();
+    if (both) take_turn();
+    if (lead) {
+      mma_qk<D, F16>(tS, dQ, dK(it % C::kSlots));
+      tc_commit(bar(C::kSFull + X));
+      if (nt == 1) tc_commit(bar(C::kQEmpty + X));
+      tc_commit(bar(C::kKVEmpty + it % C::kSlots));
+    }
+    __syncwarp();
+    if (both) named_arrive(turn_barrier(X ^ 1), 64);
+    ++it;
+#pragma unroll 1
+    for (int j = 0; j < nt; ++j) {
+      const bool more = j + 1 < nt;
+      const int sV = it % C::kSlots, sK = (it + 1) % C::kSlots;
+      ok = wait_v(it) && (!more || wait_k(it + 1));
+      it += more ? 2 : 1;
+      ok = ok && *abort == 0;
+      if (!__all_sync(0xffffffffu, ok)) break;
+      if (both) take_turn();
+      named_sync(p_barrier(X, 0), kPThreads);
+      tc_fence_after();
+      if (lead) mma_pv<D, F16, 0, 4>(tO, tS, dV(sV), j > 0);
+      __syncwarp();
+      named_sync(p_barrier(X, 1), kPThreads);
+      tc_fence_after();
+      if (lead) {
+        mma_pv<D, F16, 4, 8>(tO, tS, dV(sV), 1);
+        if (more) {
+          mma_qk<D, F16>(tS, dQ, dK(sK));
+          tc_commit(bar(C::kSFull + X));
+          // the item's last Q K^T: the next item's queries may come
+          if (j + 2 == nt) tc_commit(bar(C::kQEmpty + X));
+          tc_commit(bar(C::kKVEmpty + sV));
+          tc_commit(bar(C::kKVEmpty + sK));
+        } else {
+          tc_commit(bar(C::kODone + X));
+          tc_commit(bar(C::kKVEmpty + sV));
+        }
+      }
+      __syncwarp();
+      if (both) named_arrive(turn_barrier(X ^ 1), 64);
+    }
+    if (!ok) break;
+  }
+  // a wait that gave up has raised the flag
+  if (__all_sync(0xffffffffu, *abort == 0)) return true;
+  if (lead) flag_error(p, 2);
+  return false;
+}
+
+// ---------------------------------------------------------------------------------------
+// Softmax and results (128 threads, thread = row of query tile X)
+// ---------------------------------------------------------------------------------------
+template <bool F16>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  return F16 ? pack_f16x2(lo, hi) : pack_bf16x2(lo, hi);
+}
+template <bool F16>
+__device__ __forceinline__ void store8(uint16_t* dst, const float* o, float scale) {
+  *reinterpret_cast<uint4*>(dst) =
+      make_uint4(pack2<F16>(o[0] * scale, o[1] * scale), pack2<F16>(o[2] * scale, o[3] * scale),
+                 pack2<F16>(o[4] * scale, o[5] * scale), pack2<F16>(o[6] * scale, o[7] * scale));
+}
+
+// The running maximum (in units of log2, scaled) and sum of a row over a CTA's K/V tiles of an
+// item, with P left in tensor memory for the MMA warp.  False: a wait gave up.
+template <int D, bool F16, bool CLEAN>
+__device__ __forceinline__ bool softmax_item(const CrossParams& p, const Item& t, int X, uint32_t tS,
+                                             uint32_t tO, uint32_t bar_s, int& s_cnt, float& m_out,
+                                             float& l_out, volatile int* abort) {
+  const float sl2 = p.scale_log2;
+  float m = -INFINITY, l = 0.f;
+  KeyBits bits{};
+  if (CLEAN) bits = key_bits(p, t, t.j0);
+#pragma unroll 1
+  for (int j = t.j0; j < t.j1; ++j) {
+    if (!all_wait(bar_s, s_cnt & 1, abort)) return false;
+    ++s_cnt;
+    tc_fence_after();
+    uint32_t s[kBN];
+#pragma unroll
+    for (int c = 0; c < kBN / 32; ++c)
+      tmem_ld32(tS + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&s[c * 32]));
+    tmem_wait_ld();
+    float* sf = reinterpret_cast<float*>(s);
+    if (CLEAN) {
+      if (!bits.all()) {
+#pragma unroll
+        for (int c = 0; c < kBN; ++c)
+          if (!((bits.w[c >> 5] >> (c & 31)) & 1u)) sf[c] = -INFINITY;
+      }
+      if (j + 1 < t.j1) bits = key_bits(p, t, j + 1);
+    } else if ((j + 1) * kBN > t.end) {
+      const int valid = t.end - j * kBN;
+#pragma unroll
+      for (int c = 0; c < kBN; ++c)
+        if (c >= valid) sf[c] = -INFINITY;
+    }
+    // row maximum over 8 independent chains
+    float mx8[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) mx8[i] = fmaxf(sf[i], sf[i + 8]);
+#pragma unroll
+    for (int c = 16; c < kBN; c += 16)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) mx8[i] = fmax3(mx8[i], sf[c + i], sf[c + 8 + i]);
+    const float mx = fmaxf(fmaxf(fmaxf(mx8[0], mx8[1]), fmaxf(mx8[2], mx8[3])),
+                           fmaxf(fmaxf(mx8[4], mx8[5]), fmaxf(mx8[6], mx8[7])));
+    const float m_new = fmaxf(m, mx * sl2);
+    const bool rescale = __any_sync(0xffffffffu, m_new > m + kRescaleLog2);
+    float fac = 1.f;
+    if (rescale) {
+      // a row that has seen no key yet has m = m_new = -inf: factor 1, not 2^(-inf + inf)
+      fac = m == m_new ? 1.f : ex2_approx(m - m_new);
+      l *= fac;
+      m = m_new;
+    }
+    // O was last written by the previous tile's P V, which completed before S(j) was signalled; at
+    // the first tile it holds nothing yet
+    if (rescale && j > t.j0) {
+#pragma unroll 1
+      for (int c = 0; c < D / 32; ++c) {
+        uint32_t o[32];
+        tmem_ld32(tO + c * 32, o);
+        tmem_wait_ld();
+#pragma unroll
+        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * fac);
+        tmem_st32(tO + c * 32, o);
+      }
+    }
+    // p = 2^(s scale log2 e - m); while every key was masked m is -inf: p = 2^(-inf - 0) = 0.
+    // P is rounded to the inputs' 16 bits for the product (at most 2^-8 of each probability in
+    // bf16, averaged over the keys); the sum l is of the unrounded ones, in fp32.
+    const float nm = m == -INFINITY ? 0.f : -m;
+    const uint64_t sl2x2 = f2_pack(sl2, sl2), nmx2 = f2_pack(nm, nm);
+    uint64_t l4[4] = {0ull, 0ull, 0ull, 0ull};
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      uint32_t pk[16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        float x0, x1;
+        f2_unpack(ffma2(f2_pack(sf[q * 32 + 2 * e], sf[q * 32 + 2 * e + 1]), sl2x2, nmx2), x0, x1);
+        const float p0 = ex2_approx(x0), p1 = ex2_approx(x1);
+        l4[e & 3] = fadd2(l4[e & 3], f2_pack(p0, p1));
+        pk[e] = pack2<F16>(p0, p1);
+      }
+      tmem_st16(tS + q * 16, pk);
+      if (q & 1) {
+        tmem_wait_st();
+        tc_fence_before();
+        named_arrive(p_barrier(X, q >> 1), kPThreads);
+      }
+    }
+    float a, b;
+    f2_unpack(fadd2(fadd2(l4[0], l4[1]), fadd2(l4[2], l4[3])), a, b);
+    l += a + b;
+  }
+  m_out = m;
+  l_out = l;
+  return true;
+}
+
+template <int D, bool F16, bool CLEAN>
+__device__ __forceinline__ bool softmax_group(const CrossParams& p, const Work& w, int rank, int X,
+                                              uint32_t tmem, uint8_t* smem, uint32_t bar0,
+                                              volatile int* abort) {
+  using C = Cfg<D>;
+  auto bar = [&](int i) { return bar0 + 8u * i; };
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int row = (warp & 3) * 32 + lane;  // and lane of tensor memory
+  const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
+  const uint32_t tS = tmem + lane_base + X * 128, tO = tmem + lane_base + 256 + X * 128;
+  int s_cnt = 0, o_cnt = 0;
+  for (int i = blockIdx.x / p.cluster; i < w.items; i += gridDim.x / p.cluster) {
+    const Item t = get_item(p, w, i, rank);
+    const int tile = 2 * t.pair + X;
+    if (tile >= w.tiles) continue;
+    float m = -INFINITY, l = 0.f;
+    if (t.j0 < t.j1) {
+      if (!softmax_item<D, F16, CLEAN>(p, t, X, tS, tO, bar(C::kSFull + X), s_cnt, m, l, abort) ||
+          !all_wait(bar(C::kODone + X), o_cnt & 1, abort)) {
+        if (lane == 0) flag_error(p, 3);
+        return false;
+      }
+      ++o_cnt;
+      tc_fence_after();
+    }
+    if (p.cluster > 1) {
+      // the ring holds the other tile's keys until that one is done too
+      const bool other = t.j0 < t.j1 && 2 * t.pair + 1 < w.tiles;
+      if (other && !all_wait(bar(C::kODone + (X ^ 1)), 0, abort)) {
+        if (lane == 0) flag_error(p, 4);
+        return false;
+      }
+      float4* part = reinterpret_cast<float4*>(smem + C::kOffKV) + X * (D / 4 * 128) + row;
+      if (t.j0 < t.j1)
+#pragma unroll 1
+        for (int c = 0; c < D / 32; ++c) {
+          uint32_t o[32];
+          tmem_ld32(tO + c * 32, o);
+          tmem_wait_ld();
+#pragma unroll
+          for (int q = 0; q < 8; ++q)
+            part[(c * 8 + q) * 128] =
+                make_float4(__uint_as_float(o[4 * q]), __uint_as_float(o[4 * q + 1]),
+                            __uint_as_float(o[4 * q + 2]), __uint_as_float(o[4 * q + 3]));
+        }
+      reinterpret_cast<float2*>(smem)[X * 128 + row] = make_float2(m, l);
+      return true;  // one item per CTA; joined after the cluster's barrier
+    }
+    int head;
+    const int64_t token = row_of(p, w, t, tile, row, head);
+    const bool valid = token >= 0;
+    uint16_t* orow = p.O + token * p.o_row_stride + static_cast<int64_t>(head) * D;
+    // no key: zeros, not 0 * accumulator, which may hold anything
+    const bool none = l == 0.f;
+    const float inv_l = none ? 0.f : 1.0f / l;
+#pragma unroll 1
+    for (int c = 0; c < D / 32; ++c) {
+      uint32_t o[32];
+      tmem_ld32(tO + c * 32, o);
+      tmem_wait_ld();
+      if (none) {
+#pragma unroll
+        for (int e = 0; e < 32; ++e) o[e] = 0u;
+      }
+      if (valid)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          store8<F16>(orow + c * 32 + q * 8, reinterpret_cast<const float*>(o) + q * 8, inv_l);
+    }
+    if (valid && p.lse)
+      p.lse[static_cast<int64_t>(head) * p.rows.T + token] =
+          none ? -INFINITY : (m + __log2f(l)) * 0.69314718055994531f;
+    // (the accumulator is read before the next item's first P, so before its first P V)
+  }
+  return true;
+}
+
+// A split item's rows from all CTAs of the cluster: O = sum_c 2^(m_c - M) O_c / sum_c 2^(m_c - M) l_c.
+// Each CTA takes its share of the columns of every row.
+template <int D, bool F16>
+__device__ __forceinline__ void join(const CrossParams& p, const Work& w, int rank, int X,
+                                     uint32_t sbase) {
+  using C = Cfg<D>;
+  const int i = blockIdx.x / p.cluster;
+  if (i >= w.items) return;
+  const Item t = get_item(p, w, i, rank);
+  const int tile = 2 * t.pair + X;
+  if (tile >= w.tiles) return;
+  const int row = threadIdx.x & 127;
+  int head;
+  const int64_t token = row_of(p, w, t, tile, row, head);
+  if (token < 0) return;
+  float ms[8], M = -INFINITY, Lsum = 0.f;
+  float ls[8];
+#pragma unroll
+  for (int c = 0; c < 8; ++c) {
+    ms[c] = -INFINITY;
+    ls[c] = 0.f;
+    if (c < p.cluster) {
+      const uint32_t at = map_to_rank(sbase + (X * 128 + row) * 8, c);
+      ms[c] = ld_cluster_f(at);
+      ls[c] = ld_cluster_f(at + 4);
+    }
+    M = fmaxf(M, ms[c]);
+  }
+#pragma unroll
+  for (int c = 0; c < 8; ++c) {
+    ms[c] = ls[c] == 0.f ? 0.f : ex2_approx(ms[c] - M);  // now the weight; no key seen: 0
+    Lsum += ms[c] * ls[c];
+  }
+  const bool none = Lsum == 0.f;
+  const float inv = none ? 0.f : 1.0f / Lsum;
+  uint16_t* orow = p.O + token * p.o_row_stride + static_cast<int64_t>(head) * D;
+  // columns in groups of 8: cluster <= 8 = D / 8 at D = 64
+  for (int c8 = rank; c8 < D / 8; c8 += p.cluster) {
+    float acc[8] = {};
+    const uint32_t at = sbase + C::kOffKV + (X * (D / 4 * 128) + c8 * 2 * 128 + row) * 16;
+#pragma unroll
+    for (int c = 0; c < 8; ++c)
+      if (c < p.cluster && ms[c] != 0.f) {
+        const uint32_t r = map_to_rank(at, c);
+        const float4 a = ld_cluster_f4(r), b = ld_cluster_f4(r + 128 * 16);
+        acc[0] = fmaf(ms[c], a.x, acc[0]);
+        acc[1] = fmaf(ms[c], a.y, acc[1]);
+        acc[2] = fmaf(ms[c], a.z, acc[2]);
+        acc[3] = fmaf(ms[c], a.w, acc[3]);
+        acc[4] = fmaf(ms[c], b.x, acc[4]);
+        acc[5] = fmaf(ms[c], b.y, acc[5]);
+        acc[6] = fmaf(ms[c], b.z, acc[6]);
+        acc[7] = fmaf(ms[c], b.w, acc[7]);
+      }
+    store8<F16>(orow + c8 * 8, acc, inv);
+  }
+  if (rank == 0 && p.lse)
+    p.lse[static_cast<int64_t>(head) * p.rows.T + token] =
+        none ? -INFINITY : (M + __log2f(Lsum)) * 0.69314718055994531f;
+}
+
+// A warp that gave up releases the MMA warp that waits for it, until that warp has left (2 s at
+// most: it reads the abort flag, which is up, in every round).
+__device__ __forceinline__ void release_mma(const volatile int* done, int bar_a, int bar_b,
+                                            int threads) {
+  for (int n = 0; n < 2000000 && !__all_sync(0xffffffffu, *done != 0); ++n) {
+    named_arrive(bar_a, threads);
+    if (bar_b != bar_a) named_arrive(bar_b, threads);
+    __nanosleep(1000);
+  }
+}
+
+template <int D, bool F16, bool CLEAN>
+__global__ void __launch_bounds__(kThreads, 1)
+    cross_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmBox,
+                 const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+                 const CrossParams p) {
+  using C = Cfg<D>;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw);
+  const uint32_t sbase = (raw + 1023u) & ~1023u;
+  uint8_t* smem = smem_raw + (sbase - raw);
+  const uint32_t sQ0 = sbase, sKV0 = sbase + C::kOffKV, bar0 = sbase + C::kOffBar;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::kOffMisc);
+  volatile int* abort = reinterpret_cast<volatile int*>(smem + C::kOffMisc + 4);
+  volatile int* mma_done = reinterpret_cast<volatile int*>(smem + C::kOffMisc + 8);  // [2]
+  const int warp = threadIdx.x >> 5;
+  const int rank = p.cluster > 1 ? static_cast<int>(cluster_rank()) : 0;
+
+  __shared__ Work work;
+  if (threadIdx.x == 64) work = make_work(p);
+  if (threadIdx.x == 0) {
+    for (int X = 0; X < 2; ++X) {
+      mbar_init(bar0 + 8 * (C::kQFull + X), 1);
+      mbar_init(bar0 + 8 * (C::kQEmpty + X), 1);
+      mbar_init(bar0 + 8 * (C::kSFull + X), 1);
+      mbar_init(bar0 + 8 * (C::kODone + X), 1);
+      mbar_init(bar0 + 8 * (C::kDrain + X), 1);
+      mma_done[X] = 0;
+    }
+    for (int s = 0; s < C::kSlots; ++s) {
+      mbar_init(bar0 + 8 * (C::kKVFull + s), 1);
+      mbar_init(bar0 + 8 * (C::kKVEmpty + s), 2);
+      mbar_init(bar0 + 8 * (C::kVClean + s), 1);
+    }
+    *abort = 0;
+    fence_mbar_init();
+    tma_prefetch_desc(&tmQ);
+    tma_prefetch_desc(&tmK);
+    tma_prefetch_desc(&tmV);
+  }
+  if (warp == 1) {
+    tmem_alloc(smem_u32(tmem_slot), kTmemCols);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  const Work& w = work;
+
+  // Every warp of warpgroup 0 gives registers back before any softmax warp asks for more, so the
+  // increase below always finds them.
+  if (warp < 4) {
+    reg_dealloc<kRegsControl>();
+    if (warp == 0) {
+      producer<D>(&tmQ, &tmBox, &tmK, &tmV, p, w, rank, sQ0, sKV0, bar0, abort);
+    } else if (warp < 3) {
+      const int X = warp - 1;
+      const bool ok =
+          mma_issuer<D, F16, CLEAN>(p, w, rank, X, tmem, sQ0, sKV0, bar0, abort);
+      __syncwarp();
+      mma_done[X] = 1;  // waits on no named barrier any more
+      if (!ok) release_mma(mma_done + (X ^ 1), turn_barrier(X ^ 1), turn_barrier(X ^ 1), 64);
+      // all MMAs issued so far complete before tensor memory is released
+      if (elect_one()) tc_commit(bar0 + 8 * (C::kDrain + X));
+      __syncwarp();
+      mbar_drain(bar0 + 8 * (C::kDrain + X), 0, kDrainLimitNs);
+    } else if (CLEAN) {
+      cleaner<D>(p, w, rank, sKV0, smem + C::kOffKV, bar0, abort);
+    }
+  } else {
+    reg_alloc<kRegsSoftmax>();
+    const int X = (warp - 4) >> 2;
+    if (!softmax_group<D, F16, CLEAN>(p, w, rank, X, tmem, smem, bar0, abort))
+      release_mma(mma_done + X, p_barrier(X, 0), p_barrier(X, 1), kPThreads);
+  }
+  __syncwarp();
+  if (p.cluster > 1) {
+    cluster_arrive();
+    cluster_wait();
+    if (warp >= 4) join<D, F16>(p, w, rank, (warp - 4) >> 2, sbase);
+    __syncwarp();
+    cluster_arrive();  // every CTA has read the others' rows
+    cluster_wait();
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem, kTmemCols);
+  }
+}
+
+// ---------------------------------------------------------------------------------------
+// Host side
+// ---------------------------------------------------------------------------------------
+struct Maps {
+  CUtensorMap q, box, k, v;
+};
+
+// [rows][heads][d] elements of 16 bits, boxes of 64 x box_heads x box_rows.
+rf_status map_heads(CUtensorMap* m, int dtype, const void* base, int d, int heads, int64_t rows,
+                    int64_t row_stride, int box_heads, int box_rows) {
+  const uint64_t dims[3] = {static_cast<uint64_t>(d), static_cast<uint64_t>(heads),
+                            static_cast<uint64_t>(rows)};
+  const uint64_t strides[2] = {static_cast<uint64_t>(d) * 2, static_cast<uint64_t>(row_stride) * 2};
+  const uint32_t box[3] = {64, static_cast<uint32_t>(box_heads), static_cast<uint32_t>(box_rows)};
+  return make_tensor_map(m, dtype, base, 3, dims, strides, box);
+}
+
+template <int D, bool F16, bool CLEAN>
+rf_status launch(const Maps& m, const CrossParams& p, int grid, const DeviceInfo& di,
+                 cudaStream_t s) {
+  constexpr int smem = Cfg<D>::kSmem;
+  static bool done[64] = {};
+  if (smem > di.max_smem_optin) return fail(RF_ERR_UNSUPPORTED, "rf_cross_attn: shared memory");
+  if (!done[di.device]) {
+    if (cudaError_t e = cudaFuncSetAttribute(cross_kernel<D, F16, CLEAN>,
+                                             cudaFuncAttributeMaxDynamicSharedMemorySize, smem))
+      return fail(RF_ERR_CUDA, "cudaFuncSetAttribute(rf_cross_attn)", e);
+    done[di.device] = true;
+  }
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(static_cast<unsigned>(grid));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = static_cast<unsigned>(p.cluster);
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = p.cluster > 1 ? 1 : 0;
+  if (cudaError_t e = cudaLaunchKernelEx(&cfg, cross_kernel<D, F16, CLEAN>, m.q, m.box, m.k, m.v, p)) {
+    cudaGetLastError();
+    return fail(RF_ERR_CUDA, "rf_cross_attn launch", e);
+  }
+  return RF_OK;
+}
+
+template <int D>
+rf_status launch_dim(bool f16, bool clean, const Maps& m, const CrossParams& p, int grid,
+                     const DeviceInfo& di, cudaStream_t s) {
+  if (f16)
+    return clean ? launch<D, true, true>(m, p, grid, di, s) : launch<D, true, false>(m, p, grid, di, s);
+  return clean ? launch<D, false, true>(m, p, grid, di, s) : launch<D, false, false>(m, p, grid, di, s);
+}
+
+// CTAs per item: the number whose busiest SM has the least to do, in K/V tiles.  A further round of
+// items costs about kRound tiles (start, queries, results), a join kJoin more.
+int cluster_size(int64_t items, int64_t kv_tiles, int sms) {
+  constexpr int64_t kRound = 2, kJoin = 2;
+  int best = 1;
+  int64_t least = 0;
+  for (int c = 1; c <= 8; c *= 2) {
+    if (c > 1 && c > kv_tiles) break;
+    const int64_t rounds = (items * c + sms - 1) / sms;
+    const int64_t cost = rounds * ((kv_tiles + c - 1) / c + kRound + (c > 1 ? kJoin : 0));
+    if (c == 1 || cost < least) {
+      best = c;
+      least = cost;
+    }
+  }
+  return best;
+}
+
+}  // namespace
+}  // namespace rf
+
+using namespace rf;
+
+extern "C" rf_status rf_cross_attn(void* d_O, float* d_lse, const void* d_Q, const void* d_K,
+                                   const void* d_V, int64_t o_row_stride, int64_t q_row_stride,
+                                   int64_t k_row_stride, int64_t v_row_stride, int dtype, int F,
+                                   int N, int H, int Hkv, int d, int L, const int32_t* d_kv_range,
+                                   const uint8_t* d_key_mask, const int32_t* d_active,
+                                   const int32_t* d_counts, float softmax_scale, int32_t* d_status,
+                                   rf_stream_t stream) {
+  if (!d_O || !d_Q) return fail(RF_ERR_INVALID_ARG, "rf_cross_attn: null pointer");
+  if (L < 0 || (L > 0 && (!d_K || !d_V)))
+    return fail(RF_ERR_INVALID_ARG, "rf_cross_attn: keys and values");
+  if (dtype != RF_BF16 && dtype != RF_FP16) return fail(RF_ERR_UNSUPPORTED, "rf_cross_attn: dtype");
+  if (F < 1 || N < 1 || H < 1 || Hkv < 1 || H > 65535 || H % Hkv)
+    return fail(RF_ERR_INVALID_ARG, "rf_cross_attn: sizes >= 1, Hkv divides H");
+  if (d != 64 && d != 128) return fail(RF_ERR_UNSUPPORTED, "rf_cross_attn: head dim 64 or 128");
+  if (!(softmax_scale > 0.f) || !std::isfinite(softmax_scale))
+    return fail(RF_ERR_INVALID_ARG, "rf_cross_attn: softmax scale");
+  if ((d_active == nullptr) != (d_counts == nullptr))
+    return fail(RF_ERR_INVALID_ARG, "rf_cross_attn: active list and counts come together");
+  const int64_t q_row = static_cast<int64_t>(H) * d, kv_row = static_cast<int64_t>(Hkv) * d;
+  if (q_row_stride < q_row || o_row_stride < q_row || k_row_stride < kv_row || v_row_stride < kv_row)
+    return fail(RF_ERR_INVALID_ARG, "rf_cross_attn: row stride below the row's length");
+  if (q_row_stride % 8 || o_row_stride % 8 || k_row_stride % 8 || v_row_stride % 8 ||
+      !aligned16(d_Q) || !aligned16(d_O) || !aligned16(d_K) || !aligned16(d_V))
+    return fail(RF_ERR_MISALIGNED, "rf_cross_attn: bases and row strides on 16-byte boundaries");
+  if ((reinterpret_cast<uintptr_t>(d_kv_range) & 7) || (reinterpret_cast<uintptr_t>(d_lse) & 3))
+    return fail(RF_ERR_MISALIGNED, "rf_cross_attn: ranges on 8-byte boundaries, lse on 4-byte ones");
+  const int64_t T = static_cast<int64_t>(F) * N;
+  const int g = H / Hkv;
+  // packed rows: where they save reading K and V (several heads), or a frame has few tokens
+  const bool packed = static_cast<int64_t>(N) * g <= kBM && (d_kv_range || g > 1 || N < 8);
+  const int box = N < 8 ? 1 : 8;
+  // without a list and without ranges the tokens are one frame; packed rows need the frames
+  const bool one = !d_active && !d_kv_range && !packed;
+  const int64_t Fr = one ? 1 : F, Nr = one ? T : N;
+  const int64_t Np = (Nr + box - 1) / box * box;
+  if (T > 0x7FFFFFFF - 65536 || Fr * Np > 0x7FFFFFFF - 65536 || L > 0x7FFFFFFF - 65536)
+    return fail(RF_ERR_INVALID_ARG, "rf_cross_attn: too many tokens");
+  DeviceInfo di;
+  if (rf_status st = current_device_info(&di)) return st;
+  if (di.cc_major != 10 || di.cc_minor != 3) return fail(RF_ERR_UNSUPPORTED, "needs sm_103");
+
+  CrossParams p{};
+  p.O = static_cast<uint16_t*>(d_O);
+  p.lse = d_lse;
+  p.kv_range = reinterpret_cast<const int2*>(d_kv_range);
+  p.key_mask = d_key_mask;
+  p.status = d_status;
+  p.rows = {d_active, d_counts, static_cast<int>(Fr), static_cast<int>(Nr), static_cast<int>(Np), box,
+            static_cast<int>(T)};
+  p.o_row_stride = o_row_stride;
+  p.L = L;
+  p.g = g;
+  p.packed = packed;
+  p.units = packed ? Hkv : H;
+  p.frame_rows = packed ? N * g : 0;
+  p.tile_frames = packed ? (d_kv_range ? 1 : kBM / p.frame_rows) : 0;
+  p.scale_log2 = static_cast<float>(static_cast<double>(softmax_scale) * 1.4426950408889634);
+
+  // at most, with every frame active
+  const int64_t groups = d_kv_range ? F : 1;
+  const int64_t tiles = packed ? (d_kv_range ? 1 : (Fr + p.tile_frames - 1) / p.tile_frames)
+                               : ((d_kv_range ? Nr : Fr * Np) + kBM - 1) / kBM;
+  const int64_t items = p.units * groups * ((tiles + 1) / 2);
+  if (items > 0x7FFFFFFF / 16) return fail(RF_ERR_INVALID_ARG, "rf_cross_attn: too many rows");
+  const int kv_tiles = (L + kBN - 1) / kBN;
+  p.cluster = cluster_size(items, kv_tiles, di.sm_count);
+  const int grid = p.cluster > 1 ? static_cast<int>(items) * p.cluster
+                                 : static_cast<int>(std::min<int64_t>(items, di.sm_count));
+
+  Maps m;
+  // (no states: nothing is loaded, the maps only have to exist)
+  const void* K = L > 0 ? d_K : d_Q;
+  const void* V = L > 0 ? d_V : d_Q;
+  const int64_t rows_kv = L > 0 ? L : 1;
+  if (rf_status st = map_heads(&m.q, dtype, d_Q, d, H, T, q_row_stride, 1, kBM)) return st;
+  if (rf_status st = packed ? map_heads(&m.box, dtype, d_Q, d, H, T, q_row_stride, g, N)
+                            : map_heads(&m.box, dtype, d_Q, d, H, T, q_row_stride, 1, box))
+    return st;
+  if (rf_status st = map_heads(&m.k, dtype, K, d, Hkv, rows_kv, k_row_stride, 1, kBN)) return st;
+  if (rf_status st = map_heads(&m.v, dtype, V, d, Hkv, rows_kv, v_row_stride, 1, kBN)) return st;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  const bool clean = d_kv_range || d_key_mask;
+  return d == 128 ? launch_dim<128>(dtype == RF_FP16, clean, m, p, grid, di, s)
+                  : launch_dim<64>(dtype == RF_FP16, clean, m, p, grid, di, s);
+}
