@@ -119,7 +119,11 @@ def _ptr(t) -> Optional[int]:
 def _stream(stream) -> Optional[int]:
     if stream is None:
         import torch
-        return torch.cuda.current_stream().cuda_stream
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        if raw is None:
+            return torch.cuda.current_stream().cuda_stream
+        # the same handle without a Stream object: 0.2 us of host time instead of 2.9
+        return raw(torch._C._cuda_getDevice())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -248,30 +252,49 @@ def rf_step_core(mask, cur_slot, alpha, beta, dt, F: int, N: int, E: int, H: int
         _ptr(status), _stream(stream)))
 
 
-_DTYPES = {"torch.bfloat16": 0, "torch.float16": 1, "torch.float32": 2}
+_DTYPES: dict = {}  # torch types -> rf_dtype (torch is imported with the first tensor's call)
 _PAIRINGS = {"interleaved": 0, "half": 1}
 _ACTS = {None: 0, "none": 0, "gelu": 1, "gelu_tanh": 2, "silu": 3}
+_F32 = 2
 
 
-def _dtype(fn: str, *tensors) -> int:
-    """rf_dtype shared by the given tensors (None is skipped)."""
-    kinds = {str(t.dtype) for t in tensors if t is not None}
-    if len(kinds) != 1 or not kinds <= _DTYPES.keys():
-        raise ValueError(f"{fn}: tensors of one type out of bf16, fp16 and fp32, got {sorted(kinds)}")
-    return _DTYPES[kinds.pop()]
+def _dtype(fn: str, t, *same) -> int:
+    """rf_dtype of t; the tensors `same` (None is skipped) have to share it."""
+    if not _DTYPES:
+        import torch
+        _DTYPES.update({torch.bfloat16: 0, torch.float16: 1, torch.float32: _F32})
+    kind = t.dtype
+    for o in same:
+        if o is not None and o.dtype is not kind:
+            raise ValueError(f"{fn}: tensors of one type wanted, got {kind} and {o.dtype}")
+    if kind not in _DTYPES:
+        raise ValueError(f"{fn}: bf16, fp16 or fp32 wanted, got {kind}")
+    return _DTYPES[kind]
 
 
-def _rows(fn: str, name: str, t, *shape) -> int:
-    """Row stride of t, whose rows have to be contiguous; its shape is checked."""
-    if tuple(t.shape) != shape:
+def _rows(fn: str, name: str, t, shape) -> int:
+    """Row stride of t [rows, n] or [rows, heads, d], whose rows have to be contiguous."""
+    if t.shape != shape:
         raise ValueError(f"{fn}: {name} has shape {tuple(t.shape)}, not {shape}")
-    n = 1
-    for size, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
-        if size > 1 and stride != n:
-            raise ValueError(f"{fn}: a row of {name} is not contiguous (strides {t.stride()})")
-        n *= size
+    st = t.stride()
+    n = shape[-1]
+    ok = st[-1] == 1 or n <= 1
+    if len(shape) == 3:
+        ok = ok and (st[1] == n or shape[1] <= 1)
+        n *= shape[1]
+    if not ok:
+        raise ValueError(f"{fn}: a row of {name} is not contiguous (strides {st})")
     # one row: its stride is free, and torch may report any
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), n)
+    return st[0] if shape[0] > 1 or st[0] > n else n
+
+
+def _whole(fn: str, name: str, t, shape, kinds) -> Optional[int]:
+    """Address of an optional contiguous tensor of a given shape and type."""
+    if t is None:
+        return None
+    if t.shape != shape or str(t.dtype) not in kinds or not t.is_contiguous():
+        raise ValueError(f"{fn}: {name} is not a contiguous {shape} of {' or '.join(kinds)}")
+    return t.data_ptr()
 
 
 def rf_rope_table(pos, dim: int, base: float = 10000.0):
@@ -287,23 +310,25 @@ def rf_rope(Yq, Xq, Yk, Xk, F: int, gh: int, gw: int, dims, tables, pairing: str
     """Rotary positions of queries Xq [F*gh*gw, Hq, d] and keys Xk (or None) into Yq and Yk, which
     may be the inputs themselves.  dims: rotated elements (time, height, width); tables: the three
     axes' device tables of rf_rope_table, None where dims is 0."""
-    fn, T = "rf_rope", F * gh * gw
-    d = Xq.shape[-1]
-    keys = Xk is not None
-    dt = _dtype(fn, Yq, Xq, *((Yk, Xk) if keys else ()))
-    side = []
-    for y, x, name in ((Yq, Xq, "q"),) + (((Yk, Xk, "k"),) if keys else ()):
-        shape = (T, x.shape[1], d)
-        side += [_ptr(y), _ptr(x), _rows(fn, "Y" + name, y, *shape), _rows(fn, "X" + name, x, *shape),
-                 x.shape[1]]
-    for n, dim, t in zip((F, gh, gw), dims, tables):
-        if t is not None and (tuple(t.shape) != (n, dim // 2, 2) or _dtype(fn, t) != 2
-                              or not t.is_contiguous()):
-            raise ValueError(f"{fn}: a table is not a contiguous fp32 [{n}, {dim // 2}, 2]")
+    fn = "rf_rope"
+    shape = (F * gh * gw, *Xq.shape[1:])
+    dim_t, dim_h, dim_w = dims
+    t, h, w = tables
+    yq, xq = _rows(fn, "Yq", Yq, shape), _rows(fn, "Xq", Xq, shape)
+    kp = (None, None, 0, 0, 0)
+    if Xk is not None:
+        ks = (shape[0], Xk.shape[1], shape[2])
+        kp = (Yk.data_ptr(), Xk.data_ptr(), _rows(fn, "Yk", Yk, ks), _rows(fn, "Xk", Xk, ks), ks[1])
+    elif Yk is not None:
+        raise ValueError(f"{fn}: Yk without Xk")
+    dt = _dtype(fn, Xq, Yq, Xk, Yk)
+    f32 = ("torch.float32",)
     _check(fn, load().rf_rope(
-        *side, *(() if keys else (None, None, 0, 0, 0)), dt, F, gh, gw, d, *dims,
-        *(_ptr(t) for t in tables), _PAIRINGS[pairing], int(inverse), _ptr(active), _ptr(counts),
-        _stream(stream)))
+        Yq.data_ptr(), Xq.data_ptr(), yq, xq, shape[1], *kp, dt, F, gh, gw, shape[2], dim_t, dim_h,
+        dim_w, _whole(fn, "time's table", t, (F, dim_t // 2, 2), f32),
+        _whole(fn, "height's table", h, (gh, dim_h // 2, 2), f32),
+        _whole(fn, "width's table", w, (gw, dim_w // 2, 2), f32), _PAIRINGS[pairing], inverse,
+        _ptr(active), _ptr(counts), _stream(stream)))
 
 
 def rf_cross_attn(O, lse, Q, K, V, F: int, N: int, softmax_scale: float, kv_range=None,
@@ -314,19 +339,18 @@ def rf_cross_attn(O, lse, Q, K, V, F: int, N: int, softmax_scale: float, kv_rang
     zero = not seen; lse fp32 [H, F*N] or None."""
     fn = "rf_cross_attn"
     H, d = Q.shape[1:]
-    L, Hkv = K.shape[:2]
-    dt = _dtype(fn, O, Q, K, V)
-    for name, t, shape, kinds in (("lse", lse, (H, F * N), ("torch.float32",)),
-                                  ("kv_range", kv_range, (F, 2), ("torch.int32",)),
-                                  ("key_mask", key_mask, (L,), ("torch.uint8", "torch.bool"))):
-        if t is not None and (tuple(t.shape) != shape or str(t.dtype) not in kinds
-                              or not t.is_contiguous()):
-            raise ValueError(f"{fn}: {name} is not a contiguous {shape} of {' or '.join(kinds)}")
+    kv = tuple(K.shape)
+    L, Hkv, _ = kv
+    rows = (F * N, H, d)
+    if kv[2] != d:
+        raise ValueError(f"{fn}: head dim {d} of Q, {kv[2]} of K")
     _check(fn, load().rf_cross_attn(
-        _ptr(O), _ptr(lse), _ptr(Q), _ptr(K), _ptr(V), _rows(fn, "O", O, F * N, H, d),
-        _rows(fn, "Q", Q, F * N, H, d), _rows(fn, "K", K, L, Hkv, d), _rows(fn, "V", V, L, Hkv, d),
-        dt, F, N, H, Hkv, d, L, _ptr(kv_range), _ptr(key_mask), _ptr(active), _ptr(counts),
-        float(softmax_scale), _ptr(status), _stream(stream)))
+        O.data_ptr(), _whole(fn, "lse", lse, (H, F * N), ("torch.float32",)), Q.data_ptr(),
+        K.data_ptr(), V.data_ptr(), _rows(fn, "O", O, rows), _rows(fn, "Q", Q, rows),
+        _rows(fn, "K", K, kv), _rows(fn, "V", V, kv), _dtype(fn, Q, O, K, V), F, N, H, Hkv, d, L,
+        _whole(fn, "kv_range", kv_range, (F, 2), ("torch.int32",)),
+        _whole(fn, "key_mask", key_mask, (L,), ("torch.uint8", "torch.bool")), _ptr(active),
+        _ptr(counts), softmax_scale, _ptr(status), _stream(stream)))
 
 
 def rf_linear(Y, X, W, F: int, N: int, bias=None, act=None, gate=None, residual=None, active=None,
@@ -337,24 +361,28 @@ def rf_linear(Y, X, W, F: int, N: int, bias=None, act=None, gate=None, residual=
     in that type or fp32; gate fp32 [d_out], or [F, d_out] for one per frame; act None, "gelu",
     "gelu_tanh" or "silu".  residual may be Y."""
     fn = "rf_linear"
+    T = F * N
     d_out, d_in = W.shape
     dt, out = _dtype(fn, X, W, bias), _dtype(fn, Y, residual)
-    if bias is not None and (tuple(bias.shape) != (d_out,) or not bias.is_contiguous()):
-        raise ValueError(f"{fn}: bias is not a contiguous [{d_out}]")
-    gate_stride = 0
+    b = g = r = None
+    gate_stride = r_stride = 0
+    if bias is not None:
+        _rows(fn, "bias", bias[None] if bias.dim() == 1 else bias, (1, d_out))
+        b = bias.data_ptr()
     if gate is not None:
-        if _dtype(fn, gate) != 2:
+        if _dtype(fn, gate) != _F32:
             raise ValueError(f"{fn}: gate is not fp32")
         if gate.dim() == 1:
-            _rows(fn, "gate", gate[None], 1, d_out)
+            _rows(fn, "gate", gate[None], (1, d_out))
         else:
-            gate_stride = _rows(fn, "gate", gate, F, d_out)
+            gate_stride = _rows(fn, "gate", gate, (F, d_out))
+        g = gate.data_ptr()
+    if residual is not None:
+        r, r_stride = residual.data_ptr(), _rows(fn, "residual", residual, (T, d_out))
     _check(fn, load().rf_linear(
-        _ptr(Y), _rows(fn, "Y", Y, F * N, d_out), out, _ptr(X), _rows(fn, "X", X, F * N, d_in),
-        _ptr(W), _rows(fn, "W", W, d_out, d_in), dt, F, N, d_in, d_out, _ptr(bias), _ACTS[act],
-        _ptr(gate), gate_stride, _ptr(residual),
-        0 if residual is None else _rows(fn, "residual", residual, F * N, d_out), _ptr(active),
-        _ptr(counts), _ptr(status), _stream(stream)))
+        Y.data_ptr(), _rows(fn, "Y", Y, (T, d_out)), out, X.data_ptr(), _rows(fn, "X", X, (T, d_in)),
+        W.data_ptr(), _rows(fn, "W", W, (d_out, d_in)), dt, F, N, d_in, d_out, b, _ACTS[act], g,
+        gate_stride, r, r_stride, _ptr(active), _ptr(counts), _ptr(status), _stream(stream)))
 
 
 def rf_pipeline_create(F: int, N: int, H: int, d: int, E: int, plan: dict, z2, K0, V0,
