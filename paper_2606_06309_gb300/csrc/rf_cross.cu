@@ -33,6 +33,7 @@
 #include <cmath>
 
 #include "rf_ops.h"
+#include "rf_rows.cuh"
 #include "rf_tc_ptx.cuh"
 
 namespace rf {
@@ -66,7 +67,8 @@ struct Cfg {
                        kVClean = 4 + 2 * kSlots, kSFull = 4 + 3 * kSlots, kODone = kSFull + 2,
                        kDrain = kODone + 2, kBars = kDrain + 2;
   static constexpr int kOffMisc = kOffBar + kBars * 8;  // tensor memory address, abort, MMA done [2]
-  static constexpr int kSmem = kOffMisc + 32 + 1024;    // + slack to align the base
+  static constexpr int kOffList = kOffMisc + 32;        // boxes of a query tile
+  static constexpr int kSmem = kOffList + 128 * 8 + 1024;  // + slack to align the base
   // A split item's rows: [tile][D / 4][128] float4 over the K/V ring, {max, sum} [tile][128] over
   // the queries
   static_assert(2 * 128 * D * 4 <= kSlots * kTileBytes, "partial rows fit the ring");
@@ -178,64 +180,54 @@ __device__ __forceinline__ KeyBits key_bits(const CrossParams& p, const Item& t,
 // ---------------------------------------------------------------------------------------
 // TMA producer
 // ---------------------------------------------------------------------------------------
+// The maps of Q: boxes of a tile, of kBoxRows rows, and of rows.unit rows or (packed) a frame.
+struct QueryMaps {
+  const CUtensorMap *whole, *many, *unit;
+};
 template <int D>
-__device__ __forceinline__ void load_queries(const CUtensorMap* tmQ, const CUtensorMap* tmBox,
-                                             const CrossParams& p, const Work& w, const Item& t,
-                                             int tile, uint32_t dst, uint32_t bar, bool lead) {
+__device__ __forceinline__ void load_queries(const QueryMaps& maps, const CrossParams& p,
+                                             const Work& w, const Item& t, int tile, int2* list,
+                                             uint32_t dst, uint32_t bar, bool lead) {
   using C = Cfg<D>;
-  const int lane = threadIdx.x & 31;
+  auto load = [&](const CUtensorMap* m, int row, int head, int tok) {
+#pragma unroll
+    for (int hb = 0; hb < C::kHalves; ++hb)
+      tma_load_3d(dst + hb * C::kHalfBytes + row * 128, m, bar, hb * 64, head, tok);
+  };
   if (p.packed) {
     // one box per frame: its tokens, and for each the query heads of the key head
     const int a0 = p.kv_range ? t.group : tile * p.tile_frames;
     const int n = min(p.tile_frames, w.A - a0);
-    if (lead) mbar_arrive_expect_tx(bar, n * p.frame_rows * 128 * C::kHalves);
-    __syncwarp();
-    for (int i = lane; i < n; i += 32)
-#pragma unroll
-      for (int hb = 0; hb < C::kHalves; ++hb)
-        tma_load_3d(dst + hb * C::kHalfBytes + i * p.frame_rows * 128, tmBox, bar, hb * 64,
-                    t.unit * p.g, p.rows.frame(a0 + i) * p.rows.N);
-    __syncwarp();
-    return;
-  }
-  const int r0 = tile * kBM;
-  int whole = -1;  // first token, where the tile's rows are consecutive tokens
-  if (p.kv_range) {
-    whole = p.rows.frame(t.group) * p.rows.N + r0;
+    if (lead) {
+      mbar_arrive_expect_tx(bar, n * p.frame_rows * 128 * C::kHalves);
+      for (int i = 0; i < n; ++i)
+        load(maps.unit, i * p.frame_rows, t.unit * p.g, p.rows.frame(a0 + i) * p.rows.N);
+    }
+  } else if (p.kv_range) {
+    if (lead) {
+      mbar_arrive_expect_tx(bar, C::kTileBytes);
+      load(maps.whole, 0, t.unit, p.rows.frame(t.group) * p.rows.N + tile * kBM);
+    }
   } else {
-    const int a0 = r0 / p.rows.Np;
-    if (a0 == (min(r0 + kBM, w.A * p.rows.Np) - 1) / p.rows.Np)
-      whole = p.rows.frame(a0) * p.rows.N + (r0 - a0 * p.rows.Np);
-  }
-  if (lead) {
-    mbar_arrive_expect_tx(bar, C::kTileBytes);
-    if (whole >= 0)
-#pragma unroll
-      for (int hb = 0; hb < C::kHalves; ++hb)
-        tma_load_3d(dst + hb * C::kHalfBytes, tmQ, bar, hb * 64, t.unit, whole);
+    const RowBoxes x = list_boxes(p.rows, w.A * p.rows.Np, tile * kBM, kBM, list);
+    if (lead) {
+      mbar_arrive_expect_tx(bar, x.rows * 128 * C::kHalves);
+      if (x.n_many + x.n_unit == 0) load(maps.whole, 0, t.unit, x.tok);
+#pragma unroll 2
+      for (int i = 0; i < x.n_many; ++i) load(maps.many, list[i].y, t.unit, list[i].x);
+#pragma unroll 2
+      for (int i = 0; i < x.n_unit; ++i)
+        load(maps.unit, list[kBM - 1 - i].y, t.unit, list[kBM - 1 - i].x);
+    }
   }
   __syncwarp();
-  if (whole < 0) {
-    for (int b = lane; b * p.rows.box < kBM; b += 32) {
-      const int r = r0 + b * p.rows.box;
-      const int a = r / p.rows.Np;
-      // past the active rows: out of bounds, zeros
-      const int tok = a < w.A ? p.rows.frame(a) * p.rows.N + (r - a * p.rows.Np) : p.rows.T;
-#pragma unroll
-      for (int hb = 0; hb < C::kHalves; ++hb)
-        tma_load_3d(dst + hb * C::kHalfBytes + b * p.rows.box * 128, tmBox, bar, hb * 64, t.unit,
-                    tok);
-    }
-    __syncwarp();
-  }
 }
 
 template <int D>
-__device__ __forceinline__ void producer(const CUtensorMap* tmQ, const CUtensorMap* tmBox,
-                                         const CUtensorMap* tmK, const CUtensorMap* tmV,
-                                         const CrossParams& p, const Work& w, int rank,
-                                         uint32_t sQ0, uint32_t sKV0, uint32_t bar0,
-                                         volatile int* abort) {
+__device__ __forceinline__ void producer(const QueryMaps& maps, const CUtensorMap* tmK,
+                                         const CUtensorMap* tmV, const CrossParams& p,
+                                         const Work& w, int rank, int2* list, uint32_t sQ0,
+                                         uint32_t sKV0, uint32_t bar0, volatile int* abort) {
   using C = Cfg<D>;
   auto bar = [&](int i) { return bar0 + 8u * i; };
   const bool lead = elect_one();
@@ -251,7 +243,7 @@ __device__ __forceinline__ void producer(const CUtensorMap* tmQ, const CUtensorM
       if (tile >= w.tiles) break;
       ok = all_wait(bar(C::kQEmpty + X), (q_cnt[X] & 1) ^ 1, abort);
       if (!ok) break;
-      load_queries<D>(tmQ, tmBox, p, w, t, tile, sQ0 + X * C::kTileBytes, bar(C::kQFull + X), lead);
+      load_queries<D>(maps, p, w, t, tile, list, sQ0 + X * C::kTileBytes, bar(C::kQFull + X), lead);
       ++q_cnt[X];
     }
     for (int j = t.j0; ok && j < t.j1; ++j)
@@ -693,9 +685,9 @@ __device__ __forceinline__ void release_mma(const volatile int* done, int bar_a,
 
 template <int D, bool F16, bool CLEAN>
 __global__ void __launch_bounds__(kThreads, 1)
-    cross_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmBox,
-                 const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
-                 const CrossParams p) {
+    cross_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmMany,
+                 const __grid_constant__ CUtensorMap tmUnit, const __grid_constant__ CUtensorMap tmK,
+                 const __grid_constant__ CUtensorMap tmV, const CrossParams p) {
   using C = Cfg<D>;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
@@ -745,7 +737,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (warp < 4) {
     reg_dealloc<kRegsControl>();
     if (warp == 0) {
-      producer<D>(&tmQ, &tmBox, &tmK, &tmV, p, w, rank, sQ0, sKV0, bar0, abort);
+      producer<D>({&tmQ, &tmMany, &tmUnit}, &tmK, &tmV, p, w, rank,
+                  reinterpret_cast<int2*>(smem + C::kOffList), sQ0, sKV0, bar0, abort);
     } else if (warp < 3) {
       const int X = warp - 1;
       const bool ok =
@@ -787,7 +780,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 // Host side
 // ---------------------------------------------------------------------------------------
 struct Maps {
-  CUtensorMap q, box, k, v;
+  CUtensorMap q, many, unit, k, v;
 };
 
 // [rows][heads][d] elements of 16 bits, boxes of 64 x box_heads x box_rows.
@@ -823,7 +816,8 @@ rf_status launch(const Maps& m, const CrossParams& p, int grid, const DeviceInfo
   attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = p.cluster > 1 ? 1 : 0;
-  if (cudaError_t e = cudaLaunchKernelEx(&cfg, cross_kernel<D, F16, CLEAN>, m.q, m.box, m.k, m.v, p)) {
+  if (cudaError_t e = cudaLaunchKernelEx(&cfg, cross_kernel<D, F16, CLEAN>, m.q, m.many, m.unit, m.k,
+                                         m.v, p)) {
     cudaGetLastError();
     return fail(RF_ERR_CUDA, "rf_cross_attn launch", e);
   }
@@ -891,11 +885,11 @@ extern "C" rf_status rf_cross_attn(void* d_O, float* d_lse, const void* d_Q, con
   const int g = H / Hkv;
   // packed rows: where they save reading K and V (several heads), or a frame has few tokens
   const bool packed = static_cast<int64_t>(N) * g <= kBM && (d_kv_range || g > 1 || N < 8);
-  const int box = N < 8 ? 1 : 8;
   // without a list and without ranges the tokens are one frame; packed rows need the frames
   const bool one = !d_active && !d_kv_range && !packed;
   const int64_t Fr = one ? 1 : F, Nr = one ? T : N;
-  const int64_t Np = (Nr + box - 1) / box * box;
+  const int unit = row_unit(Nr);
+  const int64_t Np = (Nr + unit - 1) / unit * unit;
   if (T > 0x7FFFFFFF - 65536 || Fr * Np > 0x7FFFFFFF - 65536 || L > 0x7FFFFFFF - 65536)
     return fail(RF_ERR_INVALID_ARG, "rf_cross_attn: too many tokens");
   DeviceInfo di;
@@ -908,7 +902,7 @@ extern "C" rf_status rf_cross_attn(void* d_O, float* d_lse, const void* d_Q, con
   p.kv_range = reinterpret_cast<const int2*>(d_kv_range);
   p.key_mask = d_key_mask;
   p.status = d_status;
-  p.rows = {d_active, d_counts, static_cast<int>(Fr), static_cast<int>(Nr), static_cast<int>(Np), box,
+  p.rows = {d_active, d_counts, static_cast<int>(Fr), static_cast<int>(Nr), static_cast<int>(Np), unit,
             static_cast<int>(T)};
   p.o_row_stride = o_row_stride;
   p.L = L;
@@ -936,9 +930,13 @@ extern "C" rf_status rf_cross_attn(void* d_O, float* d_lse, const void* d_Q, con
   const void* V = L > 0 ? d_V : d_Q;
   const int64_t rows_kv = L > 0 ? L : 1;
   if (rf_status st = map_heads(&m.q, dtype, d_Q, d, H, T, q_row_stride, 1, kBM)) return st;
-  if (rf_status st = packed ? map_heads(&m.box, dtype, d_Q, d, H, T, q_row_stride, g, N)
-                            : map_heads(&m.box, dtype, d_Q, d, H, T, q_row_stride, 1, box))
-    return st;
+  m.many = m.unit = m.q;
+  if (packed) {
+    if (rf_status st = map_heads(&m.unit, dtype, d_Q, d, H, T, q_row_stride, g, N)) return st;
+  } else if (Fr > 1 && !d_kv_range) {  // a tile can lie across frames
+    if (rf_status st = map_heads(&m.many, dtype, d_Q, d, H, T, q_row_stride, 1, kBoxRows)) return st;
+    if (rf_status st = map_heads(&m.unit, dtype, d_Q, d, H, T, q_row_stride, 1, unit)) return st;
+  }
   if (rf_status st = map_heads(&m.k, dtype, K, d, Hkv, rows_kv, k_row_stride, 1, kBN)) return st;
   if (rf_status st = map_heads(&m.v, dtype, V, d, Hkv, rows_kv, v_row_stride, 1, kBN)) return st;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);

@@ -15,9 +15,11 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 
 #include "rf_ops.h"
+#include "rf_rows.cuh"
 #include "rf_tc_ptx.cuh"
 
 namespace rf {
@@ -26,7 +28,6 @@ namespace {
 constexpr uint32_t kWaitLimitNs = 2000000000u;    // 2 s: no legitimate wait comes close
 constexpr uint64_t kDrainLimitNs = 200000000ull;  // 0.2 s for what is in flight at teardown
 constexpr int kBlockK = 64;                       // columns of K per stage: 128 bytes, one swizzle atom
-constexpr int kMaxBoxes = 8;                      // gathered boxes per lane: 256 rows / 32 lanes
 
 // ---------------------------------------------------------------------------------------
 // Epilogue
@@ -201,50 +202,26 @@ __device__ __forceinline__ int row_token(const LinearParams& p, int r, int& fram
   return q < p.rows.N ? token : -1;
 }
 
-// How the n rows from row r0 are loaded: one box if they lie in one frame, else boxes of
-// rows.box rows, box lane + 32 i by its first token.
-struct RowTile {
-  bool whole;
-  int tok[kMaxBoxes];
+// The maps of X: boxes of a whole tile, of kBoxRows rows and of rows.unit rows.
+struct RowMaps {
+  const CUtensorMap *whole, *many, *unit;
 };
-__device__ __forceinline__ RowTile find_rows(const RowMap& m, int R, int r0, int n) {
-  RowTile t;
-  const int a0 = r0 / m.Np;
-  t.whole = r0 >= R || a0 == (min(r0 + n, R) - 1) / m.Np;
-  if (t.whole) {
-    // (rows past the frame read the following tokens, past the last one zeros: never stored)
-    t.tok[0] = r0 >= R ? m.T : m.frame(a0) * m.N + (r0 - a0 * m.Np);
-    return t;
-  }
-#pragma unroll
-  for (int i = 0; i < kMaxBoxes; ++i) {
-    const int r = r0 + ((threadIdx.x & 31) + 32 * i) * m.box;
-    const int a = r / m.Np;
-    t.tok[i] = r < R ? m.frame(a) * m.N + (r - a * m.Np) : m.T;
-  }
-  return t;
-}
-// Issue the copies of one k block of the tile into dst (all lanes; the bytes are announced before).
+// Issue the copies of one k block of a tile of n rows (the bytes are announced before; one thread).
 template <bool PAIR>
-__device__ __forceinline__ void load_rows(const RowTile& t, const CUtensorMap* whole,
-                                          const CUtensorMap* boxes, int box, int n, uint32_t dst,
-                                          uint32_t bar, int k0, bool lead) {
-  if (t.whole) {
-    if (lead) {
-      if (PAIR) tma_load_2d_pair(dst, whole, bar, k0, t.tok[0]);
-      else tma_load_2d(dst, whole, bar, k0, t.tok[0]);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < kMaxBoxes; ++i) {
-      const int b = (threadIdx.x & 31) + 32 * i;
-      if (b * box < n) {
-        if (PAIR) tma_load_2d_pair(dst + b * box * 128, boxes, bar, k0, t.tok[i]);
-        else tma_load_2d(dst + b * box * 128, boxes, bar, k0, t.tok[i]);
-      }
-    }
+__device__ __forceinline__ void load_rows(const RowBoxes& x, const int2* list, int n,
+                                          const RowMaps& maps, uint32_t dst, uint32_t bar, int k0) {
+  auto load = [&](const CUtensorMap* m, int row, int tok) {
+    if (PAIR) tma_load_2d_pair(dst + row * 128, m, bar, k0, tok);
+    else tma_load_2d(dst + row * 128, m, bar, k0, tok);
+  };
+  if (x.n_many + x.n_unit == 0) {
+    load(maps.whole, 0, x.tok);
+    return;
   }
-  __syncwarp();
+#pragma unroll 2
+  for (int i = 0; i < x.n_many; ++i) load(maps.many, list[i].y, list[i].x);
+#pragma unroll 2
+  for (int i = 0; i < x.n_unit; ++i) load(maps.unit, list[n - 1 - i].y, list[n - 1 - i].x);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -267,7 +244,8 @@ struct PairCfg {
                        kBarAccEmpty = kBarAccFull + 2, kBars = kBarAccEmpty + 2;
   static constexpr int kOffBar = kStages * kStageBytes;
   static constexpr int kOffMisc = kOffBar + kBars * 8;
-  static constexpr int kSmem = kOffMisc + 16 + 1024;
+  static constexpr int kOffList = kOffMisc + 16;
+  static constexpr int kSmem = kOffList + 128 * 8 + 1024;
   static constexpr uint32_t kTmemCols = 2 * BN;
 };
 
@@ -284,8 +262,9 @@ __device__ __forceinline__ void tile_at(int t, int m_tiles, int n_tiles, int& m,
 
 template <int BN>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
-    pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmBox,
-                const __grid_constant__ CUtensorMap tmW, const LinearParams p) {
+    pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmMany,
+                const __grid_constant__ CUtensorMap tmUnit, const __grid_constant__ CUtensorMap tmW,
+                const LinearParams p) {
   using C = PairCfg<BN>;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
@@ -330,13 +309,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
 
   if (warp == 0) {
     const bool lead = elect_one();
+    int2* list = reinterpret_cast<int2*>(smem + C::kOffList);
     int it = 0;
     bool ok = true;
     for (int t = pair; ok && t < tiles; t += pairs) {
       int m, n;
       tile_at(t, m_tiles, p.n_tiles, m, n);
-      const RowTile rt = find_rows(p.rows, R, m * 256 + rank * 128, 128);
+      const RowBoxes x = list_boxes(p.rows, R, m * 256 + rank * 128, 128, list);
       const int w0 = n * BN + rank * (BN / 2);
+      // of both CTAs, the other one's rows included
+      const int bytes = 2 * C::kBBytes +
+                        (x.rows + (rank == 0 ? boxed_rows(p.rows, R, m * 256 + 128, 128) : 0)) * 128;
       for (int kb = 0; kb < p.kblocks; ++kb, ++it) {
         const int s = it % C::kStages;
         if (!__all_sync(0xffffffffu,
@@ -349,10 +332,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
         // the first CTA's barrier counts the bytes of both
         const uint32_t full = map_to_rank(bar(C::kBarFull + s), 0);
         const uint32_t dst = sbase + s * C::kStageBytes;
-        if (lead && rank == 0) mbar_arrive_expect_tx(bar(C::kBarFull + s), 2 * C::kStageBytes);
-        if (lead) tma_load_2d_pair(dst + C::kABytes, &tmW, full, kb * kBlockK, w0);
+        if (lead) {
+          if (rank == 0) mbar_arrive_expect_tx(bar(C::kBarFull + s), bytes);
+          tma_load_2d_pair(dst + C::kABytes, &tmW, full, kb * kBlockK, w0);
+          load_rows<true>(x, list, 128, {&tmX, &tmMany, &tmUnit}, dst, full, kb * kBlockK);
+        }
         __syncwarp();
-        load_rows<true>(rt, &tmX, &tmBox, p.rows.box, 128, dst, full, kb * kBlockK, lead);
       }
     }
     // every stage that was filled has been given back (so no arrival from the other CTA is still
@@ -458,11 +443,12 @@ constexpr int kSplitRing = 212992;  // bytes for stages; the sums of a split tak
 constexpr int kSplitBarFull = 0, kSplitBarEmpty = kSplitMaxStages,
               kSplitBarAcc = 2 * kSplitMaxStages, kSplitBars = kSplitBarAcc + 1;
 constexpr int kSplitOffBar = kSplitRing, kSplitOffMisc = kSplitOffBar + kSplitBars * 8,
-              kSplitSmem = kSplitOffMisc + 16 + 1024;
+              kSplitOffList = kSplitOffMisc + 16, kSplitSmem = kSplitOffList + 256 * 8 + 1024;
 
 __global__ void __launch_bounds__(kSplitThreads, 1)
-    split_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmBox,
-                 const __grid_constant__ CUtensorMap tmW, const LinearParams p) {
+    split_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmMany,
+                 const __grid_constant__ CUtensorMap tmUnit, const __grid_constant__ CUtensorMap tmW,
+                 const LinearParams p) {
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t sbase = (raw + 1023u) & ~1023u;
@@ -505,7 +491,8 @@ __global__ void __launch_bounds__(kSplitThreads, 1)
 
   if (warp == 0) {
     const bool lead = elect_one();
-    const RowTile rt = find_rows(p.rows, R, r0, BT);
+    int2* list = reinterpret_cast<int2*>(smem + kSplitOffList);
+    const RowBoxes x = list_boxes(p.rows, R, r0, BT, list);
     int it = 0;
     for (int kb = kb0; kb < kb1; ++kb, ++it) {
       const int s = it % p.stages;
@@ -516,12 +503,12 @@ __global__ void __launch_bounds__(kSplitThreads, 1)
       }
       const uint32_t dst = sbase + s * stage_bytes;
       if (lead) {
-        mbar_arrive_expect_tx(bar(kSplitBarFull + s), stage_bytes);
+        mbar_arrive_expect_tx(bar(kSplitBarFull + s), 16384 + x.rows * 128);
         tma_load_2d(dst, &tmW, bar(kSplitBarFull + s), kb * kBlockK, n * 128);
+        load_rows<false>(x, list, BT, {&tmX, &tmMany, &tmUnit}, dst + 16384,
+                         bar(kSplitBarFull + s), kb * kBlockK);
       }
       __syncwarp();
-      load_rows<false>(rt, &tmX, &tmBox, p.rows.box, BT, dst + 16384, bar(kSplitBarFull + s),
-                       kb * kBlockK, lead);
     }
     for (int s = 0; s < p.stages; ++s)  // every copy has landed
       if (it > s) mbar_drain(bar(kSplitBarFull + s), ((it - 1 - s) / p.stages) & 1, kDrainLimitNs);
@@ -646,19 +633,48 @@ int split_ranges(int64_t tiles, int kblocks, int sms) {
   return c;
 }
 
+struct Maps {
+  CUtensorMap x, many, unit, w;
+};
+// The maps of a launch with tiles of `tile` rows of X; w_rows rows of W per box.  Boxes of part of a
+// tile are made where a tile can lie across frames.
+rf_status make_maps(Maps* t, const LinearParams& p, const void* d_X, int64_t x_stride,
+                    const void* d_W, int64_t w_stride, int d_in, int tile, int w_rows) {
+  const int dt = p.epi.in_dtype;
+  if (rf_status st = map_2d(&t->x, dt, d_X, d_in, p.rows.T, x_stride, tile)) return st;
+  if (rf_status st = map_2d(&t->w, dt, d_W, d_in, p.epi.n_out, w_stride, w_rows)) return st;
+  t->many = t->unit = t->x;
+  if (p.rows.F == 1) return RF_OK;
+  if (p.rows.unit > 1 && p.rows.Np >= kBoxRows)
+    if (rf_status st = map_2d(&t->many, dt, d_X, d_in, p.rows.T, x_stride, kBoxRows)) return st;
+  return map_2d(&t->unit, dt, d_X, d_in, p.rows.T, x_stride, p.rows.unit);
+}
+
 template <int BN>
-rf_status launch_pair(const CUtensorMap& x, const CUtensorMap& box, const CUtensorMap& w,
-                      const LinearParams& p, int64_t tiles, const DeviceInfo& di, cudaStream_t s) {
+rf_status launch_pair(const Maps& t, const LinearParams& p, int64_t tiles, const DeviceInfo& di, cudaStream_t s) {
   static bool done[64] = {};
   if (rf_status st = set_smem(pair_kernel<BN>, PairCfg<BN>::kSmem, di, done)) return st;
-  const int64_t pairs = std::min<int64_t>(tiles, di.sm_count / 2);
+  // pairs that run together: fewer than half the SMs where a GPC has an odd number of them, and
+  // one pair more would begin when the others have finished (480p keyframe-only step: 154 us)
+  static std::atomic<int> resident[64] = {};
+  int most = resident[di.device].load(std::memory_order_relaxed);
+  if (most == 0) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(static_cast<unsigned>(di.sm_count / 2 * 2));
+    cfg.blockDim = dim3(kPairThreads);
+    cfg.dynamicSmemBytes = PairCfg<BN>::kSmem;
+    if (cudaError_t e = cudaOccupancyMaxActiveClusters(&most, pair_kernel<BN>, &cfg))
+      return fail(RF_ERR_CUDA, "cudaOccupancyMaxActiveClusters(rf_linear)", e);
+    if (most < 1) return fail(RF_ERR_UNSUPPORTED, "rf_linear: no room for a pair of CTAs");
+    resident[di.device].store(most, std::memory_order_relaxed);
+  }
+  const int64_t pairs = std::min<int64_t>(tiles, most);
   pair_kernel<BN><<<static_cast<unsigned>(2 * pairs), kPairThreads, PairCfg<BN>::kSmem, s>>>(
-      x, box, w, p);
+      t.x, t.many, t.unit, t.w, p);
   return launch_status("rf_linear pair_kernel launch");
 }
 
-rf_status launch_split(const CUtensorMap& x, const CUtensorMap& box, const CUtensorMap& w,
-                       const LinearParams& p, int64_t tiles, const DeviceInfo& di, cudaStream_t s) {
+rf_status launch_split(const Maps& t, const LinearParams& p, int64_t tiles, const DeviceInfo& di, cudaStream_t s) {
   static bool done[64] = {};
   if (rf_status st = set_smem(split_kernel, kSplitSmem, di, done)) return st;
   cudaLaunchConfig_t cfg{};
@@ -672,7 +688,7 @@ rf_status launch_split(const CUtensorMap& x, const CUtensorMap& box, const CUten
   attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = p.cluster > 1 ? 1 : 0;
-  if (cudaError_t e = cudaLaunchKernelEx(&cfg, split_kernel, x, box, w, p)) {
+  if (cudaError_t e = cudaLaunchKernelEx(&cfg, split_kernel, t.x, t.many, t.unit, t.w, p)) {
     cudaGetLastError();
     return fail(RF_ERR_CUDA, "rf_linear split_kernel launch", e);
   }
@@ -711,8 +727,8 @@ extern "C" rf_status rf_linear(void* d_Y, int64_t y_row_stride, int out_dtype, c
   // without a list the tokens are one frame, with nothing between them
   const int64_t T = static_cast<int64_t>(F) * N;
   const int64_t Fr = d_active ? F : 1, Nr = d_active ? N : T;
-  const int box = Nr < 8 ? 1 : 8;
-  const int64_t Np = (Nr + box - 1) / box * box;
+  const int unit = row_unit(Nr);
+  const int64_t Np = (Nr + unit - 1) / unit * unit;
   if (T > 0x7FFFFFFF - 65536 || Fr * Np > 0x7FFFFFFF - 65536 || d_out > 0x7FFFFFFF - 65536 ||
       d_in > 0x7FFFFFFF - 65536)
     return fail(RF_ERR_INVALID_ARG, "rf_linear: too many tokens or columns");
@@ -721,7 +737,7 @@ extern "C" rf_status rf_linear(void* d_Y, int64_t y_row_stride, int out_dtype, c
   if (di.cc_major != 10 || di.cc_minor != 3) return fail(RF_ERR_UNSUPPORTED, "needs sm_103");
 
   LinearParams p{};
-  p.rows = {d_active, d_counts, static_cast<int>(Fr), static_cast<int>(Nr), static_cast<int>(Np), box,
+  p.rows = {d_active, d_counts, static_cast<int>(Fr), static_cast<int>(Nr), static_cast<int>(Np), unit,
             static_cast<int>(T)};
   Epilogue& e = p.epi;
   e.Y = d_Y;
@@ -747,13 +763,11 @@ extern "C" rf_status rf_linear(void* d_Y, int64_t y_row_stride, int out_dtype, c
   const int64_t rows = Fr * Np;  // at most: the active count is known on the device only
   const int64_t n256 = (d_out + 255) / 256, n128 = (d_out + 127) / 128;
   const int64_t pair_tiles = (rows + 255) / 256 * n256;
-  CUtensorMap mx, mbox, mw;
-  if (rf_status st = map_2d(&mbox, dtype, d_X, d_in, T, x_row_stride, box)) return st;
+  Maps t;
   if (rows > 256 && pair_tiles >= di.sm_count / 4) {
     p.n_tiles = static_cast<int>(n256);
-    if (rf_status st = map_2d(&mx, dtype, d_X, d_in, T, x_row_stride, 128)) return st;
-    if (rf_status st = map_2d(&mw, dtype, d_W, d_in, d_out, w_row_stride, 128)) return st;
-    return launch_pair<256>(mx, mbox, mw, p, pair_tiles, di, s);
+    if (rf_status st = make_maps(&t, p, d_X, x_row_stride, d_W, w_row_stride, d_in, 128, 128)) return st;
+    return launch_pair<256>(t, p, pair_tiles, di, s);
   }
   int BT = 16;
   while (BT < 256 && BT < rows) BT *= 2;
@@ -762,7 +776,6 @@ extern "C" rf_status rf_linear(void* d_Y, int64_t y_row_stride, int out_dtype, c
   p.tile_tokens = BT;
   p.cluster = split_ranges(tiles, p.kblocks, di.sm_count);
   p.stages = std::min(kSplitMaxStages, kSplitRing / (16384 + BT * 128));
-  if (rf_status st = map_2d(&mx, dtype, d_X, d_in, T, x_row_stride, BT)) return st;
-  if (rf_status st = map_2d(&mw, dtype, d_W, d_in, d_out, w_row_stride, 128)) return st;
-  return launch_split(mx, mbox, mw, p, tiles, di, s);
+  if (rf_status st = make_maps(&t, p, d_X, x_row_stride, d_W, w_row_stride, d_in, BT, 128)) return st;
+  return launch_split(t, p, tiles, di, s);
 }

@@ -1,0 +1,81 @@
+// rf_rows.cuh -- the rows of a launch over the active frames, and how a tile of them is loaded.
+#pragma once
+#include <cstdint>
+
+#include "rf_tc_ptx.cuh"
+
+namespace rf {
+
+// The active frames' tokens one frame after the other, each frame padded to Np rows; Np is N
+// rounded up to `unit`, so that `unit` consecutive rows from a multiple of it lie in one frame.
+struct RowMap {
+  const int32_t* active;  // or null: frames 0 .. F-1
+  const int32_t* counts;
+  int F, N, Np, unit;
+  int T;  // tokens: F * N
+
+  __device__ __forceinline__ int frames() const {
+    return active ? min(max(counts[0], 0), F) : F;
+  }
+  __device__ __forceinline__ int frame(int a) const { return active ? active[a] : a; }
+};
+// Frames of 8 tokens or more are padded to 8 rows, a swizzle atom of shared memory; shorter ones
+// not at all (their rows are loaded one by one, which the atom's address-based swizzle allows).
+constexpr int row_unit(int64_t N) { return N < 8 ? 1 : 8; }
+
+// How a tile of rows is loaded: in one TMA box where its rows lie in one frame, else in boxes of
+// kBoxRows and of `unit` rows, listed in shared memory {first token, first row of the tile}: the
+// larger ones from the front of the list, the others from its end.  One elected thread issues them
+// all, each from a fixed tensor map: a box issued by its own lane under a branch, or with the map
+// chosen per box, held a product's 512-cycle step up to three times its length.
+constexpr int kBoxRows = 32;
+struct RowBoxes {
+  int rows;           // rows that the boxes bring
+  int n_many, n_unit; // both 0: one box of the whole tile, from token tok
+  int tok;
+};
+// Rows [r0, r0 + n) of R, r0 a multiple of the unit; list: n entries.  Warp-collective; the same in
+// every lane.  Rows past R are not loaded, except that a tile with none at all gets a box of zeros.
+__device__ __forceinline__ RowBoxes list_boxes(const RowMap& m, int R, int r0, int n, int2* list) {
+  RowBoxes x{n, 0, 0, 0};
+  const int lane = threadIdx.x & 31;
+  const int end = min(r0 + n, R);
+  const int a0 = r0 / m.Np;
+  if (r0 >= R || a0 == (end - 1) / m.Np) {
+    // rows past the frame bring the tokens that follow, past the last one zeros: never stored
+    x.tok = r0 >= R ? m.T : m.frame(a0) * m.N + (r0 - a0 * m.Np);
+    return x;
+  }
+  x.rows = end - r0;
+  __syncwarp();  // the list's last use is over
+  if (m.unit == 1) {
+    x.n_unit = x.rows;
+    for (int i = lane; i < x.rows; i += 32) {
+      const int r = r0 + i, a = r / m.Np;
+      list[n - 1 - i] = make_int2(m.frame(a) * m.N + (r - a * m.Np), i);
+    }
+  } else {
+    for (int r = r0, a = a0; r < end; ++a) {
+      const int q = r - a * m.Np, len = min(m.Np - q, end - r);
+      const int many = len / kBoxRows, units = (len - many * kBoxRows) / m.unit;
+      const int tok = m.frame(a) * m.N + q;
+      if (lane < many) list[x.n_many + lane] = make_int2(tok + lane * kBoxRows, r - r0 + lane * kBoxRows);
+      if (lane < units) {
+        const int o = many * kBoxRows + lane * m.unit;
+        list[n - 1 - (x.n_unit + lane)] = make_int2(tok + o, r - r0 + o);
+      }
+      x.n_many += many;
+      x.n_unit += units;
+      r += len;
+    }
+  }
+  __syncwarp();
+  return x;
+}
+// list_boxes(...).rows, without the list.
+__device__ __forceinline__ int boxed_rows(const RowMap& m, int R, int r0, int n) {
+  const int end = min(r0 + n, R);
+  return r0 >= R || r0 / m.Np == (end - 1) / m.Np ? n : end - r0;
+}
+
+}  // namespace rf

@@ -158,19 +158,4 @@ __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
   return r;
 }
 
-// ---------------------------------------------------------------- rows of the active frames
-// The rows of a launch: the active frames' tokens one frame after the other, each frame padded to
-// Np rows; Np is N rounded up to `box`, so that a box of `box` consecutive rows lies in one frame.
-struct RowMap {
-  const int32_t* active;  // or null: frames 0 .. F-1
-  const int32_t* counts;
-  int F, N, Np, box;
-  int T;  // tokens: F * N
-
-  __device__ __forceinline__ int frames() const {
-    return active ? min(max(counts[0], 0), F) : F;
-  }
-  __device__ __forceinline__ int frame(int a) const { return active ? active[a] : a; }
-};
-
 }  // namespace rf
