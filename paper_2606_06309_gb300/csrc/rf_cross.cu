@@ -34,6 +34,7 @@
 
 #include "rf_ops.h"
 #include "rf_rows.cuh"
+#include "rf_stage.cuh"
 #include "rf_tc_ptx.cuh"
 
 namespace rf {
@@ -67,8 +68,10 @@ struct Cfg {
                        kVClean = 4 + 2 * kSlots, kSFull = 4 + 3 * kSlots, kODone = kSFull + 2,
                        kDrain = kODone + 2, kBars = kDrain + 2;
   static constexpr int kOffMisc = kOffBar + kBars * 8;  // tensor memory address, abort, MMA done [2]
-  static constexpr int kOffList = kOffMisc + 32;        // boxes of a query tile
-  static constexpr int kSmem = kOffList + 128 * 8 + 1024;  // + slack to align the base
+  static constexpr int kOffList = kOffMisc + 32;           // boxes of the query tiles
+  static constexpr int kOffStage =
+      (kOffList + 2 * static_cast<int>(sizeof(BoxList<kBM>)) + 15) / 16 * 16;  // rows of results, per softmax warp
+  static constexpr int kSmem = kOffStage + 8 * kTurnBytes + 1024;  // + slack to align the base
   // A split item's rows: [tile][D / 4][128] float4 over the K/V ring, {max, sum} [tile][128] over
   // the queries
   static_assert(2 * 128 * D * 4 <= kSlots * kTileBytes, "partial rows fit the ring");
@@ -134,9 +137,13 @@ __device__ __forceinline__ Item get_item(const CrossParams& p, const Work& w, in
     t.begin = min(max(r.x, 0), p.L);
     t.end = min(max(r.y, t.begin), p.L);
   }
-  const int nt = (t.end - t.begin + kBN - 1) / kBN;
-  t.j0 = static_cast<int>(static_cast<int64_t>(nt) * rank / p.cluster);
-  t.j1 = static_cast<int>(static_cast<int64_t>(nt) * (rank + 1) / p.cluster);
+  const int nt = (t.end - t.begin + kBN - 1) / kBN;  // below 2^24
+  t.j0 = 0;
+  t.j1 = nt;
+  if (p.cluster > 1) {
+    t.j0 = nt * rank / p.cluster;
+    t.j1 = nt * (rank + 1) / p.cluster;
+  }
   return t;
 }
 
@@ -184,10 +191,38 @@ __device__ __forceinline__ KeyBits key_bits(const CrossParams& p, const Item& t,
 struct QueryMaps {
   const CUtensorMap *whole, *many, *unit;
 };
+// What an item's loads need, found before they can be issued.
+struct Load {
+  Item t;
+  RowBoxes x[2];
+};
+template <int D>
+__device__ __forceinline__ void prepare_load(const QueryMaps& maps, const CrossParams& p,
+                                             const Work& w, int i, int rank, BoxList<kBM>* list, bool lead,
+                                             Load& n) {
+  n.t = get_item(p, w, i, rank);
+  if (p.packed || n.t.j0 >= n.t.j1) return;
+#pragma unroll
+  for (int X = 0; X < 2; ++X) {
+    const int tile = 2 * n.t.pair + X;
+    if (tile >= w.tiles) break;
+    if (p.kv_range)
+      n.x[X] = RowBoxes{kBM, 0, 0, p.rows.frame(n.t.group) * p.rows.N + tile * kBM};
+    else
+      n.x[X] = list_boxes(p.rows, w.A * p.rows.Np, tile * kBM, kBM, list[X]);
+    // on their way to L2 while the item before is worked on: the queries' own buffer is free only
+    // when that item's last Q K^T is done
+    if (lead && n.x[X].n_many + n.x[X].n_unit == 0)
+#pragma unroll
+      for (int hb = 0; hb < Cfg<D>::kHalves; ++hb)
+        tma_prefetch_3d(maps.whole, hb * 64, n.t.unit, n.x[X].tok);
+  }
+}
 template <int D>
 __device__ __forceinline__ void load_queries(const QueryMaps& maps, const CrossParams& p,
-                                             const Work& w, const Item& t, int tile, int2* list,
-                                             uint32_t dst, uint32_t bar, bool lead) {
+                                             const Work& w, const Item& t, int tile,
+                                             const RowBoxes& x, const BoxList<kBM>& list, uint32_t dst,
+                                             uint32_t bar) {
   using C = Cfg<D>;
   auto load = [&](const CUtensorMap* m, int row, int head, int tok) {
 #pragma unroll
@@ -198,69 +233,71 @@ __device__ __forceinline__ void load_queries(const QueryMaps& maps, const CrossP
     // one box per frame: its tokens, and for each the query heads of the key head
     const int a0 = p.kv_range ? t.group : tile * p.tile_frames;
     const int n = min(p.tile_frames, w.A - a0);
-    if (lead) {
-      mbar_arrive_expect_tx(bar, n * p.frame_rows * 128 * C::kHalves);
-      for (int i = 0; i < n; ++i)
-        load(maps.unit, i * p.frame_rows, t.unit * p.g, p.rows.frame(a0 + i) * p.rows.N);
-    }
-  } else if (p.kv_range) {
-    if (lead) {
-      mbar_arrive_expect_tx(bar, C::kTileBytes);
-      load(maps.whole, 0, t.unit, p.rows.frame(t.group) * p.rows.N + tile * kBM);
-    }
-  } else {
-    const RowBoxes x = list_boxes(p.rows, w.A * p.rows.Np, tile * kBM, kBM, list);
-    if (lead) {
-      mbar_arrive_expect_tx(bar, x.rows * 128 * C::kHalves);
-      if (x.n_many + x.n_unit == 0) load(maps.whole, 0, t.unit, x.tok);
-#pragma unroll 2
-      for (int i = 0; i < x.n_many; ++i) load(maps.many, list[i].y, t.unit, list[i].x);
-#pragma unroll 2
-      for (int i = 0; i < x.n_unit; ++i)
-        load(maps.unit, list[kBM - 1 - i].y, t.unit, list[kBM - 1 - i].x);
-    }
+    mbar_arrive_expect_tx(bar, n * p.frame_rows * 128 * C::kHalves);
+    for (int i = 0; i < n; ++i)
+      load(maps.unit, i * p.frame_rows, t.unit * p.g, p.rows.frame(a0 + i) * p.rows.N);
+    return;
   }
-  __syncwarp();
+  mbar_arrive_expect_tx(bar, x.rows * 128 * C::kHalves);
+  if (x.n_many + x.n_unit == 0) {
+    load(maps.whole, 0, t.unit, x.tok);
+    return;
+  }
+  for (int i = 0; i < x.n_many; ++i) load(maps.many, list.row[i], t.unit, list.tok[i]);
+  for (int i = kBM - x.n_unit; i < kBM; ++i) load(maps.unit, list.row[i], t.unit, list.tok[i]);
 }
 
 template <int D>
 __device__ __forceinline__ void producer(const QueryMaps& maps, const CUtensorMap* tmK,
                                          const CUtensorMap* tmV, const CrossParams& p,
-                                         const Work& w, int rank, int2* list, uint32_t sQ0,
+                                         const Work& w, int rank, BoxList<kBM>* list, uint32_t sQ0,
                                          uint32_t sKV0, uint32_t bar0, volatile int* abort) {
   using C = Cfg<D>;
   auto bar = [&](int i) { return bar0 + 8u * i; };
   const bool lead = elect_one();
+  const int step = gridDim.x / p.cluster;
   int q_cnt[2] = {0, 0};
   int it = 0;
   bool ok = true;
-  for (int i = blockIdx.x / p.cluster; ok && i < w.items; i += gridDim.x / p.cluster) {
-    const Item t = get_item(p, w, i, rank);
-    if (t.j0 >= t.j1) continue;
+  Load n;
+  int i = blockIdx.x / p.cluster;
+  if (i < w.items) prepare_load<D>(maps, p, w, i, rank, list, lead, n);
+  while (ok && i < w.items) {
+    const Item t = n.t;
     const int hk = p.packed ? t.unit : t.unit / p.g;
-    for (int X = 0; ok && X < 2; ++X) {
-      const int tile = 2 * t.pair + X;
-      if (tile >= w.tiles) break;
-      ok = all_wait(bar(C::kQEmpty + X), (q_cnt[X] & 1) ^ 1, abort);
-      if (!ok) break;
-      load_queries<D>(maps, p, w, t, tile, list, sQ0 + X * C::kTileBytes, bar(C::kQFull + X), lead);
-      ++q_cnt[X];
-    }
-    for (int j = t.j0; ok && j < t.j1; ++j)
-      for (int kv = 0; kv < 2; ++kv) {
-        const int s = it % C::kSlots;
-        ok = all_wait(bar(C::kKVEmpty + s), ((it / C::kSlots) & 1) ^ 1, abort);
-        if (!ok) break;
-        if (lead) {
-          mbar_arrive_expect_tx(bar(C::kKVFull + s), C::kTileBytes);
+    auto load_kv = [&](int j, int kv) -> bool {
+      const int s = it % C::kSlots;
+      if (!all_wait(bar(C::kKVEmpty + s), ((it / C::kSlots) & 1) ^ 1, abort)) return false;
+      if (lead) {
+        mbar_arrive_expect_tx(bar(C::kKVFull + s), C::kTileBytes);
 #pragma unroll
-          for (int hb = 0; hb < C::kHalves; ++hb)
-            tma_load_3d(sKV0 + s * C::kTileBytes + hb * C::kHalfBytes, kv ? tmV : tmK,
-                        bar(C::kKVFull + s), hb * 64, hk, t.begin + j * kBN);
-        }
-        __syncwarp();
-        ++it;
+        for (int hb = 0; hb < C::kHalves; ++hb)
+          tma_load_3d(sKV0 + s * C::kTileBytes + hb * C::kHalfBytes, kv ? tmV : tmK,
+                      bar(C::kKVFull + s), hb * 64, hk, t.begin + j * kBN);
       }
+      __syncwarp();
+      ++it;
+      return true;
+    };
+    if (t.j0 < t.j1) {
+      // the first keys go before the queries: their slot is free earlier
+      ok = load_kv(t.j0, 0);
+      for (int X = 0; ok && X < 2; ++X) {
+        const int tile = 2 * t.pair + X;
+        if (tile >= w.tiles) break;
+        ok = all_wait(bar(C::kQEmpty + X), (q_cnt[X] & 1) ^ 1, abort);
+        if (!ok) break;
+        if (lead)
+          load_queries<D>(maps, p, w, t, tile, n.x[X], list[X], sQ0 + X * C::kTileBytes,
+                          bar(C::kQFull + X));
+        __syncwarp();
+        ++q_cnt[X];
+      }
+      ok = ok && load_kv(t.j0, 1);
+      for (int j = t.j0 + 1; ok && j < t.j1; ++j) ok = load_kv(j, 0) && load_kv(j, 1);
+    }
+    i += step;
+    if (ok && i < w.items) prepare_load<D>(maps, p, w, i, rank, list, lead, n);
   }
   if (!ok && lead) flag_error(p, 0);
   // every copy has landed
@@ -429,10 +466,9 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   return F16 ? pack_f16x2(lo, hi) : pack_bf16x2(lo, hi);
 }
 template <bool F16>
-__device__ __forceinline__ void store8(uint16_t* dst, const float* o, float scale) {
-  *reinterpret_cast<uint4*>(dst) =
-      make_uint4(pack2<F16>(o[0] * scale, o[1] * scale), pack2<F16>(o[2] * scale, o[3] * scale),
-                 pack2<F16>(o[4] * scale, o[5] * scale), pack2<F16>(o[6] * scale, o[7] * scale));
+__device__ __forceinline__ uint4 pack8(const float* o, float scale) {
+  return make_uint4(pack2<F16>(o[0] * scale, o[1] * scale), pack2<F16>(o[2] * scale, o[3] * scale),
+                    pack2<F16>(o[4] * scale, o[5] * scale), pack2<F16>(o[6] * scale, o[7] * scale));
 }
 
 // The running maximum (in units of log2, scaled) and sum of a row over a CTA's K/V tiles of an
@@ -585,23 +621,25 @@ __device__ __forceinline__ bool softmax_group(const CrossParams& p, const Work& 
     int head;
     const int64_t token = row_of(p, w, t, tile, row, head);
     const bool valid = token >= 0;
-    uint16_t* orow = p.O + token * p.o_row_stride + static_cast<int64_t>(head) * D;
+    const int64_t at = valid ? (token * p.o_row_stride + static_cast<int64_t>(head) * D) * 2 : -1;
     // no key: zeros, not 0 * accumulator, which may hold anything
     const bool none = l == 0.f;
     const float inv_l = none ? 0.f : 1.0f / l;
+    uint4* stage = reinterpret_cast<uint4*>(smem + C::kOffStage + (warp - 4) * kTurnBytes);
 #pragma unroll 1
-    for (int c = 0; c < D / 32; ++c) {
-      uint32_t o[32];
-      tmem_ld32(tO + c * 32, o);
-      tmem_wait_ld();
-      if (none) {
+    for (int c = 0; c < D / 64; ++c) {
+      uint4 v[8];
 #pragma unroll
-        for (int e = 0; e < 32; ++e) o[e] = 0u;
-      }
-      if (valid)
+      for (int half = 0; half < 2; ++half) {
+        uint32_t o[32];
+        tmem_ld32(tO + c * 64 + half * 32, o);
+        tmem_wait_ld();
 #pragma unroll
         for (int q = 0; q < 4; ++q)
-          store8<F16>(orow + c * 32 + q * 8, reinterpret_cast<const float*>(o) + q * 8, inv_l);
+          v[half * 4 + q] = none ? make_uint4(0u, 0u, 0u, 0u)
+                                 : pack8<F16>(reinterpret_cast<const float*>(o) + q * 8, inv_l);
+      }
+      store_rows(stage, v, reinterpret_cast<char*>(p.O) + c * 128, at);
     }
     if (valid && p.lse)
       p.lse[static_cast<int64_t>(head) * p.rows.T + token] =
@@ -665,7 +703,7 @@ __device__ __forceinline__ void join(const CrossParams& p, const Work& w, int ra
         acc[6] = fmaf(ms[c], b.z, acc[6]);
         acc[7] = fmaf(ms[c], b.w, acc[7]);
       }
-    store8<F16>(orow + c8 * 8, acc, inv);
+    *reinterpret_cast<uint4*>(orow + c8 * 8) = pack8<F16>(acc, inv);
   }
   if (rank == 0 && p.lse)
     p.lse[static_cast<int64_t>(head) * p.rows.T + token] =
@@ -738,7 +776,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     reg_dealloc<kRegsControl>();
     if (warp == 0) {
       producer<D>({&tmQ, &tmMany, &tmUnit}, &tmK, &tmV, p, w, rank,
-                  reinterpret_cast<int2*>(smem + C::kOffList), sQ0, sKV0, bar0, abort);
+                  reinterpret_cast<BoxList<kBM>*>(smem + C::kOffList), sQ0, sKV0, bar0, abort);
     } else if (warp < 3) {
       const int X = warp - 1;
       const bool ok =

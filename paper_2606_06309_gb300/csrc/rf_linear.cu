@@ -20,6 +20,7 @@
 
 #include "rf_ops.h"
 #include "rf_rows.cuh"
+#include "rf_stage.cuh"
 #include "rf_tc_ptx.cuh"
 
 namespace rf {
@@ -89,29 +90,12 @@ __device__ __forceinline__ void unpack2(uint32_t w, int dtype, float& lo, float&
     hi = __uint_as_float(w & 0xFFFF0000u);
   }
 }
-// 32 consecutive elements from a 16-byte boundary
-__device__ __forceinline__ void load32(const void* p, int64_t i, int dtype, float (&x)[32]) {
-  if (dtype == RF_FP32) {
-    const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(p) + i);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float4 f = q[e];
-      x[4 * e] = f.x;
-      x[4 * e + 1] = f.y;
-      x[4 * e + 2] = f.z;
-      x[4 * e + 3] = f.w;
-    }
-  } else {
-    const uint4* q = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + i);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const uint4 w = q[e];
-      unpack2(w.x, dtype, x[8 * e], x[8 * e + 1]);
-      unpack2(w.y, dtype, x[8 * e + 2], x[8 * e + 3]);
-      unpack2(w.z, dtype, x[8 * e + 4], x[8 * e + 5]);
-      unpack2(w.w, dtype, x[8 * e + 6], x[8 * e + 7]);
-    }
-  }
+// lo, hi += the two elements of a word
+__device__ __forceinline__ void add2(uint32_t w, int dtype, float& lo, float& hi) {
+  float a, b;
+  unpack2(w, dtype, a, b);
+  lo += a;
+  hi += b;
 }
 
 // One element of the result from its sum.
@@ -125,58 +109,125 @@ __device__ __forceinline__ void finish_one(const Epilogue& e, int64_t token, int
   store_elem(e.Y, token * e.y_stride + n, e.out_dtype, v[0]);
 }
 
-// Columns n .. n + 31 of a row.
+// Columns n .. n + 31 of a row, element by element: the last columns of a result, and rows off the
+// 16-byte boundaries.
 __device__ __forceinline__ void finish_row(const Epilogue& e, int64_t token, int frame, int n,
                                            float (&v)[32]) {
-  if (!e.vec || n + 32 > e.n_out) {
 #pragma unroll
-    for (int i = 0; i < 32; ++i)
-      if (n + i < e.n_out && e.bias) v[i] += load_elem(e.bias, n + i, e.in_dtype);
-    activate(e.act, v);
+  for (int i = 0; i < 32; ++i)
+    if (n + i < e.n_out && e.bias) v[i] += load_elem(e.bias, n + i, e.in_dtype);
+  activate(e.act, v);
 #pragma unroll
-    for (int i = 0; i < 32; ++i)
-      if (n + i < e.n_out) {
-        if (e.gate) v[i] *= e.gate[frame * e.gate_stride + n + i];
-        if (e.R) v[i] += load_elem(e.R, token * e.r_stride + n + i, e.out_dtype);
-        store_elem(e.Y, token * e.y_stride + n + i, e.out_dtype, v[i]);
-      }
-    return;
-  }
-  float x[32];
+  for (int i = 0; i < 32; ++i)
+    if (n + i < e.n_out) {
+      if (e.gate) v[i] *= e.gate[frame * e.gate_stride + n + i];
+      if (e.R) v[i] += load_elem(e.R, token * e.r_stride + n + i, e.out_dtype);
+      store_elem(e.Y, token * e.y_stride + n + i, e.out_dtype, v[i]);
+    }
+}
+
+// 32 columns from n: bias, activation, gate.
+__device__ __forceinline__ void finish_cols(const Epilogue& e, int frame, int n, float (&v)[32]) {
   if (e.bias) {
-    load32(e.bias, n, e.in_dtype, x);
+    const uint4* q = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(e.bias) + n);
 #pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] += x[i];
+    for (int i = 0; i < 4; ++i) {
+      const uint4 w = q[i];
+      add2(w.x, e.in_dtype, v[8 * i], v[8 * i + 1]);
+      add2(w.y, e.in_dtype, v[8 * i + 2], v[8 * i + 3]);
+      add2(w.z, e.in_dtype, v[8 * i + 4], v[8 * i + 5]);
+      add2(w.w, e.in_dtype, v[8 * i + 6], v[8 * i + 7]);
+    }
   }
   activate(e.act, v);
   if (e.gate) {
-    load32(e.gate, frame * e.gate_stride + n, RF_FP32, x);
+    const float4* q = reinterpret_cast<const float4*>(e.gate + frame * e.gate_stride + n);
 #pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] *= x[i];
-  }
-  if (e.R) {
-    load32(e.R, token * e.r_stride + n, e.out_dtype, x);
-#pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] += x[i];
-  }
-  if (e.out_dtype == RF_FP32) {
-    float4* y = reinterpret_cast<float4*>(static_cast<float*>(e.Y) + token * e.y_stride + n);
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      y[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-  } else {
-    uint4* y = reinterpret_cast<uint4*>(static_cast<uint16_t*>(e.Y) + token * e.y_stride + n);
-    uint32_t w[16];
-    if (e.out_dtype == RF_FP16) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) w[i] = pack_f16x2(v[2 * i], v[2 * i + 1]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) w[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
+    for (int i = 0; i < 8; ++i) {
+      const float4 g = q[i];
+      v[4 * i] *= g.x;
+      v[4 * i + 1] *= g.y;
+      v[4 * i + 2] *= g.z;
+      v[4 * i + 3] *= g.w;
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) y[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
   }
+}
+
+// A warp's 32 rows of an accumulator (tensor memory columns from `acc`; a row per lane, its token or
+// -1), columns n0 .. n0 + cols - 1 of the result, 128 bytes of them at a time through the
+// warp's stage.  ready() is called when the residual's first loads are in flight and the
+// accumulator is wanted, read() when it has been read; false from ready() ends it.
+template <bool OUT32, typename Ready, typename Read>
+__device__ __forceinline__ bool finish_tile(const Epilogue& e, uint4* stage, uint32_t acc, int n0,
+                                            int cols, int64_t token, int frame, Ready&& ready,
+                                            Read&& read) {
+  constexpr int kCols = OUT32 ? 32 : 64, kBytes = OUT32 ? 4 : 2;
+  const int chunks = (min(cols, max(e.n_out - n0, 0)) + kCols - 1) / kCols;
+  const int64_t at_y = token < 0 ? -1 : (token * e.y_stride + n0) * kBytes;
+  const int64_t at_r = token < 0 || !e.R ? -1 : (token * e.r_stride + n0) * kBytes;
+  const char* R = static_cast<const char*>(e.R);
+  const int lane = threadIdx.x & 31;
+  auto whole = [&](int c) { return e.vec && n0 + (c + 1) * kCols <= e.n_out; };
+  if (e.R && chunks > 0 && whole(0)) fetch_rows(stage, R, at_r);
+  if (!ready()) return false;
+  if (chunks == 0) read();
+#pragma unroll 1
+  for (int c = 0; c < chunks; ++c) {
+    const int n = n0 + c * kCols;
+    if (!whole(c)) {
+#pragma unroll 1
+      for (int half = 0; half < kCols; half += 32) {
+        uint32_t v[32];
+        tmem_ld32(acc + c * kCols + half, v);
+        tmem_wait_ld();
+        if (token >= 0 && n + half < e.n_out)
+          finish_row(e, token, frame, n + half, *reinterpret_cast<float(*)[32]>(&v));
+        __syncwarp();
+      }
+      if (c == chunks - 1) read();
+      continue;
+    }
+    uint4 row[8];
+    uint32_t* w = reinterpret_cast<uint32_t*>(row);
+#pragma unroll
+    for (int half = 0; half < kCols / 32; ++half) {
+      float v[32];
+      tmem_ld32(acc + c * kCols + half * 32, reinterpret_cast<uint32_t(&)[32]>(v));
+      tmem_wait_ld();
+      if (half == kCols / 32 - 1 && c == chunks - 1) read();
+      finish_cols(e, frame, n + half * 32, v);
+      if (e.R) {
+        if (half == 0) await_rows();
+#pragma unroll
+        for (int q = 0; q < (OUT32 ? 8 : 4); ++q) {
+          const uint4 r = stage_at(stage, lane, half * 4 + q);
+          if (OUT32) {
+            v[4 * q] += __uint_as_float(r.x);
+            v[4 * q + 1] += __uint_as_float(r.y);
+            v[4 * q + 2] += __uint_as_float(r.z);
+            v[4 * q + 3] += __uint_as_float(r.w);
+          } else {
+            add2(r.x, e.out_dtype, v[(8 * q) & 31], v[(8 * q + 1) & 31]);
+            add2(r.y, e.out_dtype, v[(8 * q + 2) & 31], v[(8 * q + 3) & 31]);
+            add2(r.z, e.out_dtype, v[(8 * q + 4) & 31], v[(8 * q + 5) & 31]);
+            add2(r.w, e.out_dtype, v[(8 * q + 6) & 31], v[(8 * q + 7) & 31]);
+          }
+        }
+      }
+      if (OUT32) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) w[i] = __float_as_uint(v[i]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          w[half * 16 + i] = e.out_dtype == RF_FP16 ? pack_f16x2(v[2 * i], v[2 * i + 1])
+                                                    : pack_bf16x2(v[2 * i], v[2 * i + 1]);
+      }
+    }
+    store_rows(stage, row, static_cast<char*>(e.Y) + c * 128, at_y);
+    if (e.R && c + 1 < chunks && whole(c + 1)) fetch_rows(stage, R + (c + 1) * 128, at_r);
+  }
+  return true;
 }
 
 struct LinearParams {
@@ -207,8 +258,8 @@ struct RowMaps {
   const CUtensorMap *whole, *many, *unit;
 };
 // Issue the copies of one k block of a tile of n rows (the bytes are announced before; one thread).
-template <bool PAIR>
-__device__ __forceinline__ void load_rows(const RowBoxes& x, const int2* list, int n,
+template <bool PAIR, int ROWS>
+__device__ __forceinline__ void load_rows(const RowBoxes& x, const BoxList<ROWS>& list, int n,
                                           const RowMaps& maps, uint32_t dst, uint32_t bar, int k0) {
   auto load = [&](const CUtensorMap* m, int row, int tok) {
     if (PAIR) tma_load_2d_pair(dst + row * 128, m, bar, k0, tok);
@@ -219,9 +270,9 @@ __device__ __forceinline__ void load_rows(const RowBoxes& x, const int2* list, i
     return;
   }
 #pragma unroll 2
-  for (int i = 0; i < x.n_many; ++i) load(maps.many, list[i].y, list[i].x);
+  for (int i = 0; i < x.n_many; ++i) load(maps.many, list.row[i], list.tok[i]);
 #pragma unroll 2
-  for (int i = 0; i < x.n_unit; ++i) load(maps.unit, list[n - 1 - i].y, list[n - 1 - i].x);
+  for (int i = n - x.n_unit; i < n; ++i) load(maps.unit, list.row[i], list.tok[i]);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -245,7 +296,9 @@ struct PairCfg {
   static constexpr int kOffBar = kStages * kStageBytes;
   static constexpr int kOffMisc = kOffBar + kBars * 8;
   static constexpr int kOffList = kOffMisc + 16;
-  static constexpr int kSmem = kOffList + 128 * 8 + 1024;
+  static constexpr int kOffStage =
+      (kOffList + static_cast<int>(sizeof(BoxList<128>)) + 15) / 16 * 16;
+  static constexpr int kSmem = kOffStage + kEpiWarps * kTurnBytes + 1024;
   static constexpr uint32_t kTmemCols = 2 * BN;
 };
 
@@ -309,7 +362,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
 
   if (warp == 0) {
     const bool lead = elect_one();
-    int2* list = reinterpret_cast<int2*>(smem + C::kOffList);
+    BoxList<128>& list = *reinterpret_cast<BoxList<128>*>(smem + C::kOffList);
     int it = 0;
     bool ok = true;
     for (int t = pair; ok && t < tiles; t += pairs) {
@@ -388,6 +441,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
   } else if (warp >= 4) {
     const int quarter = warp & 3, part = (warp - 4) >> 2;  // lanes of tensor memory; half of BN
     const uint32_t lane_base = static_cast<uint32_t>(quarter * 32) << 16;
+    uint4* stage = reinterpret_cast<uint4*>(smem + C::kOffStage + (warp - 4) * kTurnBytes);
     int n_acc = 0;
     for (int t = pair; t < tiles; t += pairs, ++n_acc) {
       int m, n;
@@ -396,27 +450,25 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
       const int r = m * 256 + rank * 128 + quarter * 32 + lane;
       int frame = 0;
       const int token = r < R ? row_token(p, r, frame) : -1;
-      if (!__all_sync(0xffffffffu, mbar_wait_cluster(bar(C::kBarAccFull + b), (n_acc >> 1) & 1,
-                                                     abort, kWaitLimitNs))) {
-        if (lane == 0) flag_error(p, 3);
+      auto ready = [&]() -> bool {
+        const bool ok = __all_sync(0xffffffffu, mbar_wait_cluster(bar(C::kBarAccFull + b),
+                                                                  (n_acc >> 1) & 1, abort,
+                                                                  kWaitLimitNs));
+        if (!ok && lane == 0) flag_error(p, 3);
+        tc_fence_after();
+        return ok;
+      };
+      auto read = [&]() {  // the accumulator may be written again
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_remote(map_to_rank(bar(C::kBarAccEmpty + b), 0));
+      };
+      const uint32_t acc = tmem + lane_base + b * BN + part * (BN / 2);
+      const int n0 = n * BN + part * (BN / 2);
+      if (!(p.epi.out_dtype == RF_FP32
+                ? finish_tile<true>(p.epi, stage, acc, n0, BN / 2, token, frame, ready, read)
+                : finish_tile<false>(p.epi, stage, acc, n0, BN / 2, token, frame, ready, read)))
         break;
-      }
-      tc_fence_after();
-#pragma unroll 1
-      for (int c = 0; c < BN / 64; ++c) {
-        const int col = part * (BN / 2) + c * 32;
-        uint32_t v[32];
-        tmem_ld32(tmem + lane_base + b * BN + col, v);
-        tmem_wait_ld();
-        if (c == BN / 64 - 1) {  // the accumulator is read: it may be written again
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive_remote(map_to_rank(bar(C::kBarAccEmpty + b), 0));
-        }
-        const int n0 = n * BN + col;
-        if (token >= 0 && n0 < p.epi.n_out)
-          finish_row(p.epi, token, frame, n0, *reinterpret_cast<float(*)[32]>(&v));
-      }
     }
   }
   __syncwarp();
@@ -443,7 +495,8 @@ constexpr int kSplitRing = 212992;  // bytes for stages; the sums of a split tak
 constexpr int kSplitBarFull = 0, kSplitBarEmpty = kSplitMaxStages,
               kSplitBarAcc = 2 * kSplitMaxStages, kSplitBars = kSplitBarAcc + 1;
 constexpr int kSplitOffBar = kSplitRing, kSplitOffMisc = kSplitOffBar + kSplitBars * 8,
-              kSplitOffList = kSplitOffMisc + 16, kSplitSmem = kSplitOffList + 256 * 8 + 1024;
+              kSplitOffList = kSplitOffMisc + 16,
+              kSplitSmem = kSplitOffList + sizeof(BoxList<256>) + 1024;
 
 __global__ void __launch_bounds__(kSplitThreads, 1)
     split_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmMany,
@@ -491,7 +544,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1)
 
   if (warp == 0) {
     const bool lead = elect_one();
-    int2* list = reinterpret_cast<int2*>(smem + kSplitOffList);
+    BoxList<256>& list = *reinterpret_cast<BoxList<256>*>(smem + kSplitOffList);
     const RowBoxes x = list_boxes(p.rows, R, r0, BT, list);
     int it = 0;
     for (int kb = kb0; kb < kb1; ++kb, ++it) {

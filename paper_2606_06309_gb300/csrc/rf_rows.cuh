@@ -29,14 +29,21 @@ constexpr int row_unit(int64_t N) { return N < 8 ? 1 : 8; }
 // all, each from a fixed tensor map: a box issued by its own lane under a branch, or with the map
 // chosen per box, held a product's 512-cycle step up to three times its length.
 constexpr int kBoxRows = 32;
+template <int ROWS>  // of a tile of at most ROWS <= 256 rows
+struct BoxList {
+  int tok[ROWS];
+  uint8_t row[ROWS];
+};
 struct RowBoxes {
   int rows;           // rows that the boxes bring
   int n_many, n_unit; // both 0: one box of the whole tile, from token tok
   int tok;
 };
-// Rows [r0, r0 + n) of R, r0 a multiple of the unit; list: n entries.  Warp-collective; the same in
+// Rows [r0, r0 + n) of R, r0 a multiple of the unit; n <= ROWS.  Warp-collective; the same in
 // every lane.  Rows past R are not loaded, except that a tile with none at all gets a box of zeros.
-__device__ __forceinline__ RowBoxes list_boxes(const RowMap& m, int R, int r0, int n, int2* list) {
+template <int ROWS>
+__device__ __forceinline__ RowBoxes list_boxes(const RowMap& m, int R, int r0, int n,
+                                               BoxList<ROWS>& list) {
   RowBoxes x{n, 0, 0, 0};
   const int lane = threadIdx.x & 31;
   const int end = min(r0 + n, R);
@@ -52,17 +59,23 @@ __device__ __forceinline__ RowBoxes list_boxes(const RowMap& m, int R, int r0, i
     x.n_unit = x.rows;
     for (int i = lane; i < x.rows; i += 32) {
       const int r = r0 + i, a = r / m.Np;
-      list[n - 1 - i] = make_int2(m.frame(a) * m.N + (r - a * m.Np), i);
+      list.tok[n - 1 - i] = m.frame(a) * m.N + (r - a * m.Np);
+      list.row[n - 1 - i] = static_cast<uint8_t>(i);
     }
   } else {
     for (int r = r0, a = a0; r < end; ++a) {
       const int q = r - a * m.Np, len = min(m.Np - q, end - r);
       const int many = len / kBoxRows, units = (len - many * kBoxRows) / m.unit;
       const int tok = m.frame(a) * m.N + q;
-      if (lane < many) list[x.n_many + lane] = make_int2(tok + lane * kBoxRows, r - r0 + lane * kBoxRows);
+      if (lane < many) {
+        const int o = lane * kBoxRows;
+        list.tok[x.n_many + lane] = tok + o;
+        list.row[x.n_many + lane] = static_cast<uint8_t>(r - r0 + o);
+      }
       if (lane < units) {
-        const int o = many * kBoxRows + lane * m.unit;
-        list[n - 1 - (x.n_unit + lane)] = make_int2(tok + o, r - r0 + o);
+        const int o = many * kBoxRows + lane * m.unit, i = n - 1 - (x.n_unit + lane);
+        list.tok[i] = tok + o;
+        list.row[i] = static_cast<uint8_t>(r - r0 + o);
       }
       x.n_many += many;
       x.n_unit += units;

@@ -1,0 +1,63 @@
+// rf_stage.cuh -- rows of results between registers and global memory, through shared memory.
+//
+// Accumulators leave tensor memory with a row per lane.  Stored like that, each store instruction
+// of a warp touches 32 rows, 16 bytes in each, and holds up the load/store path that every
+// barrier of the CTA goes through: an attention item's epilogue of 128 columns took 5,700 to 8,100
+// cycles, and the other warps' waits grew with it.  So a warp turns 32 rows x 128 bytes around in 4 KB
+// of shared memory of its own, and moves whole 128-byte lines, eight lanes to a row.
+#pragma once
+#include <cstdint>
+
+#include "rf_ptx.cuh"
+
+namespace rf {
+
+constexpr int kTurnBytes = 4096;  // per warp: 32 rows of 128 bytes, 16-byte pieces swizzled by row
+
+__device__ __forceinline__ uint4& stage_at(uint4* stage, int row, int piece) {
+  return stage[row * 8 + (piece ^ (row & 7))];
+}
+__device__ __forceinline__ int64_t shfl64(int64_t v, int lane) {
+  const uint32_t lo = __shfl_sync(0xffffffffu, static_cast<uint32_t>(v), lane);
+  const uint32_t hi = __shfl_sync(0xffffffffu, static_cast<uint32_t>(v >> 32), lane);
+  return static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
+}
+
+// Each lane's row (128 bytes) to base + its byte offset `at`, nowhere if that is negative.
+__device__ __forceinline__ void store_rows(uint4* stage, const uint4 (&row)[8], char* base, int64_t at) {
+  const int lane = threadIdx.x & 31;
+  __syncwarp();  // the stage's last use is over
+#pragma unroll
+  for (int q = 0; q < 8; ++q) stage_at(stage, lane, q) = row[q];
+  __syncwarp();
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const int r = 4 * k + (lane >> 3);
+    const int64_t o = shfl64(at, r);
+    if (o >= 0) *reinterpret_cast<uint4*>(base + o + (lane & 7) * 16) = stage_at(stage, r, lane & 7);
+  }
+}
+
+// The other way: 128 bytes per row from base + at into the stage (zeros where `at` is negative), in
+// the background.  After await_rows, piece q of this lane's row is at stage_at(stage, lane, q).
+__device__ __forceinline__ void fetch_rows(uint4* stage, const char* base, int64_t at) {
+  const int lane = threadIdx.x & 31;
+  __syncwarp();  // the stage's last use is over
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const int r = 4 * k + (lane >> 3);
+    const int64_t o = shfl64(at, r);
+    const char* src = o >= 0 ? base + o + (lane & 7) * 16 : base;
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
+                     smem_u32(&stage_at(stage, r, lane & 7))),
+                 "l"(src), "r"(o >= 0 ? 16 : 0)
+                 : "memory");
+  }
+  asm volatile("cp.async.commit_group;" ::: "memory");
+}
+__device__ __forceinline__ void await_rows() {
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  __syncwarp();
+}
+
+}  // namespace rf
