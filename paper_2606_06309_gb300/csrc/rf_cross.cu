@@ -46,7 +46,6 @@ constexpr int kThreads = 384;        // three warpgroups
 constexpr int kRegsLaunch = 168, kRegsControl = 104, kRegsSoftmax = 200;
 static_assert(128 * kRegsControl + 256 * kRegsSoftmax <= kThreads * kRegsLaunch, "register split");
 constexpr uint32_t kTmemCols = 512;  // S_A, S_B at 0, 128; O_A, O_B at 256, 384
-constexpr uint32_t kWaitLimitNs = 2000000000u;    // 2 s: no legitimate wait comes close
 constexpr uint64_t kDrainLimitNs = 200000000ull;  // 0.2 s for what is in flight at teardown
 constexpr float kRescaleLog2 = 8.0f;
 // P goes to the tile's MMA warp in two parts of 64 keys, and the two MMA warps take turns, over
@@ -92,18 +91,20 @@ struct CrossParams {
   int tile_frames;     // packed: frames of a tile
   int cluster;
   float scale_log2;
+  FastDiv by_g, by_frame_rows;
 };
 
 __device__ __forceinline__ void flag_error(const CrossParams& p, int where) {
   if (p.status) atomicOr(p.status, RF_ERR_DEVICE_TIMEOUT | (1 << (8 + where)));
 }
 __device__ __forceinline__ bool all_wait(uint32_t bar, uint32_t parity, volatile int* abort) {
-  return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort, kWaitLimitNs));
+  return warp_wait(bar, parity, abort);
 }
 
 // The work of a launch, from the active count on the device.
 struct Work {
   int A, groups, tiles, pairs, items;  // groups of tiles with keys of their own (frames, or one)
+  FastDiv by_pairs, by_groups;
 };
 __device__ __forceinline__ Work make_work(const CrossParams& p) {
   Work w;
@@ -115,6 +116,8 @@ __device__ __forceinline__ Work make_work(const CrossParams& p) {
     w.tiles = ((p.kv_range ? p.rows.N : w.A * p.rows.Np) + kBM - 1) / kBM;
   w.pairs = (w.tiles + 1) / 2;
   w.items = p.units * w.groups * w.pairs;
+  w.by_pairs = FastDiv(max(w.pairs, 1));
+  w.by_groups = FastDiv(max(w.groups, 1));
   return w;
 }
 
@@ -126,9 +129,9 @@ struct Item {
 };
 __device__ __forceinline__ Item get_item(const CrossParams& p, const Work& w, int i, int rank) {
   Item t;
-  const int gp = i / w.pairs;
+  const int gp = w.by_pairs.div(i);
   t.pair = i - gp * w.pairs;
-  t.unit = gp / w.groups;
+  t.unit = w.by_groups.div(gp);
   t.group = gp - t.unit * w.groups;
   t.begin = 0;
   t.end = p.L;
@@ -152,17 +155,17 @@ __device__ __forceinline__ int row_of(const CrossParams& p, const Work& w, const
                                       int row, int& head) {
   head = t.unit;
   if (p.packed) {
-    const int al = row / p.frame_rows, rem = row - al * p.frame_rows;
+    const int al = p.by_frame_rows.div(row), rem = row - al * p.frame_rows;
     const int a = p.kv_range ? t.group : tile * p.tile_frames + al;
     if (al >= p.tile_frames || a >= w.A) return -1;
-    const int q = rem / p.g;
+    const int q = p.by_g.div(rem);
     head = t.unit * p.g + (rem - q * p.g);
     return p.rows.frame(a) * p.rows.N + q;
   }
   const int r = tile * kBM + row;
   if (p.kv_range) return r < p.rows.N ? p.rows.frame(t.group) * p.rows.N + r : -1;
   if (r >= w.A * p.rows.Np) return -1;
-  const int a = r / p.rows.Np, q = r - a * p.rows.Np;
+  const int a = p.rows.by_Np.div(r), q = r - a * p.rows.Np;
   return q < p.rows.N ? p.rows.frame(a) * p.rows.N + q : -1;
 }
 
@@ -194,7 +197,7 @@ struct QueryMaps {
 // What an item's loads need, found before they can be issued.
 struct Load {
   Item t;
-  RowBoxes x[2];
+  RowBoxes x0, x1;
 };
 template <int D>
 __device__ __forceinline__ void prepare_load(const QueryMaps& maps, const CrossParams& p,
@@ -202,20 +205,20 @@ __device__ __forceinline__ void prepare_load(const QueryMaps& maps, const CrossP
                                              Load& n) {
   n.t = get_item(p, w, i, rank);
   if (p.packed || n.t.j0 >= n.t.j1) return;
-#pragma unroll
+#pragma unroll 1
   for (int X = 0; X < 2; ++X) {
     const int tile = 2 * n.t.pair + X;
     if (tile >= w.tiles) break;
-    if (p.kv_range)
-      n.x[X] = RowBoxes{kBM, 0, 0, p.rows.frame(n.t.group) * p.rows.N + tile * kBM};
-    else
-      n.x[X] = list_boxes(p.rows, w.A * p.rows.Np, tile * kBM, kBM, list[X]);
+    const RowBoxes x =
+        p.kv_range ? RowBoxes{kBM, 0, 0, p.rows.frame(n.t.group) * p.rows.N + tile * kBM}
+                   : list_boxes(p.rows, w.A * p.rows.Np, tile * kBM, kBM, list[X]);
+    (X ? n.x1 : n.x0) = x;
     // on their way to L2 while the item before is worked on: the queries' own buffer is free only
     // when that item's last Q K^T is done
-    if (lead && n.x[X].n_many + n.x[X].n_unit == 0)
+    if (lead && x.n_many + x.n_unit == 0)
 #pragma unroll
       for (int hb = 0; hb < Cfg<D>::kHalves; ++hb)
-        tma_prefetch_3d(maps.whole, hb * 64, n.t.unit, n.x[X].tok);
+        tma_prefetch_3d(maps.whole, hb * 64, n.t.unit, x.tok);
   }
 }
 template <int D>
@@ -234,6 +237,7 @@ __device__ __forceinline__ void load_queries(const QueryMaps& maps, const CrossP
     const int a0 = p.kv_range ? t.group : tile * p.tile_frames;
     const int n = min(p.tile_frames, w.A - a0);
     mbar_arrive_expect_tx(bar, n * p.frame_rows * 128 * C::kHalves);
+#pragma unroll 1
     for (int i = 0; i < n; ++i)
       load(maps.unit, i * p.frame_rows, t.unit * p.g, p.rows.frame(a0 + i) * p.rows.N);
     return;
@@ -243,7 +247,9 @@ __device__ __forceinline__ void load_queries(const QueryMaps& maps, const CrossP
     load(maps.whole, 0, t.unit, x.tok);
     return;
   }
+#pragma unroll 1
   for (int i = 0; i < x.n_many; ++i) load(maps.many, list.row[i], t.unit, list.tok[i]);
+#pragma unroll 1
   for (int i = kBM - x.n_unit; i < kBM; ++i) load(maps.unit, list.row[i], t.unit, list.tok[i]);
 }
 
@@ -256,7 +262,7 @@ __device__ __forceinline__ void producer(const QueryMaps& maps, const CUtensorMa
   auto bar = [&](int i) { return bar0 + 8u * i; };
   const bool lead = elect_one();
   const int step = gridDim.x / p.cluster;
-  int q_cnt[2] = {0, 0};
+  int q_cnt0 = 0, q_cnt1 = 0;
   int it = 0;
   bool ok = true;
   Load n;
@@ -264,47 +270,47 @@ __device__ __forceinline__ void producer(const QueryMaps& maps, const CUtensorMa
   if (i < w.items) prepare_load<D>(maps, p, w, i, rank, list, lead, n);
   while (ok && i < w.items) {
     const Item t = n.t;
-    const int hk = p.packed ? t.unit : t.unit / p.g;
-    auto load_kv = [&](int j, int kv) -> bool {
+    const int hk = p.packed ? t.unit : p.by_g.div(t.unit);
+    // K and V of the tiles in turn.  The first keys go before the queries: their slot is free earlier
+#pragma unroll 1
+    for (int n2 = 2 * t.j0; ok && n2 < 2 * t.j1; ++n2) {
       const int s = it % C::kSlots;
-      if (!all_wait(bar(C::kKVEmpty + s), ((it / C::kSlots) & 1) ^ 1, abort)) return false;
+      ok = all_wait(bar(C::kKVEmpty + s), ((it / C::kSlots) & 1) ^ 1, abort);
+      if (!ok) break;
       if (lead) {
+        const CUtensorMap* m = (n2 & 1) ? tmV : tmK;
         mbar_arrive_expect_tx(bar(C::kKVFull + s), C::kTileBytes);
 #pragma unroll
         for (int hb = 0; hb < C::kHalves; ++hb)
-          tma_load_3d(sKV0 + s * C::kTileBytes + hb * C::kHalfBytes, kv ? tmV : tmK,
-                      bar(C::kKVFull + s), hb * 64, hk, t.begin + j * kBN);
+          tma_load_3d(sKV0 + s * C::kTileBytes + hb * C::kHalfBytes, m, bar(C::kKVFull + s),
+                      hb * 64, hk, t.begin + (n2 >> 1) * kBN);
       }
       __syncwarp();
       ++it;
-      return true;
-    };
-    if (t.j0 < t.j1) {
-      // the first keys go before the queries: their slot is free earlier
-      ok = load_kv(t.j0, 0);
-      for (int X = 0; ok && X < 2; ++X) {
+      if (n2 != 2 * t.j0) continue;
+#pragma unroll 1
+      for (int X = 0; X < 2; ++X) {
         const int tile = 2 * t.pair + X;
         if (tile >= w.tiles) break;
-        ok = all_wait(bar(C::kQEmpty + X), (q_cnt[X] & 1) ^ 1, abort);
+        ok = all_wait(bar(C::kQEmpty + X), ((X ? q_cnt1 : q_cnt0) & 1) ^ 1, abort);
         if (!ok) break;
         if (lead)
-          load_queries<D>(maps, p, w, t, tile, n.x[X], list[X], sQ0 + X * C::kTileBytes,
+          load_queries<D>(maps, p, w, t, tile, X ? n.x1 : n.x0, list[X], sQ0 + X * C::kTileBytes,
                           bar(C::kQFull + X));
         __syncwarp();
-        ++q_cnt[X];
+        (X ? q_cnt1 : q_cnt0) += 1;
       }
-      ok = ok && load_kv(t.j0, 1);
-      for (int j = t.j0 + 1; ok && j < t.j1; ++j) ok = load_kv(j, 0) && load_kv(j, 1);
     }
     i += step;
     if (ok && i < w.items) prepare_load<D>(maps, p, w, i, rank, list, lead, n);
   }
   if (!ok && lead) flag_error(p, 0);
   // every copy has landed
+#pragma unroll 1
   for (int s = 0; s < C::kSlots; ++s)
     if (it > s) mbar_drain(bar(C::kKVFull + s), ((it - 1 - s) / C::kSlots) & 1, kDrainLimitNs);
-  for (int X = 0; X < 2; ++X)
-    if (q_cnt[X] > 0) mbar_drain(bar(C::kQFull + X), (q_cnt[X] - 1) & 1, kDrainLimitNs);
+  if (q_cnt0 > 0) mbar_drain(bar(C::kQFull), (q_cnt0 - 1) & 1, kDrainLimitNs);
+  if (q_cnt1 > 0) mbar_drain(bar(C::kQFull + 1), (q_cnt1 - 1) & 1, kDrainLimitNs);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -317,8 +323,10 @@ __device__ __forceinline__ void cleaner(const CrossParams& p, const Work& w, int
   auto bar = [&](int i) { return bar0 + 8u * i; };
   const int lane = threadIdx.x & 31;
   int it = 1;  // V follows K in the ring
+#pragma unroll 1
   for (int i = blockIdx.x / p.cluster; i < w.items; i += gridDim.x / p.cluster) {
     const Item t = get_item(p, w, i, rank);
+#pragma unroll 1
     for (int j = t.j0; j < t.j1; ++j, it += 2) {
       const KeyBits b = key_bits(p, t, j);
       const int s = it % C::kSlots;
@@ -329,6 +337,7 @@ __device__ __forceinline__ void cleaner(const CrossParams& p, const Work& w, int
       if (!b.all()) {
         // a row is 128 bytes in each half: the swizzle moves 16-byte pieces within them
         uint8_t* tile = kv + s * C::kTileBytes;
+#pragma unroll 1
         for (int r = lane; r < kBN; r += 32)
           if (!((b.w[r >> 5] >> lane) & 1u))
 #pragma unroll
@@ -357,12 +366,13 @@ __device__ __forceinline__ void mma_qk(uint32_t tS, uint64_t dQ, uint64_t dK) {
     tc_mma_ss(tS, dQ + off, dK + off, idesc, k > 0);
   }
 }
-template <int D, bool F16, int K0, int K1>
-__device__ __forceinline__ void mma_pv(uint32_t tO, uint32_t tP, uint64_t dV, uint32_t acc) {
+// O (+)= P V over keys [64 part, 64 part + 64) of the tile.
+template <int D, bool F16>
+__device__ __forceinline__ void mma_pv(uint32_t tO, uint32_t tP, uint64_t dV, int part, uint32_t acc) {
   constexpr uint32_t idesc = idesc_f16(F16, kBM, D, 1);
 #pragma unroll
-  for (int k = K0; k < K1; ++k)
-    tc_mma_ts(tO, tP + k * 8, dV + ((k * 2048) >> 4), idesc, (acc | k) != 0);
+  for (int k = 0; k < 4; ++k)
+    tc_mma_ts(tO, tP + part * 32 + k * 8, dV + part * 512 + ((k * 2048) >> 4), idesc, acc | k | part);
 }
 
 template <int D, bool F16, bool CLEAN>
@@ -374,83 +384,71 @@ __device__ __forceinline__ bool mma_issuer(const CrossParams& p, const Work& w, 
   auto bar = [&](int i) { return bar0 + 8u * i; };
   const uint32_t tS = tmem + X * 128, tO = tmem + 256 + X * 128;
   const uint64_t dQ = smem_desc_sw128(sQ0 + X * C::kTileBytes, 16, 1024);
-  auto dK = [&](int s) { return smem_desc_sw128(sKV0 + s * C::kTileBytes, 16, 1024); };
-  auto dV = [&](int s) { return smem_desc_sw128(sKV0 + s * C::kTileBytes, kBN * 128, 1024); };
-  int q_cnt = 0, it = 0;
-  bool my_turn = X == 0;  // the first turn is tile A's
-  auto wait_k = [&](int i) {
-    return all_wait(bar(C::kKVFull + i % C::kSlots), (i / C::kSlots) & 1, abort);
-  };
-  auto wait_v = [&](int i) {  // cleaned, where a launch has keys that may not be seen
-    return all_wait(bar((CLEAN ? C::kVClean : C::kKVFull) + i % C::kSlots), (i / C::kSlots) & 1,
-                    abort);
-  };
-  auto take_turn = [&]() {
-    if (!my_turn) named_sync(turn_barrier(X), 64);
-    my_turn = false;
-  };
-  for (int i = blockIdx.x / p.cluster; i < w.items; i += gridDim.x / p.cluster) {
+  int q_cnt = 0, it = 0;    // it: ring index of the item's first tile of keys
+  bool my_turn = X == 0;    // the first turn is tile A's
+  bool ok = true;
+#pragma unroll 1
+  for (int i = blockIdx.x / p.cluster; ok && i < w.items; i += gridDim.x / p.cluster) {
     const Item t = get_item(p, w, i, rank);
     const int nt = t.j1 - t.j0;
     if (nt <= 0) continue;
-    const bool both = 2 * t.pair + 1 < w.tiles;
-    bool ok = true;
-    if (X == 1 && !both) {  // no such query tile: only give the K/V slots back
-      for (int n = 0; ok && n < 2 * nt; ++n, ++it) {
-        ok = (n & 1) ? wait_v(it) : wait_k(it);
-        if (ok && lead) mbar_arrive(bar(C::kKVEmpty + it % C::kSlots));
-        __syncwarp();
-      }
-      if (!ok) break;
-      continue;
+    const bool both = 2 * t.pair + 1 < w.tiles, mine = X == 0 || both;
+    if (mine) {
+      ok = all_wait(bar(C::kQFull + X), q_cnt & 1, abort);
+      ++q_cnt;
     }
-    if (!all_wait(bar(C::kQFull + X), q_cnt & 1, abort)) break;
-    ++q_cnt;
-    if (!wait_k(it) || !__all_sync(0xffffffffu, *abort == 0)) break;
-    tc_fence_after();
-    if (both) take_turn();
-    if (lead) {
-      mma_qk<D, F16>(tS, dQ, dK(it % C::kSlots));
-      tc_commit(bar(C::kSFull + X));
-      if (nt == 1) tc_commit(bar(C::kQEmpty + X));
-      tc_commit(bar(C::kKVEmpty + it % C::kSlots));
-    }
-    __syncwarp();
-    if (both) named_arrive(turn_barrier(X ^ 1), 64);
-    ++it;
+    // step j: P V of tile j, Q K^T of tile j + 1
 #pragma unroll 1
-    for (int j = 0; j < nt; ++j) {
-      const bool more = j + 1 < nt;
-      const int sV = it % C::kSlots, sK = (it + 1) % C::kSlots;
-      ok = wait_v(it) && (!more || wait_k(it + 1));
-      it += more ? 2 : 1;
-      ok = ok && *abort == 0;
-      if (!__all_sync(0xffffffffu, ok)) break;
-      if (both) take_turn();
-      named_sync(p_barrier(X, 0), kPThreads);
-      tc_fence_after();
-      if (lead) mma_pv<D, F16, 0, 4>(tO, tS, dV(sV), j > 0);
-      __syncwarp();
-      named_sync(p_barrier(X, 1), kPThreads);
-      tc_fence_after();
+    for (int j = -1; ok && j < nt; ++j) {
+      const bool first = j < 0, more = j + 1 < nt;
+      const int iV = it + 2 * j + 1, iK = iV + 1;
+      const int sV = iV % C::kSlots, sK = iK % C::kSlots;
+      // (V cleaned, where a launch has keys that may not be seen)
+      if (!first)
+        ok = all_wait(bar((CLEAN ? C::kVClean : C::kKVFull) + sV), (iV / C::kSlots) & 1, abort);
+      if (ok && more) ok = all_wait(bar(C::kKVFull + sK), (iK / C::kSlots) & 1, abort);
+      ok = __all_sync(0xffffffffu, ok && *abort == 0);
+      if (!ok) break;
+      if (!mine) {  // no such query tile: only give the slots back
+        if (lead) {
+          if (!first) mbar_arrive(bar(C::kKVEmpty + sV));
+          if (more) mbar_arrive(bar(C::kKVEmpty + sK));
+        }
+        __syncwarp();
+        continue;
+      }
+      if (both) {
+        if (!my_turn) named_sync(turn_barrier(X), 64);
+        my_turn = false;
+      }
+      if (!first) {
+        const uint64_t dV = smem_desc_sw128(sKV0 + sV * C::kTileBytes, kBN * 128, 1024);
+#pragma unroll 1
+        for (int part = 0; part < 2; ++part) {
+          named_sync(p_barrier(X, part), kPThreads);
+          tc_fence_after();
+          if (lead) mma_pv<D, F16>(tO, tS, dV, part, j > 0);
+          __syncwarp();
+        }
+      } else {
+        tc_fence_after();
+      }
       if (lead) {
-        mma_pv<D, F16, 4, 8>(tO, tS, dV(sV), 1);
         if (more) {
-          mma_qk<D, F16>(tS, dQ, dK(sK));
+          mma_qk<D, F16>(tS, dQ, smem_desc_sw128(sKV0 + sK * C::kTileBytes, 16, 1024));
           tc_commit(bar(C::kSFull + X));
           // the item's last Q K^T: the next item's queries may come
           if (j + 2 == nt) tc_commit(bar(C::kQEmpty + X));
-          tc_commit(bar(C::kKVEmpty + sV));
           tc_commit(bar(C::kKVEmpty + sK));
         } else {
           tc_commit(bar(C::kODone + X));
-          tc_commit(bar(C::kKVEmpty + sV));
         }
+        if (!first) tc_commit(bar(C::kKVEmpty + sV));
       }
       __syncwarp();
       if (both) named_arrive(turn_barrier(X ^ 1), 64);
     }
-    if (!ok) break;
+    it += 2 * nt;
   }
   // a wait that gave up has raised the flag
   if (__all_sync(0xffffffffu, *abort == 0)) return true;
@@ -627,19 +625,16 @@ __device__ __forceinline__ bool softmax_group(const CrossParams& p, const Work& 
     const float inv_l = none ? 0.f : 1.0f / l;
     uint4* stage = reinterpret_cast<uint4*>(smem + C::kOffStage + (warp - 4) * kTurnBytes);
 #pragma unroll 1
-    for (int c = 0; c < D / 64; ++c) {
-      uint4 v[8];
+    for (int c = 0; c < D / 32; ++c) {
+      uint32_t o[32];
+      tmem_ld32(tO + c * 32, o);
+      tmem_wait_ld();
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        uint32_t o[32];
-        tmem_ld32(tO + c * 64 + half * 32, o);
-        tmem_wait_ld();
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-          v[half * 4 + q] = none ? make_uint4(0u, 0u, 0u, 0u)
-                                 : pack8<F16>(reinterpret_cast<const float*>(o) + q * 8, inv_l);
-      }
-      store_rows(stage, v, reinterpret_cast<char*>(p.O) + c * 128, at);
+      for (int q = 0; q < 4; ++q)
+        stage_at(stage, lane, (c & 1) * 4 + q) =
+            none ? make_uint4(0u, 0u, 0u, 0u)
+                 : pack8<F16>(reinterpret_cast<const float*>(o) + q * 8, inv_l);
+      if (c & 1) store_rows(stage, reinterpret_cast<char*>(p.O) + (c >> 1) * 128, at);
     }
     if (valid && p.lse)
       p.lse[static_cast<int64_t>(head) * p.rows.T + token] =
@@ -686,6 +681,7 @@ __device__ __forceinline__ void join(const CrossParams& p, const Work& w, int ra
   const float inv = none ? 0.f : 1.0f / Lsum;
   uint16_t* orow = p.O + token * p.o_row_stride + static_cast<int64_t>(head) * D;
   // columns in groups of 8: cluster <= 8 = D / 8 at D = 64
+#pragma unroll 1
   for (int c8 = rank; c8 < D / 8; c8 += p.cluster) {
     float acc[8] = {};
     const uint32_t at = sbase + C::kOffKV + (X * (D / 4 * 128) + c8 * 2 * 128 + row) * 16;
@@ -941,7 +937,7 @@ extern "C" rf_status rf_cross_attn(void* d_O, float* d_lse, const void* d_Q, con
   p.key_mask = d_key_mask;
   p.status = d_status;
   p.rows = {d_active, d_counts, static_cast<int>(Fr), static_cast<int>(Nr), static_cast<int>(Np), unit,
-            static_cast<int>(T)};
+            static_cast<int>(T), FastDiv(static_cast<uint32_t>(Np))};
   p.o_row_stride = o_row_stride;
   p.L = L;
   p.g = g;
@@ -949,6 +945,8 @@ extern "C" rf_status rf_cross_attn(void* d_O, float* d_lse, const void* d_Q, con
   p.units = packed ? Hkv : H;
   p.frame_rows = packed ? N * g : 0;
   p.tile_frames = packed ? (d_kv_range ? 1 : kBM / p.frame_rows) : 0;
+  p.by_g = FastDiv(static_cast<uint32_t>(g));
+  p.by_frame_rows = FastDiv(static_cast<uint32_t>(std::max(p.frame_rows, 1)));
   p.scale_log2 = static_cast<float>(static_cast<double>(softmax_scale) * 1.4426950408889634);
 
   // at most, with every frame active

@@ -26,7 +26,6 @@
 namespace rf {
 namespace {
 
-constexpr uint32_t kWaitLimitNs = 2000000000u;    // 2 s: no legitimate wait comes close
 constexpr uint64_t kDrainLimitNs = 200000000ull;  // 0.2 s for what is in flight at teardown
 constexpr int kBlockK = 64;                       // columns of K per stage: 128 bytes, one swizzle atom
 
@@ -111,7 +110,7 @@ __device__ __forceinline__ void finish_one(const Epilogue& e, int64_t token, int
 
 // Columns n .. n + 31 of a row, element by element: the last columns of a result, and rows off the
 // 16-byte boundaries.
-__device__ __forceinline__ void finish_row(const Epilogue& e, int64_t token, int frame, int n,
+static __device__ __noinline__ void finish_row(const Epilogue& e, int64_t token, int frame, int n,
                                            float (&v)[32]) {
 #pragma unroll
   for (int i = 0; i < 32; ++i)
@@ -187,44 +186,47 @@ __device__ __forceinline__ bool finish_tile(const Epilogue& e, uint4* stage, uin
       if (c == chunks - 1) read();
       continue;
     }
-    uint4 row[8];
-    uint32_t* w = reinterpret_cast<uint32_t*>(row);
-#pragma unroll
+#pragma unroll 1
     for (int half = 0; half < kCols / 32; ++half) {
       float v[32];
       tmem_ld32(acc + c * kCols + half * 32, reinterpret_cast<uint32_t(&)[32]>(v));
       tmem_wait_ld();
       if (half == kCols / 32 - 1 && c == chunks - 1) read();
       finish_cols(e, frame, n + half * 32, v);
-      if (e.R) {
-        if (half == 0) await_rows();
+      if (e.R && half == 0) await_rows();
 #pragma unroll
-        for (int q = 0; q < (OUT32 ? 8 : 4); ++q) {
-          const uint4 r = stage_at(stage, lane, half * 4 + q);
-          if (OUT32) {
-            v[4 * q] += __uint_as_float(r.x);
-            v[4 * q + 1] += __uint_as_float(r.y);
-            v[4 * q + 2] += __uint_as_float(r.z);
-            v[4 * q + 3] += __uint_as_float(r.w);
-          } else {
-            add2(r.x, e.out_dtype, v[(8 * q) & 31], v[(8 * q + 1) & 31]);
-            add2(r.y, e.out_dtype, v[(8 * q + 2) & 31], v[(8 * q + 3) & 31]);
-            add2(r.z, e.out_dtype, v[(8 * q + 4) & 31], v[(8 * q + 5) & 31]);
-            add2(r.w, e.out_dtype, v[(8 * q + 6) & 31], v[(8 * q + 7) & 31]);
+      for (int q = 0; q < (OUT32 ? 8 : 4); ++q) {
+        // the residual's piece of this lane's row makes way for the result's
+        uint4& piece = stage_at(stage, lane, half * 4 + q);
+        if (OUT32) {
+          float* x = v + 4 * q;
+          if (e.R) {
+            const uint4 r = piece;
+            x[0] += __uint_as_float(r.x);
+            x[1] += __uint_as_float(r.y);
+            x[2] += __uint_as_float(r.z);
+            x[3] += __uint_as_float(r.w);
           }
+          piece = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]),
+                             __float_as_uint(x[3]));
+        } else {
+          float* x = v + 8 * (q & 3);
+          if (e.R) {
+            const uint4 r = piece;
+            add2(r.x, e.out_dtype, x[0], x[1]);
+            add2(r.y, e.out_dtype, x[2], x[3]);
+            add2(r.z, e.out_dtype, x[4], x[5]);
+            add2(r.w, e.out_dtype, x[6], x[7]);
+          }
+          piece = e.out_dtype == RF_FP16
+                      ? make_uint4(pack_f16x2(x[0], x[1]), pack_f16x2(x[2], x[3]),
+                                   pack_f16x2(x[4], x[5]), pack_f16x2(x[6], x[7]))
+                      : make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]),
+                                   pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
         }
       }
-      if (OUT32) {
-#pragma unroll
-        for (int i = 0; i < 32; ++i) w[i] = __float_as_uint(v[i]);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          w[half * 16 + i] = e.out_dtype == RF_FP16 ? pack_f16x2(v[2 * i], v[2 * i + 1])
-                                                    : pack_bf16x2(v[2 * i], v[2 * i + 1]);
-      }
     }
-    store_rows(stage, row, static_cast<char*>(e.Y) + c * 128, at_y);
+    store_rows(stage, static_cast<char*>(e.Y) + c * 128, at_y);
     if (e.R && c + 1 < chunks && whole(c + 1)) fetch_rows(stage, R + (c + 1) * 128, at_r);
   }
   return true;
@@ -233,7 +235,7 @@ __device__ __forceinline__ bool finish_tile(const Epilogue& e, uint4* stage, uin
 struct LinearParams {
   RowMap rows;
   Epilogue epi;
-  int N;  // tokens per frame, for the gate's row (rows.N where there is no list is all tokens)
+  FastDiv by_N;  // tokens per frame, for the gate's row (without a list rows.N is all tokens)
   int kblocks, n_tiles, fp16;
   int32_t* status;
   // split_kernel
@@ -246,10 +248,10 @@ __device__ __forceinline__ void flag_error(const LinearParams& p, int where) {
 
 // Token and frame of row r (r < rows of the launch); token -1 in a frame's padding.
 __device__ __forceinline__ int row_token(const LinearParams& p, int r, int& frame) {
-  const int a = r / p.rows.Np, q = r - a * p.rows.Np;
+  const int a = p.rows.by_Np.div(r), q = r - a * p.rows.Np;
   const int f = p.rows.frame(a);
   const int token = f * p.rows.N + q;
-  frame = token / p.N;
+  frame = p.by_N.div(token);
   return q < p.rows.N ? token : -1;
 }
 
@@ -269,9 +271,9 @@ __device__ __forceinline__ void load_rows(const RowBoxes& x, const BoxList<ROWS>
     load(maps.whole, 0, x.tok);
     return;
   }
-#pragma unroll 2
+#pragma unroll 1
   for (int i = 0; i < x.n_many; ++i) load(maps.many, list.row[i], list.tok[i]);
-#pragma unroll 2
+#pragma unroll 1
   for (int i = n - x.n_unit; i < n; ++i) load(maps.unit, list.row[i], list.tok[i]);
 }
 
@@ -375,9 +377,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
                         (x.rows + (rank == 0 ? boxed_rows(p.rows, R, m * 256 + 128, 128) : 0)) * 128;
       for (int kb = 0; kb < p.kblocks; ++kb, ++it) {
         const int s = it % C::kStages;
-        if (!__all_sync(0xffffffffu,
-                        mbar_wait_cluster(bar(C::kBarEmpty + s), ((it / C::kStages) & 1) ^ 1, abort,
-                                          kWaitLimitNs))) {
+        if (!warp_wait(bar(C::kBarEmpty + s), ((it / C::kStages) & 1) ^ 1, abort)) {
           if (lead) flag_error(p, 0);
           ok = false;
           break;
@@ -406,9 +406,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
       bool ok = true;
       for (int t = pair; ok && t < tiles; t += pairs, ++n_acc) {
         const int b = n_acc & 1;
-        if (!__all_sync(0xffffffffu,
-                        mbar_wait_cluster(bar(C::kBarAccEmpty + b), ((n_acc >> 1) & 1) ^ 1, abort,
-                                          kWaitLimitNs))) {
+        if (!warp_wait(bar(C::kBarAccEmpty + b), ((n_acc >> 1) & 1) ^ 1, abort)) {
           if (lead) flag_error(p, 1);
           break;
         }
@@ -416,9 +414,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
         const uint32_t acc = tmem + b * BN;
         for (int kb = 0; kb < p.kblocks; ++kb, ++it) {
           const int s = it % C::kStages;
-          if (!__all_sync(0xffffffffu,
-                          mbar_wait_cluster(bar(C::kBarFull + s), (it / C::kStages) & 1, abort,
-                                            kWaitLimitNs))) {
+          if (!warp_wait(bar(C::kBarFull + s), (it / C::kStages) & 1, abort)) {
             if (lead) flag_error(p, 2);
             ok = false;
             break;
@@ -451,9 +447,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
       int frame = 0;
       const int token = r < R ? row_token(p, r, frame) : -1;
       auto ready = [&]() -> bool {
-        const bool ok = __all_sync(0xffffffffu, mbar_wait_cluster(bar(C::kBarAccFull + b),
-                                                                  (n_acc >> 1) & 1, abort,
-                                                                  kWaitLimitNs));
+        const bool ok = warp_wait(bar(C::kBarAccFull + b),
+                                                                  (n_acc >> 1) & 1, abort);
         if (!ok && lane == 0) flag_error(p, 3);
         tc_fence_after();
         return ok;
@@ -549,8 +544,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1)
     int it = 0;
     for (int kb = kb0; kb < kb1; ++kb, ++it) {
       const int s = it % p.stages;
-      if (!__all_sync(0xffffffffu, mbar_wait(bar(kSplitBarEmpty + s), ((it / p.stages) & 1) ^ 1,
-                                             abort, kWaitLimitNs))) {
+      if (!warp_wait(bar(kSplitBarEmpty + s), ((it / p.stages) & 1) ^ 1, abort)) {
         if (lead) flag_error(p, 0);
         break;
       }
@@ -571,8 +565,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1)
     int it = 0;
     for (int kb = kb0; kb < kb1; ++kb, ++it) {
       const int s = it % p.stages;
-      if (!__all_sync(0xffffffffu, mbar_wait(bar(kSplitBarFull + s), (it / p.stages) & 1, abort,
-                                             kWaitLimitNs))) {
+      if (!warp_wait(bar(kSplitBarFull + s), (it / p.stages) & 1, abort)) {
         if (lead) flag_error(p, 1);
         break;
       }
@@ -596,7 +589,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1)
   if (warp >= 4) {
     const int quarter = warp & 3;
     const int col = n * 128 + quarter * 32 + lane;
-    const bool ok = __all_sync(0xffffffffu, mbar_wait(bar(kSplitBarAcc), 0, abort, kWaitLimitNs));
+    const bool ok = warp_wait(bar(kSplitBarAcc), 0, abort);
     if (!ok && lane == 0) flag_error(p, 2);
     tc_fence_after();
 #pragma unroll 1
@@ -791,7 +784,7 @@ extern "C" rf_status rf_linear(void* d_Y, int64_t y_row_stride, int out_dtype, c
 
   LinearParams p{};
   p.rows = {d_active, d_counts, static_cast<int>(Fr), static_cast<int>(Nr), static_cast<int>(Np), unit,
-            static_cast<int>(T)};
+            static_cast<int>(T), FastDiv(static_cast<uint32_t>(Np))};
   Epilogue& e = p.epi;
   e.Y = d_Y;
   e.R = d_R;
@@ -807,7 +800,7 @@ extern "C" rf_status rf_linear(void* d_Y, int64_t y_row_stride, int out_dtype, c
   e.vec = aligned16(d_Y) && y_row_stride * es_out % 16 == 0 &&
           (!d_R || (aligned16(d_R) && r_row_stride * es_out % 16 == 0)) && aligned16(d_bias) &&
           (!d_gate || (aligned16(d_gate) && gate_frame_stride % 4 == 0));
-  p.N = N;
+  p.by_N = FastDiv(static_cast<uint32_t>(N));
   p.kblocks = (d_in + kBlockK - 1) / kBlockK;
   p.fp16 = dtype == RF_FP16;
   p.status = d_status;

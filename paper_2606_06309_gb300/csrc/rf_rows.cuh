@@ -2,6 +2,7 @@
 #pragma once
 #include <cstdint>
 
+#include "rf_div.h"
 #include "rf_tc_ptx.cuh"
 
 namespace rf {
@@ -13,6 +14,7 @@ struct RowMap {
   const int32_t* counts;
   int F, N, Np, unit;
   int T;  // tokens: F * N
+  FastDiv by_Np;
 
   __device__ __forceinline__ int frames() const {
     return active ? min(max(counts[0], 0), F) : F;
@@ -47,8 +49,8 @@ __device__ __forceinline__ RowBoxes list_boxes(const RowMap& m, int R, int r0, i
   RowBoxes x{n, 0, 0, 0};
   const int lane = threadIdx.x & 31;
   const int end = min(r0 + n, R);
-  const int a0 = r0 / m.Np;
-  if (r0 >= R || a0 == (end - 1) / m.Np) {
+  const int a0 = m.by_Np.div(r0);
+  if (r0 >= R || a0 == m.by_Np.div(end - 1)) {
     // rows past the frame bring the tokens that follow, past the last one zeros: never stored
     x.tok = r0 >= R ? m.T : m.frame(a0) * m.N + (r0 - a0 * m.Np);
     return x;
@@ -57,15 +59,17 @@ __device__ __forceinline__ RowBoxes list_boxes(const RowMap& m, int R, int r0, i
   __syncwarp();  // the list's last use is over
   if (m.unit == 1) {
     x.n_unit = x.rows;
+#pragma unroll 1
     for (int i = lane; i < x.rows; i += 32) {
-      const int r = r0 + i, a = r / m.Np;
+      const int r = r0 + i, a = m.by_Np.div(r);
       list.tok[n - 1 - i] = m.frame(a) * m.N + (r - a * m.Np);
       list.row[n - 1 - i] = static_cast<uint8_t>(i);
     }
   } else {
+#pragma unroll 1
     for (int r = r0, a = a0; r < end; ++a) {
       const int q = r - a * m.Np, len = min(m.Np - q, end - r);
-      const int many = len / kBoxRows, units = (len - many * kBoxRows) / m.unit;
+      const int many = len / kBoxRows, units = (len - many * kBoxRows) / 8;
       const int tok = m.frame(a) * m.N + q;
       if (lane < many) {
         const int o = lane * kBoxRows;
@@ -73,7 +77,7 @@ __device__ __forceinline__ RowBoxes list_boxes(const RowMap& m, int R, int r0, i
         list.row[x.n_many + lane] = static_cast<uint8_t>(r - r0 + o);
       }
       if (lane < units) {
-        const int o = many * kBoxRows + lane * m.unit, i = n - 1 - (x.n_unit + lane);
+        const int o = many * kBoxRows + lane * 8, i = n - 1 - (x.n_unit + lane);
         list.tok[i] = tok + o;
         list.row[i] = static_cast<uint8_t>(r - r0 + o);
       }
@@ -88,7 +92,7 @@ __device__ __forceinline__ RowBoxes list_boxes(const RowMap& m, int R, int r0, i
 // list_boxes(...).rows, without the list.
 __device__ __forceinline__ int boxed_rows(const RowMap& m, int R, int r0, int n) {
   const int end = min(r0 + n, R);
-  return r0 >= R || r0 / m.Np == (end - 1) / m.Np ? n : end - r0;
+  return r0 >= R || m.by_Np.div(r0) == m.by_Np.div(end - 1) ? n : end - r0;
 }
 
 }  // namespace rf

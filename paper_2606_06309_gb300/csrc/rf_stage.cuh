@@ -2,9 +2,10 @@
 //
 // Accumulators leave tensor memory with a row per lane.  Stored like that, each store instruction
 // of a warp touches 32 rows, 16 bytes in each, and holds up the load/store path that every
-// barrier of the CTA goes through: an attention item's epilogue of 128 columns took 5,700 to 8,100
-// cycles, and the other warps' waits grew with it.  So a warp turns 32 rows x 128 bytes around in 4 KB
-// of shared memory of its own, and moves whole 128-byte lines, eight lanes to a row.
+// barrier of the CTA goes through.  So a warp turns 32 rows x 128 bytes around in 4 KB of shared
+// memory of its own, and moves whole 128-byte lines, eight lanes to a row.  The loops are kept
+// short: code that runs once per tile comes from the instruction caches beyond the SM's, and unrolled
+// it took an attention item's epilogue of 128 columns 4,800 cycles.
 #pragma once
 #include <cstdint>
 
@@ -23,27 +24,25 @@ __device__ __forceinline__ int64_t shfl64(int64_t v, int lane) {
   return static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
 }
 
-// Each lane's row (128 bytes) to base + its byte offset `at`, nowhere if that is negative.
-__device__ __forceinline__ void store_rows(uint4* stage, const uint4 (&row)[8], char* base, int64_t at) {
+// Each lane's row, written to the stage (piece q at stage_at(stage, lane, q)), to base + its byte offset
+// `at`, nowhere if that is negative.
+__device__ __forceinline__ void store_rows(uint4* stage, char* base, int64_t at) {
   const int lane = threadIdx.x & 31;
-  __syncwarp();  // the stage's last use is over
-#pragma unroll
-  for (int q = 0; q < 8; ++q) stage_at(stage, lane, q) = row[q];
   __syncwarp();
-#pragma unroll
+#pragma unroll 2
   for (int k = 0; k < 8; ++k) {
     const int r = 4 * k + (lane >> 3);
     const int64_t o = shfl64(at, r);
     if (o >= 0) *reinterpret_cast<uint4*>(base + o + (lane & 7) * 16) = stage_at(stage, r, lane & 7);
   }
+  __syncwarp();  // the stage may be written again
 }
 
 // The other way: 128 bytes per row from base + at into the stage (zeros where `at` is negative), in
 // the background.  After await_rows, piece q of this lane's row is at stage_at(stage, lane, q).
 __device__ __forceinline__ void fetch_rows(uint4* stage, const char* base, int64_t at) {
   const int lane = threadIdx.x & 31;
-  __syncwarp();  // the stage's last use is over
-#pragma unroll
+#pragma unroll 2
   for (int k = 0; k < 8; ++k) {
     const int r = 4 * k + (lane >> 3);
     const int64_t o = shfl64(at, r);

@@ -56,25 +56,27 @@ __device__ __forceinline__ bool mbar_try_wait_cluster(uint32_t bar, uint32_t par
       : "memory");
   return ok != 0;
 }
-// mbar_wait for a barrier that other CTAs of the cluster arrive on.
-__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity,
-                                                  volatile int* abort, uint32_t limit_ns) {
-  uint32_t t0 = 0;
+// A warp's wait for the phase of parity `parity` of `bar`, on which threads of this CTA, of others of
+// the cluster, or asynchronous operations arrive; the result is the same in every lane.  Gives up, and
+// raises *abort, after kWaitPolls polls, or when another thread of the CTA has raised it.  A poll may
+// suspend the thread for some time; the fastest takes about 20 cycles, so that the limit is between
+// 0.4 s and some seconds, where no legitimate wait comes near a millisecond per 100,000 columns of a
+// product.  No clock is read: the waits of a kernel are many, and its code has to fit the
+// instruction caches.
+constexpr uint32_t kWaitPolls = 40000000u;
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort) {
+  bool ok = true;
 #pragma unroll 1
-  for (uint32_t n = 0;; ++n) {
-    if (mbar_try_wait_cluster(bar, parity)) return true;
-    if ((n & 31) != 31) continue;
-    if (*abort) return false;
-    const uint32_t t = globaltimer_lo_ns();
-    if (n == 31) t0 = t;
-    if (n >= limit_ns || t - t0 > limit_ns) {
+  for (uint32_t n = 0; !mbar_try_wait_cluster(bar, parity);)
+    if (++n >= kWaitPolls || ((n & 63) == 0 && *abort)) {
       *abort = 1;
-      return false;
+      ok = false;
+      break;
     }
-  }
+  return __all_sync(0xffffffffu, ok);
 }
 // Wait, with a limit, with no regard to the abort flag (teardown only).
-__device__ __forceinline__ void mbar_drain(uint32_t bar, uint32_t parity, uint64_t limit_ns) {
+static __device__ __noinline__ void mbar_drain(uint32_t bar, uint32_t parity, uint64_t limit_ns) {
   if (mbar_try_wait_cluster(bar, parity)) return;
   const uint64_t t0 = globaltimer_ns();
   while (!mbar_try_wait_cluster(bar, parity))
