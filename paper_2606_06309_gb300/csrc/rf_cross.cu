@@ -62,15 +62,15 @@ struct Cfg {
   static constexpr int kHalfBytes = 128 * 128;
   static constexpr int kSlots = D == 128 ? 4 : 8;  // K in even slots, V in odd ones
   static constexpr int kOffKV = 2 * kTileBytes;
-  static constexpr int kOffBar = kOffKV + kSlots * kTileBytes;
+  static constexpr int kOffStage = kOffKV + kSlots * kTileBytes;  // rows of results, per softmax warp
+  static constexpr int kOffBar = kOffStage + 8 * kTurnBytes;
   static constexpr int kQFull = 0, kQEmpty = 2, kKVFull = 4, kKVEmpty = 4 + kSlots,
                        kVClean = 4 + 2 * kSlots, kSFull = 4 + 3 * kSlots, kODone = kSFull + 2,
                        kDrain = kODone + 2, kBars = kDrain + 2;
   static constexpr int kOffMisc = kOffBar + kBars * 8;  // tensor memory address, abort, MMA done [2]
-  static constexpr int kOffList = kOffMisc + 32;           // boxes of the query tiles
-  static constexpr int kOffStage =
-      (kOffList + 2 * static_cast<int>(sizeof(BoxList<kBM>)) + 15) / 16 * 16;  // rows of results, per softmax warp
-  static constexpr int kSmem = kOffStage + 8 * kTurnBytes + 1024;  // + slack to align the base
+  static constexpr int kOffList = kOffMisc + 32;        // boxes of the query tiles
+  static constexpr int kSmem =                          // + slack to align the base
+      kOffList + 2 * static_cast<int>(sizeof(BoxList<kBM>)) + 1024;
   // A split item's rows: [tile][D / 4][128] float4 over the K/V ring, {max, sum} [tile][128] over
   // the queries
   static_assert(2 * 128 * D * 4 <= kSlots * kTileBytes, "partial rows fit the ring");
@@ -98,7 +98,7 @@ __device__ __forceinline__ void flag_error(const CrossParams& p, int where) {
   if (p.status) atomicOr(p.status, RF_ERR_DEVICE_TIMEOUT | (1 << (8 + where)));
 }
 __device__ __forceinline__ bool all_wait(uint32_t bar, uint32_t parity, volatile int* abort) {
-  return warp_wait(bar, parity, abort);
+  return warp_wait<false>(bar, parity, abort);
 }
 
 // The work of a launch, from the active count on the device.
@@ -167,6 +167,16 @@ __device__ __forceinline__ int row_of(const CrossParams& p, const Work& w, const
   if (r >= w.A * p.rows.Np) return -1;
   const int a = p.rows.by_Np.div(r), q = r - a * p.rows.Np;
   return q < p.rows.N ? p.rows.frame(a) * p.rows.N + q : -1;
+}
+
+// The first of the 128 consecutive tokens of one head that a tile's rows are, or -1: rows of several
+// frames or heads, or fewer than 128.
+__device__ __forceinline__ int whole_tile(const CrossParams& p, const Work& w, const Item& t, int tile) {
+  const int r = tile * kBM;
+  if (p.packed) return -1;
+  if (p.kv_range) return r + kBM <= p.rows.N ? p.rows.frame(t.group) * p.rows.N + r : -1;
+  const int a = p.rows.by_Np.div(r), q = r - a * p.rows.Np;
+  return a < w.A && q + kBM <= p.rows.N ? p.rows.frame(a) * p.rows.N + q : -1;
 }
 
 // Which keys of tile j a row may see: bit c of word c / 32.  Warp-collective.
@@ -569,7 +579,7 @@ __device__ __forceinline__ bool softmax_item(const CrossParams& p, const Item& t
 }
 
 template <int D, bool F16, bool CLEAN>
-__device__ __forceinline__ bool softmax_group(const CrossParams& p, const Work& w, int rank, int X,
+__device__ __forceinline__ bool softmax_group(const CUtensorMap* tmO, const CrossParams& p, const Work& w, int rank, int X,
                                               uint32_t tmem, uint8_t* smem, uint32_t bar0,
                                               volatile int* abort) {
   using C = Cfg<D>;
@@ -578,7 +588,10 @@ __device__ __forceinline__ bool softmax_group(const CrossParams& p, const Work& 
   const int row = (warp & 3) * 32 + lane;  // and lane of tensor memory
   const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
   const uint32_t tS = tmem + lane_base + X * 128, tO = tmem + lane_base + 256 + X * 128;
+  uint4* stage = reinterpret_cast<uint4*>(smem + C::kOffStage + (warp - 4) * kTurnBytes);
+  int64_t at = -1;  // byte offset of this thread's row in O
   int s_cnt = 0, o_cnt = 0;
+#pragma unroll 1
   for (int i = blockIdx.x / p.cluster; i < w.items; i += gridDim.x / p.cluster) {
     const Item t = get_item(p, w, i, rank);
     const int tile = 2 * t.pair + X;
@@ -616,31 +629,47 @@ __device__ __forceinline__ bool softmax_group(const CrossParams& p, const Work& 
       reinterpret_cast<float2*>(smem)[X * 128 + row] = make_float2(m, l);
       return true;  // one item per CTA; joined after the cluster's barrier
     }
-    int head;
-    const int64_t token = row_of(p, w, t, tile, row, head);
-    const bool valid = token >= 0;
-    const int64_t at = valid ? (token * p.o_row_stride + static_cast<int64_t>(head) * D) * 2 : -1;
     // no key: zeros, not 0 * accumulator, which may hold anything
     const bool none = l == 0.f;
     const float inv_l = none ? 0.f : 1.0f / l;
-    uint4* stage = reinterpret_cast<uint4*>(smem + C::kOffStage + (warp - 4) * kTurnBytes);
-#pragma unroll 1
-    for (int c = 0; c < D / 32; ++c) {
-      uint32_t o[32];
-      tmem_ld32(tO + c * 32, o);
-      tmem_wait_ld();
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-        stage_at(stage, lane, (c & 1) * 4 + q) =
-            none ? make_uint4(0u, 0u, 0u, 0u)
-                 : pack8<F16>(reinterpret_cast<const float*>(o) + q * 8, inv_l);
-      if (c & 1) store_rows(stage, reinterpret_cast<char*>(p.O) + (c >> 1) * 128, at);
+    const int first = whole_tile(p, w, t, tile);
+    if (first < 0 || p.lse) {
+      int head;
+      const int64_t token = row_of(p, w, t, tile, row, head);
+      at = token < 0 ? -1 : (token * p.o_row_stride + static_cast<int64_t>(head) * D) * 2;
+      if (token >= 0 && p.lse)
+        p.lse[static_cast<int64_t>(head) * p.rows.T + token] =
+            none ? -INFINITY : (m + __log2f(l)) * 0.69314718055994531f;
     }
-    if (valid && p.lse)
-      p.lse[static_cast<int64_t>(head) * p.rows.T + token] =
-          none ? -INFINITY : (m + __log2f(l)) * 0.69314718055994531f;
+#pragma unroll 1
+    for (int c = 0; c < D / 64; ++c) {
+      uint32_t o[64];
+      tmem_ld32(tO + c * 64, reinterpret_cast<uint32_t(&)[32]>(o[0]));
+      tmem_ld32(tO + c * 64 + 32, reinterpret_cast<uint32_t(&)[32]>(o[32]));
+      tmem_wait_ld();
+      if (lane == 0) bulk_wait_read();  // the stage's last tile has been read
+      __syncwarp();
+#pragma unroll
+      for (int q = 0; q < 8; ++q)
+        stage_at(stage, lane, q) = none ? make_uint4(0u, 0u, 0u, 0u)
+                                        : pack8<F16>(reinterpret_cast<const float*>(o) + q * 8, inv_l);
+      if (first >= 0) {
+        // 32 consecutive tokens: in the background
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) {
+          tma_store_3d(tmO, smem_u32(stage), c * 64, t.unit, first + (warp & 3) * 32);
+          bulk_commit();
+        }
+      } else {
+        store_rows(stage, reinterpret_cast<char*>(p.O) + c * 128, row_span(at, p.o_row_stride * 2),
+                   p.o_row_stride * 2);
+      }
+    }
     // (the accumulator is read before the next item's first P, so before its first P V)
   }
+  if (lane == 0) bulk_wait_all();
+  __syncwarp();
   return true;
 }
 
@@ -721,7 +750,8 @@ template <int D, bool F16, bool CLEAN>
 __global__ void __launch_bounds__(kThreads, 1)
     cross_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmMany,
                  const __grid_constant__ CUtensorMap tmUnit, const __grid_constant__ CUtensorMap tmK,
-                 const __grid_constant__ CUtensorMap tmV, const CrossParams p) {
+                 const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmO,
+                 const CrossParams p) {
   using C = Cfg<D>;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
@@ -790,7 +820,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   } else {
     reg_alloc<kRegsSoftmax>();
     const int X = (warp - 4) >> 2;
-    if (!softmax_group<D, F16, CLEAN>(p, w, rank, X, tmem, smem, bar0, abort))
+    if (!softmax_group<D, F16, CLEAN>(&tmO, p, w, rank, X, tmem, smem, bar0, abort))
       release_mma(mma_done + X, p_barrier(X, 0), p_barrier(X, 1), kPThreads);
   }
   __syncwarp();
@@ -814,7 +844,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 // Host side
 // ---------------------------------------------------------------------------------------
 struct Maps {
-  CUtensorMap q, many, unit, k, v;
+  CUtensorMap q, many, unit, k, v, o;
 };
 
 // [rows][heads][d] elements of 16 bits, boxes of 64 x box_heads x box_rows.
@@ -851,7 +881,7 @@ rf_status launch(const Maps& m, const CrossParams& p, int grid, const DeviceInfo
   cfg.attrs = &attr;
   cfg.numAttrs = p.cluster > 1 ? 1 : 0;
   if (cudaError_t e = cudaLaunchKernelEx(&cfg, cross_kernel<D, F16, CLEAN>, m.q, m.many, m.unit, m.k,
-                                         m.v, p)) {
+                                         m.v, m.o, p)) {
     cudaGetLastError();
     return fail(RF_ERR_CUDA, "rf_cross_attn launch", e);
   }
@@ -975,6 +1005,7 @@ extern "C" rf_status rf_cross_attn(void* d_O, float* d_lse, const void* d_Q, con
   }
   if (rf_status st = map_heads(&m.k, dtype, K, d, Hkv, rows_kv, k_row_stride, 1, kBN)) return st;
   if (rf_status st = map_heads(&m.v, dtype, V, d, Hkv, rows_kv, v_row_stride, 1, kBN)) return st;
+  if (rf_status st = map_heads(&m.o, dtype, d_O, d, H, T, o_row_stride, 1, 32)) return st;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   const bool clean = d_kv_range || d_key_mask;
   return d == 128 ? launch_dim<128>(dtype == RF_FP16, clean, m, p, grid, di, s)

@@ -162,12 +162,14 @@ __device__ __forceinline__ bool finish_tile(const Epilogue& e, uint4* stage, uin
                                             Read&& read) {
   constexpr int kCols = OUT32 ? 32 : 64, kBytes = OUT32 ? 4 : 2;
   const int chunks = (min(cols, max(e.n_out - n0, 0)) + kCols - 1) / kCols;
-  const int64_t at_y = token < 0 ? -1 : (token * e.y_stride + n0) * kBytes;
-  const int64_t at_r = token < 0 || !e.R ? -1 : (token * e.r_stride + n0) * kBytes;
-  const char* R = static_cast<const char*>(e.R);
+  const int64_t y_bytes = e.y_stride * kBytes, r_bytes = e.r_stride * kBytes;
+  const RowSpan span_y = row_span(token < 0 ? -1 : token * y_bytes, y_bytes);
+  const RowSpan span_r = row_span(token < 0 ? -1 : token * r_bytes, r_bytes);
+  char* Y = static_cast<char*>(e.Y) + static_cast<int64_t>(n0) * kBytes;
+  const char* R = static_cast<const char*>(e.R) + static_cast<int64_t>(n0) * kBytes;
   const int lane = threadIdx.x & 31;
   auto whole = [&](int c) { return e.vec && n0 + (c + 1) * kCols <= e.n_out; };
-  if (e.R && chunks > 0 && whole(0)) fetch_rows(stage, R, at_r);
+  if (e.R && chunks > 0 && whole(0)) fetch_rows(stage, R, span_r, r_bytes);
   if (!ready()) return false;
   if (chunks == 0) read();
 #pragma unroll 1
@@ -226,8 +228,9 @@ __device__ __forceinline__ bool finish_tile(const Epilogue& e, uint4* stage, uin
         }
       }
     }
-    store_rows(stage, static_cast<char*>(e.Y) + c * 128, at_y);
-    if (e.R && c + 1 < chunks && whole(c + 1)) fetch_rows(stage, R + (c + 1) * 128, at_r);
+    store_rows(stage, Y + c * 128, span_y, y_bytes);
+    if (e.R && c + 1 < chunks && whole(c + 1)) 
+      fetch_rows(stage, R + (c + 1) * 128, span_r, r_bytes);
   }
   return true;
 }
@@ -377,7 +380,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
                         (x.rows + (rank == 0 ? boxed_rows(p.rows, R, m * 256 + 128, 128) : 0)) * 128;
       for (int kb = 0; kb < p.kblocks; ++kb, ++it) {
         const int s = it % C::kStages;
-        if (!warp_wait(bar(C::kBarEmpty + s), ((it / C::kStages) & 1) ^ 1, abort)) {
+        if (!warp_wait<true>(bar(C::kBarEmpty + s), ((it / C::kStages) & 1) ^ 1, abort)) {
           if (lead) flag_error(p, 0);
           ok = false;
           break;
@@ -406,7 +409,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
       bool ok = true;
       for (int t = pair; ok && t < tiles; t += pairs, ++n_acc) {
         const int b = n_acc & 1;
-        if (!warp_wait(bar(C::kBarAccEmpty + b), ((n_acc >> 1) & 1) ^ 1, abort)) {
+        if (!warp_wait<true>(bar(C::kBarAccEmpty + b), ((n_acc >> 1) & 1) ^ 1, abort)) {
           if (lead) flag_error(p, 1);
           break;
         }
@@ -414,7 +417,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
         const uint32_t acc = tmem + b * BN;
         for (int kb = 0; kb < p.kblocks; ++kb, ++it) {
           const int s = it % C::kStages;
-          if (!warp_wait(bar(C::kBarFull + s), (it / C::kStages) & 1, abort)) {
+          if (!warp_wait<true>(bar(C::kBarFull + s), (it / C::kStages) & 1, abort)) {
             if (lead) flag_error(p, 2);
             ok = false;
             break;
@@ -447,7 +450,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
       int frame = 0;
       const int token = r < R ? row_token(p, r, frame) : -1;
       auto ready = [&]() -> bool {
-        const bool ok = warp_wait(bar(C::kBarAccFull + b),
+        const bool ok = warp_wait<true>(bar(C::kBarAccFull + b),
                                                                   (n_acc >> 1) & 1, abort);
         if (!ok && lane == 0) flag_error(p, 3);
         tc_fence_after();
@@ -544,7 +547,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1)
     int it = 0;
     for (int kb = kb0; kb < kb1; ++kb, ++it) {
       const int s = it % p.stages;
-      if (!warp_wait(bar(kSplitBarEmpty + s), ((it / p.stages) & 1) ^ 1, abort)) {
+      if (!warp_wait<false>(bar(kSplitBarEmpty + s), ((it / p.stages) & 1) ^ 1, abort)) {
         if (lead) flag_error(p, 0);
         break;
       }
@@ -565,7 +568,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1)
     int it = 0;
     for (int kb = kb0; kb < kb1; ++kb, ++it) {
       const int s = it % p.stages;
-      if (!warp_wait(bar(kSplitBarFull + s), (it / p.stages) & 1, abort)) {
+      if (!warp_wait<false>(bar(kSplitBarFull + s), (it / p.stages) & 1, abort)) {
         if (lead) flag_error(p, 1);
         break;
       }
@@ -589,7 +592,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1)
   if (warp >= 4) {
     const int quarter = warp & 3;
     const int col = n * 128 + quarter * 32 + lane;
-    const bool ok = warp_wait(bar(kSplitBarAcc), 0, abort);
+    const bool ok = warp_wait<false>(bar(kSplitBarAcc), 0, abort);
     if (!ok && lane == 0) flag_error(p, 2);
     tc_fence_after();
 #pragma unroll 1

@@ -13,7 +13,7 @@
 
 namespace rf {
 
-constexpr int kTurnBytes = 4096;  // per warp: 32 rows of 128 bytes, 16-byte pieces swizzled by row
+constexpr int kTurnBytes = 4096;  // per warp: 32 rows of 128 bytes, 16-byte pieces swizzled by row (TMA's 128-byte swizzle)
 
 __device__ __forceinline__ uint4& stage_at(uint4* stage, int row, int piece) {
   return stage[row * 8 + (piece ^ (row & 7))];
@@ -24,28 +24,55 @@ __device__ __forceinline__ int64_t shfl64(int64_t v, int lane) {
   return static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
 }
 
-// Each lane's row, written to the stage (piece q at stage_at(stage, lane, q)), to base + its byte offset
-// `at`, nowhere if that is negative.
-__device__ __forceinline__ void store_rows(uint4* stage, char* base, int64_t at) {
+// Where a warp's 32 rows lie in global memory.
+struct RowSpan {
+  int64_t at;    // this lane's byte offset, negative: none
+  int64_t at0;   // lane 0's
+  int n;         // regular: rows 0 .. n - 1 lie at at0 + row * stride, the others nowhere
+  bool regular;
+};
+__device__ __forceinline__ RowSpan row_span(int64_t at, int64_t stride) {
+  RowSpan s;
+  s.at = at;
+  s.at0 = shfl64(at, 0);
+  s.n = __popc(__ballot_sync(0xffffffffu, at >= 0));
+  const int lane = threadIdx.x & 31;
+  s.regular = __all_sync(0xffffffffu, at == (lane < s.n ? s.at0 + lane * stride : -1));
+  return s;
+}
+
+// Each lane's row, written to the stage (piece q at stage_at(stage, lane, q)), to base + its offset.
+__device__ __forceinline__ void store_rows(uint4* stage, char* base, const RowSpan& s,
+                                           int64_t stride) {
   const int lane = threadIdx.x & 31;
   __syncwarp();
-#pragma unroll 2
-  for (int k = 0; k < 8; ++k) {
-    const int r = 4 * k + (lane >> 3);
-    const int64_t o = shfl64(at, r);
-    if (o >= 0) *reinterpret_cast<uint4*>(base + o + (lane & 7) * 16) = stage_at(stage, r, lane & 7);
+  if (s.regular) {
+    char* p = base + s.at0 + (lane >> 3) * stride + (lane & 7) * 16;
+#pragma unroll
+    for (int k = 0; k < 8; ++k, p += 4 * stride)
+      if (4 * k + (lane >> 3) < s.n)
+        *reinterpret_cast<uint4*>(p) = stage_at(stage, 4 * k + (lane >> 3), lane & 7);
+  } else {
+#pragma unroll 1
+    for (int k = 0; k < 8; ++k) {
+      const int r = 4 * k + (lane >> 3);
+      const int64_t o = shfl64(s.at, r);
+      if (o >= 0)
+        *reinterpret_cast<uint4*>(base + o + (lane & 7) * 16) = stage_at(stage, r, lane & 7);
+    }
   }
   __syncwarp();  // the stage may be written again
 }
 
-// The other way: 128 bytes per row from base + at into the stage (zeros where `at` is negative), in
+// The other way: 128 bytes per row from base + at into the stage (zeros where there is no row), in
 // the background.  After await_rows, piece q of this lane's row is at stage_at(stage, lane, q).
-__device__ __forceinline__ void fetch_rows(uint4* stage, const char* base, int64_t at) {
+__device__ __forceinline__ void fetch_rows(uint4* stage, const char* base, const RowSpan& s,
+                                           int64_t stride) {
   const int lane = threadIdx.x & 31;
-#pragma unroll 2
+#pragma unroll 1
   for (int k = 0; k < 8; ++k) {
     const int r = 4 * k + (lane >> 3);
-    const int64_t o = shfl64(at, r);
+    const int64_t o = s.regular ? (r < s.n ? s.at0 + r * stride : -1) : shfl64(s.at, r);
     const char* src = o >= 0 ? base + o + (lane & 7) * 16 : base;
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
                      smem_u32(&stage_at(stage, r, lane & 7))),

@@ -64,10 +64,12 @@ __device__ __forceinline__ bool mbar_try_wait_cluster(uint32_t bar, uint32_t par
 // product.  No clock is read: the waits of a kernel are many, and its code has to fit the
 // instruction caches.
 constexpr uint32_t kWaitPolls = 40000000u;
+template <bool CLUSTER>  // whether other CTAs arrive on the barrier
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort) {
   bool ok = true;
 #pragma unroll 1
-  for (uint32_t n = 0; !mbar_try_wait_cluster(bar, parity);)
+  for (uint32_t n = 0;
+       !(CLUSTER ? mbar_try_wait_cluster(bar, parity) : mbar_try_wait(bar, parity));)
     if (++n >= kWaitPolls || ((n & 63) == 0 && *abort)) {
       *abort = 1;
       ok = false;
@@ -113,6 +115,25 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map
       " [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
       "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1), "r"(c2)
       : "memory");
+}
+// A tile from shared memory, after fence_proxy_async by the threads that wrote it.
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, uint32_t src, int c0, int c1,
+                                             int c2) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(
+          reinterpret_cast<uint64_t>(map)),
+      "r"(src), "r"(c0), "r"(c1), "r"(c2)
+      : "memory");
+}
+__device__ __forceinline__ void bulk_commit() {
+  asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+// This thread's bulk stores have read their shared memory; have been written.
+__device__ __forceinline__ void bulk_wait_read() {
+  asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+}
+__device__ __forceinline__ void bulk_wait_all() {
+  asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
 }
 // Bring a tile to L2 only.
 __device__ __forceinline__ void tma_prefetch_3d(const CUtensorMap* map, int c0, int c1, int c2) {
