@@ -263,8 +263,8 @@ struct RowMaps {
   const CUtensorMap *whole, *many, *unit;
 };
 // Issue the copies of one k block of a tile of n rows (the bytes are announced before; one thread).
-template <bool PAIR, int ROWS>
-__device__ __forceinline__ void load_rows(const RowBoxes& x, const BoxList<ROWS>& list, int n,
+template <bool PAIR, int CAP>
+__device__ __forceinline__ void load_rows(const RowBoxes& x, const BoxList<CAP>& list,
                                           const RowMaps& maps, uint32_t dst, uint32_t bar, int k0) {
   auto load = [&](const CUtensorMap* m, int row, int tok) {
     if (PAIR) tma_load_2d_pair(dst + row * 128, m, bar, k0, tok);
@@ -277,7 +277,7 @@ __device__ __forceinline__ void load_rows(const RowBoxes& x, const BoxList<ROWS>
 #pragma unroll 1
   for (int i = 0; i < x.n_many; ++i) load(maps.many, list.row[i], list.tok[i]);
 #pragma unroll 1
-  for (int i = n - x.n_unit; i < n; ++i) load(maps.unit, list.row[i], list.tok[i]);
+  for (int i = CAP - x.n_unit; i < CAP; ++i) load(maps.unit, list.row[i], list.tok[i]);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -391,7 +391,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
         if (lead) {
           if (rank == 0) mbar_arrive_expect_tx(bar(C::kBarFull + s), bytes);
           tma_load_2d_pair(dst + C::kABytes, &tmW, full, kb * kBlockK, w0);
-          load_rows<true>(x, list, 128, {&tmX, &tmMany, &tmUnit}, dst, full, kb * kBlockK);
+          load_rows<true>(x, list, {&tmX, &tmMany, &tmUnit}, dst, full, kb * kBlockK);
         }
         __syncwarp();
       }
@@ -555,7 +555,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1)
       if (lead) {
         mbar_arrive_expect_tx(bar(kSplitBarFull + s), 16384 + x.rows * 128);
         tma_load_2d(dst, &tmW, bar(kSplitBarFull + s), kb * kBlockK, n * 128);
-        load_rows<false>(x, list, BT, {&tmX, &tmMany, &tmUnit}, dst + 16384,
+        load_rows<false>(x, list, {&tmX, &tmMany, &tmUnit}, dst + 16384,
                          bar(kSplitBarFull + s), kb * kBlockK);
       }
       __syncwarp();

@@ -31,21 +31,22 @@ constexpr int row_unit(int64_t N) { return N < 8 ? 1 : 8; }
 // all, each from a fixed tensor map: a box issued by its own lane under a branch, or with the map
 // chosen per box, held a product's 512-cycle step up to three times its length.
 constexpr int kBoxRows = 32;
-template <int ROWS>  // of a tile of at most ROWS <= 256 rows
+template <int CAP>  // boxes at most; a tile has at most 256 rows
 struct BoxList {
-  int tok[ROWS];
-  uint8_t row[ROWS];
+  int tok[CAP];
+  uint8_t row[CAP];
 };
 struct RowBoxes {
   int rows;           // rows that the boxes bring
   int n_many, n_unit; // both 0: one box of the whole tile, from token tok
   int tok;
 };
-// Rows [r0, r0 + n) of R, r0 a multiple of the unit; n <= ROWS.  Warp-collective; the same in
+// Rows [r0, r0 + n) of R, r0 a multiple of the unit; with room for n / unit
+// boxes.  Warp-collective; the same in
 // every lane.  Rows past R are not loaded, except that a tile with none at all gets a box of zeros.
-template <int ROWS>
+template <int CAP>
 __device__ __forceinline__ RowBoxes list_boxes(const RowMap& m, int R, int r0, int n,
-                                               BoxList<ROWS>& list) {
+                                               BoxList<CAP>& list) {
   RowBoxes x{n, 0, 0, 0};
   const int lane = threadIdx.x & 31;
   const int end = min(r0 + n, R);
@@ -62,8 +63,8 @@ __device__ __forceinline__ RowBoxes list_boxes(const RowMap& m, int R, int r0, i
 #pragma unroll 1
     for (int i = lane; i < x.rows; i += 32) {
       const int r = r0 + i, a = m.by_Np.div(r);
-      list.tok[n - 1 - i] = m.frame(a) * m.N + (r - a * m.Np);
-      list.row[n - 1 - i] = static_cast<uint8_t>(i);
+      list.tok[CAP - 1 - i] = m.frame(a) * m.N + (r - a * m.Np);
+      list.row[CAP - 1 - i] = static_cast<uint8_t>(i);
     }
   } else {
 #pragma unroll 1
@@ -77,7 +78,7 @@ __device__ __forceinline__ RowBoxes list_boxes(const RowMap& m, int R, int r0, i
         list.row[x.n_many + lane] = static_cast<uint8_t>(r - r0 + o);
       }
       if (lane < units) {
-        const int o = many * kBoxRows + lane * 8, i = n - 1 - (x.n_unit + lane);
+        const int o = many * kBoxRows + lane * 8, i = CAP - 1 - (x.n_unit + lane);
         list.tok[i] = tok + o;
         list.row[i] = static_cast<uint8_t>(r - r0 + o);
       }
