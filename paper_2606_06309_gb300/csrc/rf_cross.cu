@@ -5,14 +5,13 @@
 // over the keys j of the token's frame: all L states, or the frame's own range of them, without the
 // masked ones.  A row that sees no key gets O = 0 and LSE = -inf.
 //
-// One CTA per SM, 512 threads.  Warp 0 brings query tiles and K/V tiles of 128 keys by TMA, warps 1
-// and 2 issue the products of query tile A and B (S = Q K^T, O += P V, P over S in tensor memory),
-// warpgroups 1 and 2 hold the running maximum and sum of their tile's rows in registers, fp32, and
-// rescale O only when a row's maximum grows by more than 2^8, and warpgroup 3 writes the results.
-// Encoder states are few: an item (a pair of query tiles over one frame's keys) is often only four K/V
-// tiles long, 9,200 cycles, and what stands between two items counts.  So the next item's queries
-// and keys are loaded, and its first products and softmax run, while warpgroup 3 still reads the
-// last one's accumulators.
+// One CTA per SM, 384 threads, in the roles of the step core's attention: warp 0 brings query
+// tiles and K/V tiles of 128 keys by TMA, warps 1 and 2 issue the products of query tile A and B
+// (S = Q K^T, O += P V, P over S in tensor memory), warpgroups 1 and 2 hold the running maximum and
+// sum of their tile's rows in registers, fp32, and rescale O only when a row's maximum grows by more
+// than 2^8.  Encoder states are few: an item (a pair of query tiles over one frame's keys) is often
+// only four K/V tiles long, so the next item's queries and keys are loaded, and its first product
+// issued, while the softmax warps still write the last one's rows.
 //
 // What masked keys hold must not matter, and 0 * NaN is NaN in a product: their scores are
 // replaced by -inf before anything is computed with them, and warp 3 sets their rows of V to zero
@@ -42,10 +41,10 @@ namespace rf {
 namespace {
 
 constexpr int kBM = 128, kBN = 128;  // rows of a query tile, keys of a K/V tile
-constexpr int kThreads = 512;        // four warpgroups: control, softmax A and B, results
-// Registers after setmaxnreg: 256 * 56 + 256 * 200 = 65536 = 512 * 128, what the launch holds.
-constexpr int kRegsLaunch = 128, kRegsOther = 56, kRegsSoftmax = 200;
-static_assert(256 * kRegsOther + 256 * kRegsSoftmax <= kThreads * kRegsLaunch, "register split");
+constexpr int kThreads = 384;        // three warpgroups
+// Registers after setmaxnreg: 128 * 104 + 256 * 200 = 64512 = 384 * 168, what the launch holds.
+constexpr int kRegsLaunch = 168, kRegsControl = 104, kRegsSoftmax = 200;
+static_assert(128 * kRegsControl + 256 * kRegsSoftmax <= kThreads * kRegsLaunch, "register split");
 constexpr uint32_t kTmemCols = 512;  // S_A, S_B at 0, 128; O_A, O_B at 256, 384
 constexpr uint64_t kDrainLimitNs = 200000000ull;  // 0.2 s for what is in flight at teardown
 constexpr float kRescaleLog2 = 8.0f;
@@ -56,9 +55,6 @@ constexpr int kPThreads = 128 + 32;
 __device__ __forceinline__ int p_barrier(int X, int part) { return 1 + 2 * X + part; }
 __device__ __forceinline__ int turn_barrier(int X) { return 5 + X; }
 
-// Boxes of a query tile, 8 or 32 rows each.
-using QueryList = BoxList<32>;
-
 template <int D>
 struct Cfg {
   static constexpr int kHalves = D / 64;           // 128-byte swizzle atoms across the head dim
@@ -66,19 +62,17 @@ struct Cfg {
   static constexpr int kHalfBytes = 128 * 128;
   static constexpr int kSlots = D == 128 ? 4 : 8;  // K in even slots, V in odd ones
   static constexpr int kOffKV = 2 * kTileBytes;
-  static constexpr int kOffStage = kOffKV + kSlots * kTileBytes;  // a tile of results
-  static constexpr int kStageWarp = kHalves * kTurnBytes;         // 32 rows of it
-  static constexpr int kOffStats = kOffStage + 4 * kStageWarp;    // {maximum, sum} [tile][128]
-  static constexpr int kOffBar = kOffStats + 2 * 128 * 8;
+  static constexpr int kOffStage = kOffKV + kSlots * kTileBytes;  // rows of results, per softmax warp
+  static constexpr int kOffBar = kOffStage + 8 * kTurnBytes;
   static constexpr int kQFull = 0, kQEmpty = 2, kKVFull = 4, kKVEmpty = 4 + kSlots,
                        kVClean = 4 + 2 * kSlots, kSFull = 4 + 3 * kSlots, kODone = kSFull + 2,
-                       kStats = kODone + 2, kFree = kStats + 2, kDrain = kFree + 2,
-                       kBars = kDrain + 2;
+                       kDrain = kODone + 2, kBars = kDrain + 2;
   static constexpr int kOffMisc = kOffBar + kBars * 8;  // tensor memory address, abort, MMA done [2]
-  static constexpr int kOffWork = kOffMisc + 16;
-  static constexpr int kOffList = kOffWork + 64;        // boxes of the query tiles
-  static constexpr int kSmem = kOffList + 2 * static_cast<int>(sizeof(QueryList));
-  // A split item's rows lie over the K/V ring: [tile][D / 4][128] float4
+  static constexpr int kOffList = kOffMisc + 32;        // boxes of the query tiles
+  static constexpr int kSmem =                          // + slack to align the base
+      kOffList + 2 * static_cast<int>(sizeof(BoxList<kBM>)) + 1024;
+  // A split item's rows: [tile][D / 4][128] float4 over the K/V ring, {max, sum} [tile][128] over
+  // the queries
   static_assert(2 * 128 * D * 4 <= kSlots * kTileBytes, "partial rows fit the ring");
 };
 
@@ -113,7 +107,6 @@ struct Work {
   int first, step;  // this CTA's items
   FastDiv by_pairs, by_groups;
 };
-static_assert(sizeof(Work) <= 64, "work");
 __device__ __forceinline__ Work make_work(const CrossParams& p) {
   Work w;
   w.A = p.rows.frames();
@@ -221,7 +214,7 @@ struct Load {
 };
 template <int D>
 __device__ __forceinline__ void prepare_load(const QueryMaps& maps, const CrossParams& p,
-                                             const Work& w, int i, int rank, QueryList* list, bool lead,
+                                             const Work& w, int i, int rank, BoxList<kBM>* list, bool lead,
                                              Load& n) {
   n.t = get_item(p, w, i, rank);
   if (p.packed || n.t.j0 >= n.t.j1) return;
@@ -229,7 +222,6 @@ __device__ __forceinline__ void prepare_load(const QueryMaps& maps, const CrossP
   for (int X = 0; X < 2; ++X) {
     const int tile = 2 * n.t.pair + X;
     if (tile >= w.tiles) break;
-    if (p.rows.unit == 1 && !p.kv_range) break;  // rows one by one: no list
     const RowBoxes x =
         p.kv_range ? RowBoxes{kBM, 0, 0, p.rows.frame(n.t.group) * p.rows.N + tile * kBM}
                    : list_boxes(p.rows, w.A * p.rows.Np, tile * kBM, kBM, list[X]);
@@ -245,7 +237,7 @@ __device__ __forceinline__ void prepare_load(const QueryMaps& maps, const CrossP
 template <int D>
 __device__ __forceinline__ void load_queries(const QueryMaps& maps, const CrossParams& p,
                                              const Work& w, const Item& t, int tile,
-                                             const RowBoxes& x, const QueryList& list, uint32_t dst,
+                                             const RowBoxes& x, const BoxList<kBM>& list, uint32_t dst,
                                              uint32_t bar) {
   using C = Cfg<D>;
   auto load = [&](const CUtensorMap* m, int row, int head, int tok) {
@@ -263,17 +255,6 @@ __device__ __forceinline__ void load_queries(const QueryMaps& maps, const CrossP
       load(maps.unit, i * p.frame_rows, t.unit * p.g, p.rows.frame(a0 + i) * p.rows.N);
     return;
   }
-  if (p.rows.unit == 1 && !p.kv_range) {
-    // frames of fewer than 8 tokens: not padded, so rows are loaded one by one
-    const int r0 = tile * kBM, n = min(kBM, w.A * p.rows.Np - r0);
-    mbar_arrive_expect_tx(bar, n * 128 * C::kHalves);
-#pragma unroll 1
-    for (int i = 0; i < n; ++i) {
-      const int a = p.rows.by_Np.div(r0 + i);
-      load(maps.unit, i, t.unit, p.rows.frame(a) * p.rows.N + (r0 + i - a * p.rows.Np));
-    }
-    return;
-  }
   mbar_arrive_expect_tx(bar, x.rows * 128 * C::kHalves);
   if (x.n_many + x.n_unit == 0) {
     load(maps.whole, 0, t.unit, x.tok);
@@ -282,13 +263,13 @@ __device__ __forceinline__ void load_queries(const QueryMaps& maps, const CrossP
 #pragma unroll 1
   for (int i = 0; i < x.n_many; ++i) load(maps.many, list.row[i], t.unit, list.tok[i]);
 #pragma unroll 1
-  for (int i = 32 - x.n_unit; i < 32; ++i) load(maps.unit, list.row[i], t.unit, list.tok[i]);
+  for (int i = kBM - x.n_unit; i < kBM; ++i) load(maps.unit, list.row[i], t.unit, list.tok[i]);
 }
 
 template <int D>
 __device__ __forceinline__ void producer(const QueryMaps& maps, const CUtensorMap* tmK,
                                          const CUtensorMap* tmV, const CrossParams& p,
-                                         const Work& w, int rank, QueryList* list, uint32_t sQ0,
+                                         const Work& w, int rank, BoxList<kBM>* list, uint32_t sQ0,
                                          uint32_t sKV0, uint32_t bar0, volatile int* abort) {
   using C = Cfg<D>;
   auto bar = [&](int i) { return bar0 + 8u * i; };
@@ -416,20 +397,14 @@ __device__ __forceinline__ bool mma_issuer(const CrossParams& p, const Work& w, 
   const uint32_t tS = tmem + X * 128, tO = tmem + 256 + X * 128;
   const uint64_t dQ = smem_desc_sw128(sQ0 + X * C::kTileBytes, 16, 1024);
   int q_cnt = 0, it = 0;    // it: ring index of the item's first tile of keys
-  int items = 0;
   bool my_turn = X == 0;    // the first turn is tile A's
   bool ok = true;
 #pragma unroll 1
   for (int i = w.first; ok && i < w.items; i += w.step) {
     const Item t = get_item(p, w, i, rank);
     const int nt = t.j1 - t.j0;
+    if (nt <= 0) continue;
     const bool both = 2 * t.pair + 1 < w.tiles, mine = X == 0 || both;
-    const int n_item = items;  // items of this tile before this one
-    items += mine;
-    if (nt <= 0) {
-      if (mine) ok = all_wait(bar(C::kFree + X), (n_item & 1) ^ 1, abort);
-      continue;
-    }
     if (mine) {
       ok = all_wait(bar(C::kQFull + X), q_cnt & 1, abort);
       ++q_cnt;
@@ -444,8 +419,6 @@ __device__ __forceinline__ bool mma_issuer(const CrossParams& p, const Work& w, 
       if (!first)
         ok = all_wait(bar((CLEAN ? C::kVClean : C::kKVFull) + sV), (iV / C::kSlots) & 1, abort);
       if (ok && more) ok = all_wait(bar(C::kKVFull + sK), (iK / C::kSlots) & 1, abort);
-      // the accumulator of the item before has been read
-      if (ok && mine && j == 0) ok = all_wait(bar(C::kFree + X), (n_item & 1) ^ 1, abort);
       ok = __all_sync(0xffffffffu, ok && *abort == 0);
       if (!ok) break;
       if (!mine) {  // no such query tile: only give the slots back
@@ -608,7 +581,7 @@ __device__ __forceinline__ bool softmax_item(const CrossParams& p, const Item& t
 }
 
 template <int D, bool F16, bool CLEAN>
-__device__ __forceinline__ bool softmax_group(const CrossParams& p, const Work& w, int rank, int X,
+__device__ __forceinline__ bool softmax_group(const CUtensorMap* tmO, const CrossParams& p, const Work& w, int rank, int X,
                                               uint32_t tmem, uint8_t* smem, uint32_t bar0,
                                               volatile int* abort) {
   using C = Cfg<D>;
@@ -617,137 +590,99 @@ __device__ __forceinline__ bool softmax_group(const CrossParams& p, const Work& 
   const int row = (warp & 3) * 32 + lane;  // and lane of tensor memory
   const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
   const uint32_t tS = tmem + lane_base + X * 128, tO = tmem + lane_base + 256 + X * 128;
-  int s_cnt = 0, items = 0;
+  uint4* stage = reinterpret_cast<uint4*>(smem + C::kOffStage + (warp - 4) * kTurnBytes);
+  int64_t at = -1;  // byte offset of this thread's row in O
+  int s_cnt = 0, o_cnt = 0;
+  Item next;
+  if (w.first < w.items) next = get_item(p, w, w.first, rank);
 #pragma unroll 1
-  for (int i = w.first; i < w.items; i += w.step) {
-    const Item t = get_item(p, w, i, rank);
-    if (2 * t.pair + X >= w.tiles) continue;
+  for (int i = w.first; i < w.items;) {
+    const Item t = next;
+    i += w.step;
+    const int tile = 2 * t.pair + X;
+    if (tile >= w.tiles) {
+      if (i < w.items) next = get_item(p, w, i, rank);
+      continue;
+    }
     float m = -INFINITY, l = 0.f;
     bool ok = t.j0 >= t.j1 ||
               softmax_item<D, F16, CLEAN>(p, t, X, tS, tO, bar(C::kSFull + X), s_cnt, m, l, abort);
-    if (p.cluster == 1) {
-      // to warpgroup 3, which has taken the item before
-      ok = ok && all_wait(bar(C::kFree + X), (items & 1) ^ 1, abort);
-      if (!ok) {
-        if (lane == 0) flag_error(p, 3);
-        return false;
-      }
-      ++items;
-      reinterpret_cast<float2*>(smem + C::kOffStats)[X * 128 + row] = make_float2(m, l);
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar(C::kStats + X));
-      continue;
+    // found while the last P V runs: behind it every cycle counts
+    if (i < w.items) next = get_item(p, w, i, rank);
+    const int first = whole_tile(p, w, t, tile);
+    // no key: zeros, not 0 * accumulator, which may hold anything
+    const bool none = l == 0.f;
+    const float inv_l = none ? 0.f : 1.0f / l;
+    if (t.j0 < t.j1) {
+      ok = ok && all_wait(bar(C::kODone + X), o_cnt & 1, abort);
+      ++o_cnt;
+      tc_fence_after();
     }
-    // A cluster CTA's share, its only one.  The ring holds the keys until both tiles are done.
-    if (t.j0 < t.j1)
-      for (int Y = 0; ok && Y < 2; ++Y)
-        if (2 * t.pair + Y < w.tiles) ok = all_wait(bar(C::kODone + Y), 0, abort);
     if (!ok) {
-      if (lane == 0) flag_error(p, 4);
+      if (lane == 0) flag_error(p, 3);
       return false;
     }
-    tc_fence_after();
-    float4* part = reinterpret_cast<float4*>(smem + C::kOffKV) + X * (D / 4 * 128) + row;
-    if (t.j0 < t.j1)
-#pragma unroll 1
-      for (int c = 0; c < D / 32; ++c) {
-        uint32_t o[32];
-        tmem_ld32(tO + c * 32, o);
-        tmem_wait_ld();
-#pragma unroll
-        for (int q = 0; q < 8; ++q)
-          part[(c * 8 + q) * 128] =
-              make_float4(__uint_as_float(o[4 * q]), __uint_as_float(o[4 * q + 1]),
-                          __uint_as_float(o[4 * q + 2]), __uint_as_float(o[4 * q + 3]));
+    if (p.cluster > 1) {
+      // the ring holds the other tile's keys until that one is done too
+      const bool other = t.j0 < t.j1 && 2 * t.pair + 1 < w.tiles;
+      if (other && !all_wait(bar(C::kODone + (X ^ 1)), 0, abort)) {
+        if (lane == 0) flag_error(p, 4);
+        return false;
       }
-    reinterpret_cast<float2*>(smem + C::kOffStats)[X * 128 + row] = make_float2(m, l);
-    return true;  // joined after the cluster's barrier
-  }
-  return true;
-}
-
-// Rows of results from the accumulators and statistics of whole items (warpgroup 3).
-template <int D, bool F16>
-__device__ __forceinline__ void write_results(const CUtensorMap* tmO, const CrossParams& p,
-                                              const Work& w, uint32_t tmem, uint8_t* smem,
-                                              uint32_t bar0, volatile int* abort) {
-  using C = Cfg<D>;
-  auto bar = [&](int i) { return bar0 + 8u * i; };
-  const int quarter = (threadIdx.x >> 5) & 3, lane = threadIdx.x & 31;
-  const int row = quarter * 32 + lane;
-  const uint32_t lane_base = static_cast<uint32_t>(quarter * 32) << 16;
-  uint4* stage = reinterpret_cast<uint4*>(smem + C::kOffStage + quarter * C::kStageWarp);
-  const int64_t stride = p.o_row_stride * 2;
-  int items0 = 0, items1 = 0, done0 = 0, done1 = 0;  // of tile A and B; done: those with keys
-  bool ok = true;
+      float4* part = reinterpret_cast<float4*>(smem + C::kOffKV) + X * (D / 4 * 128) + row;
+      if (t.j0 < t.j1)
 #pragma unroll 1
-  for (int i = w.first; ok && i < w.items; i += w.step) {
-    const Item t = get_item(p, w, i, 0);
-    const bool keys = t.j0 < t.j1;
-#pragma unroll 1
-    for (int X = 0; X < 2; ++X) {
-      const int tile = 2 * t.pair + X;
-      if (tile >= w.tiles) break;
-      const int first = whole_tile(p, w, t, tile);
-      int64_t token = -1;
-      int head = 0;
-      if (first < 0 || p.lse) token = row_of(p, w, t, tile, row, head);
-      if (lane == 0) bulk_wait_read();  // the tile before has left the stage
-      ok = all_wait(bar(C::kStats + X), (X ? items1 : items0) & 1, abort);
-      (X ? items1 : items0) += 1;
-      if (ok && keys) ok = all_wait(bar(C::kODone + X), (X ? done1 : done0) & 1, abort);
-      (X ? done1 : done0) += keys;
-      if (!ok) {
-        if (lane == 0) flag_error(p, 5);
-        break;
-      }
-      tc_fence_after();
-      const float2 ml = reinterpret_cast<const float2*>(smem + C::kOffStats)[X * 128 + row];
-      // no key: zeros, not 0 * accumulator, which may hold anything
-      const bool none = ml.y == 0.f;
-      const float inv_l = none ? 0.f : 1.0f / ml.y;
-#pragma unroll 1
-      for (int c = 0; c < D / 32; ++c) {
-        uint32_t o[32];
-        tmem_ld32(tmem + lane_base + 256 + X * 128 + c * 32, o);
-        tmem_wait_ld();
-        uint4* half = stage + (c >> 1) * (kTurnBytes / 16);
+        for (int c = 0; c < D / 32; ++c) {
+          uint32_t o[32];
+          tmem_ld32(tO + c * 32, o);
+          tmem_wait_ld();
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-          stage_at(half, lane, (c & 1) * 4 + q) =
-              none ? make_uint4(0u, 0u, 0u, 0u)
-                   : pack8<F16>(reinterpret_cast<const float*>(o) + q * 8, inv_l);
-      }
-      // accumulator and statistics may be written again
-      tc_fence_before();
-      fence_proxy_async();
-      __syncwarp();
-      if (lane == 0) {
-        mbar_arrive(bar(C::kFree + X));
-        if (first >= 0) {
-#pragma unroll
-          for (int hb = 0; hb < C::kHalves; ++hb)
-            tma_store_3d(tmO, smem_u32(stage) + hb * kTurnBytes, hb * 64, t.unit,
-                         first + quarter * 32);
-          bulk_commit();
+          for (int q = 0; q < 8; ++q)
+            part[(c * 8 + q) * 128] =
+                make_float4(__uint_as_float(o[4 * q]), __uint_as_float(o[4 * q + 1]),
+                            __uint_as_float(o[4 * q + 2]), __uint_as_float(o[4 * q + 3]));
         }
-      }
-      __syncwarp();
-      if (first < 0) {
-        const RowSpan span =
-            row_span(token >= 0 ? token * stride + static_cast<int64_t>(head) * D * 2 : -1, stride);
-#pragma unroll 1
-        for (int hb = 0; hb < C::kHalves; ++hb)
-          store_rows(stage + hb * (kTurnBytes / 16), reinterpret_cast<char*>(p.O) + hb * 128, span,
-                     stride);
-      }
+      reinterpret_cast<float2*>(smem)[X * 128 + row] = make_float2(m, l);
+      return true;  // one item per CTA; joined after the cluster's barrier
+    }
+    if (first < 0 || p.lse) {
+      int head;
+      const int64_t token = row_of(p, w, t, tile, row, head);
+      at = token < 0 ? -1 : (token * p.o_row_stride + static_cast<int64_t>(head) * D) * 2;
       if (token >= 0 && p.lse)
         p.lse[static_cast<int64_t>(head) * p.rows.T + token] =
-            none ? -INFINITY : (ml.x + __log2f(ml.y)) * 0.69314718055994531f;
+            none ? -INFINITY : (m + __log2f(l)) * 0.69314718055994531f;
     }
+#pragma unroll 1
+    for (int c = 0; c < D / 64; ++c) {
+      uint32_t o[64];
+      tmem_ld32(tO + c * 64, reinterpret_cast<uint32_t(&)[32]>(o[0]));
+      tmem_ld32(tO + c * 64 + 32, reinterpret_cast<uint32_t(&)[32]>(o[32]));
+      tmem_wait_ld();
+      if (lane == 0) bulk_wait_read();  // the stage's last tile has been read
+      __syncwarp();
+#pragma unroll
+      for (int q = 0; q < 8; ++q)
+        stage_at(stage, lane, q) = none ? make_uint4(0u, 0u, 0u, 0u)
+                                        : pack8<F16>(reinterpret_cast<const float*>(o) + q * 8, inv_l);
+      if (first >= 0) {
+        // 32 consecutive tokens: in the background
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) {
+          tma_store_3d(tmO, smem_u32(stage), c * 64, t.unit, first + (warp & 3) * 32);
+          bulk_commit();
+        }
+      } else {
+        store_rows(stage, reinterpret_cast<char*>(p.O) + c * 128, row_span(at, p.o_row_stride * 2),
+                   p.o_row_stride * 2);
+      }
+    }
+    // (the accumulator is read before the next item's first P, so before its first P V)
   }
   if (lane == 0) bulk_wait_all();
   __syncwarp();
+  return true;
 }
 
 // A split item's rows from all CTAs of the cluster: O = sum_c 2^(m_c - M) O_c / sum_c 2^(m_c - M) l_c.
@@ -772,7 +707,7 @@ __device__ __forceinline__ void join(const CrossParams& p, const Work& w, int ra
     ms[c] = -INFINITY;
     ls[c] = 0.f;
     if (c < p.cluster) {
-      const uint32_t at = map_to_rank(sbase + C::kOffStats + (X * 128 + row) * 8, c);
+      const uint32_t at = map_to_rank(sbase + (X * 128 + row) * 8, c);
       ms[c] = ld_cluster_f(at);
       ls[c] = ld_cluster_f(at + 4);
     }
@@ -830,9 +765,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                  const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmO,
                  const CrossParams p) {
   using C = Cfg<D>;
-  // (the swizzle goes by address: tiles start on 1024-byte boundaries)
-  extern __shared__ __align__(1024) uint8_t smem[];
-  const uint32_t sbase = smem_u32(smem);
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw);
+  const uint32_t sbase = (raw + 1023u) & ~1023u;
+  uint8_t* smem = smem_raw + (sbase - raw);
   const uint32_t sQ0 = sbase, sKV0 = sbase + C::kOffKV, bar0 = sbase + C::kOffBar;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::kOffMisc);
   volatile int* abort = reinterpret_cast<volatile int*>(smem + C::kOffMisc + 4);
@@ -840,16 +776,14 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int warp = threadIdx.x >> 5;
   const int rank = p.cluster > 1 ? static_cast<int>(cluster_rank()) : 0;
 
-  Work& w = *reinterpret_cast<Work*>(smem + C::kOffWork);
-  if (threadIdx.x == 64) w = make_work(p);
+  __shared__ Work work;
+  if (threadIdx.x == 64) work = make_work(p);
   if (threadIdx.x == 0) {
     for (int X = 0; X < 2; ++X) {
       mbar_init(bar0 + 8 * (C::kQFull + X), 1);
       mbar_init(bar0 + 8 * (C::kQEmpty + X), 1);
       mbar_init(bar0 + 8 * (C::kSFull + X), 1);
       mbar_init(bar0 + 8 * (C::kODone + X), 1);
-      mbar_init(bar0 + 8 * (C::kStats + X), 4);
-      mbar_init(bar0 + 8 * (C::kFree + X), 4);
       mbar_init(bar0 + 8 * (C::kDrain + X), 1);
       mma_done[X] = 0;
     }
@@ -872,16 +806,15 @@ __global__ void __launch_bounds__(kThreads, 1)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
+  const Work& w = work;
 
-  // Warpgroups 0 and 3 give registers back unconditionally, so the increase below always finds them.
-  if (warp >= 12) {
-    reg_dealloc<kRegsOther>();
-    if (p.cluster == 1) write_results<D, F16>(&tmO, p, w, tmem, smem, bar0, abort);
-  } else if (warp < 4) {
-    reg_dealloc<kRegsOther>();
+  // Every warp of warpgroup 0 gives registers back before any softmax warp asks for more, so the
+  // increase below always finds them.
+  if (warp < 4) {
+    reg_dealloc<kRegsControl>();
     if (warp == 0) {
       producer<D>({&tmQ, &tmMany, &tmUnit}, &tmK, &tmV, p, w, rank,
-                  reinterpret_cast<QueryList*>(smem + C::kOffList), sQ0, sKV0, bar0, abort);
+                  reinterpret_cast<BoxList<kBM>*>(smem + C::kOffList), sQ0, sKV0, bar0, abort);
     } else if (warp < 3) {
       const int X = warp - 1;
       const bool ok =
@@ -899,14 +832,14 @@ __global__ void __launch_bounds__(kThreads, 1)
   } else {
     reg_alloc<kRegsSoftmax>();
     const int X = (warp - 4) >> 2;
-    if (!softmax_group<D, F16, CLEAN>(p, w, rank, X, tmem, smem, bar0, abort))
+    if (!softmax_group<D, F16, CLEAN>(&tmO, p, w, rank, X, tmem, smem, bar0, abort))
       release_mma(mma_done + X, p_barrier(X, 0), p_barrier(X, 1), kPThreads);
   }
   __syncwarp();
   if (p.cluster > 1) {
     cluster_arrive();
     cluster_wait();
-    if (warp >= 4 && warp < 12) join<D, F16>(p, w, rank, (warp - 4) >> 2, sbase);
+    if (warp >= 4) join<D, F16>(p, w, rank, (warp - 4) >> 2, sbase);
     __syncwarp();
     cluster_arrive();  // every CTA has read the others' rows
     cluster_wait();

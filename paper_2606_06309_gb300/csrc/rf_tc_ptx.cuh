@@ -56,25 +56,29 @@ __device__ __forceinline__ bool mbar_try_wait_cluster(uint32_t bar, uint32_t par
       : "memory");
   return ok != 0;
 }
-// A warp's wait for the phase of parity `parity` of `bar`, on which threads of this CTA, of others of
-// the cluster, or asynchronous operations arrive; the result is the same in every lane.  Gives up, and
-// raises *abort, after kWaitPolls polls, or when another thread of the CTA has raised it.  A poll may
-// suspend the thread for some time; the fastest takes about 20 cycles, so that the limit is between
-// 0.4 s and some seconds, where no legitimate wait comes near a millisecond per 100,000 columns of a
-// product.  No clock is read: the waits of a kernel are many, and its code has to fit the
-// instruction caches.
-constexpr uint32_t kWaitPolls = 40000000u;
-template <bool CLUSTER>  // whether other CTAs arrive on the barrier
+// A warp's wait for the phase of parity `parity` of `bar`; the result is the same in every lane.
+// CLUSTER: threads of other CTAs arrive on the barrier.  Gives up, and raises *abort, after
+// kWaitLimitNs, or when another thread of the CTA has raised it.  A poll may suspend the thread for
+// some time, so the clock is read from the 257th on; kWaitPolls bounds the loop even if it stood.
+constexpr uint32_t kWaitLimitNs = 2000000000u;  // 2 s: no legitimate wait comes close
+constexpr uint32_t kWaitPolls = 200000000u;
+template <bool CLUSTER>
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort) {
-  bool ok = true;
+  auto poll = [&]() {
+    return CLUSTER ? mbar_try_wait_cluster(bar, parity) : mbar_try_wait(bar, parity);
+  };
+  bool ok = poll();
 #pragma unroll 1
-  for (uint32_t n = 0;
-       !(CLUSTER ? mbar_try_wait_cluster(bar, parity) : mbar_try_wait(bar, parity));)
-    if (++n >= kWaitPolls || ((n & 63) == 0 && *abort)) {
-      *abort = 1;
-      ok = false;
-      break;
-    }
+  for (int n = 0; !ok && n < 256; ++n) ok = poll();
+  if (!ok) {
+    const uint32_t t0 = globaltimer_lo_ns();
+#pragma unroll 1
+    for (uint32_t n = 0; !(ok = poll());)
+      if (*abort || globaltimer_lo_ns() - t0 > kWaitLimitNs || ++n >= kWaitPolls) {
+        *abort = 1;
+        break;
+      }
+  }
   return __all_sync(0xffffffffu, ok);
 }
 // Wait, with a limit, with no regard to the abort flag (teardown only).
@@ -174,6 +178,29 @@ __device__ __forceinline__ void tc_mma_ss_pair(uint32_t d_tmem, uint64_t a_desc,
       "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
       "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
       : "memory");
+}
+
+// 32 lanes x 16 consecutive 32-bit columns, and the wait for them, which the values pass through: what
+// is computed with them cannot be moved in front of it.
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+        "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
+        "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_wait_ld16(uint32_t (&r)[16]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]),
+                 "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]),
+                 "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])::"memory");
+}
+__device__ __forceinline__ uint64_t fmul2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
 }
 
 // Instruction descriptor of kind::f16 with an fp32 accumulator; A and B both bf16 or both fp16.

@@ -33,6 +33,7 @@ SHAPES = [
     (3, 9, (0, 2), 40, 1, 64, 64),             # forty heads on a key head, frames off 8 rows
     (2, 6, (0, 1), 32, 1, 64, 200),            # rows gathered one by one
     (2, 17, (1,), 2, 2, 128, 4000),            # long states, few rows: dealt to a cluster
+    (3, 100, (0, 1, 2), 160, 160, 64, 200),    # several items per SM, every second without a tile B
     (3, 16, (), 2, 2, 64, 64),                 # nothing active
 ]
 
