@@ -97,17 +97,6 @@ __device__ __forceinline__ void add2(uint32_t w, int dtype, float& lo, float& hi
   hi += b;
 }
 
-// One element of the result from its sum.
-__device__ __forceinline__ void finish_one(const Epilogue& e, int64_t token, int frame, int n,
-                                           float sum) {
-  float v[1] = {sum};
-  if (e.bias) v[0] += load_elem(e.bias, n, e.in_dtype);
-  activate(e.act, v);
-  if (e.gate) v[0] *= e.gate[frame * e.gate_stride + n];
-  if (e.R) v[0] += load_elem(e.R, token * e.r_stride + n, e.out_dtype);
-  store_elem(e.Y, token * e.y_stride + n, e.out_dtype, v[0]);
-}
-
 // Columns n .. n + 31 of a row, element by element: the last columns of a result, and rows off the
 // 16-byte boundaries.
 static __device__ __noinline__ void finish_row(const Epilogue& e, int64_t token, int frame, int n,
@@ -157,7 +146,7 @@ __device__ __forceinline__ void finish_cols(const Epilogue& e, int frame, int n,
 // warp's stage.  ready() is called when the residual's first loads are in flight and the
 // accumulator is wanted, read() when it has been read; false from ready() ends it.
 template <bool OUT32, typename Ready, typename Read>
-__device__ __forceinline__ bool finish_tile(const Epilogue& e, uint4* stage, uint32_t acc, int n0,
+__device__ __forceinline__ bool finish_tile(const Epilogue& e, const CUtensorMap* tmY, uint4* stage, uint32_t acc, int n0,
                                             int cols, int64_t token, int frame, Ready&& ready,
                                             Read&& read) {
   constexpr int kCols = OUT32 ? 32 : 64, kBytes = OUT32 ? 4 : 2;
@@ -169,7 +158,17 @@ __device__ __forceinline__ bool finish_tile(const Epilogue& e, uint4* stage, uin
   const char* R = static_cast<const char*>(e.R) + static_cast<int64_t>(n0) * kBytes;
   const int lane = threadIdx.x & 31;
   auto whole = [&](int c) { return e.vec && n0 + (c + 1) * kCols <= e.n_out; };
-  if (e.R && chunks > 0 && whole(0)) fetch_rows(stage, R, span_r, r_bytes);
+  // 32 consecutive tokens leave through TMA, in the background
+  const bool bulk = span_y.regular && span_y.n == 32;
+  const int token0 = __shfl_sync(0xffffffffu, static_cast<int>(token), 0);
+  auto stage_free = [&]() {
+    if (lane == 0) bulk_wait_read();
+    __syncwarp();
+  };
+  if (e.R && chunks > 0 && whole(0)) {
+    stage_free();
+    fetch_rows(stage, R, span_r, r_bytes);
+  }
   if (!ready()) return false;
   if (chunks == 0) read();
 #pragma unroll 1
@@ -195,7 +194,10 @@ __device__ __forceinline__ bool finish_tile(const Epilogue& e, uint4* stage, uin
       tmem_wait_ld();
       if (half == kCols / 32 - 1 && c == chunks - 1) read();
       finish_cols(e, frame, n + half * 32, v);
-      if (e.R && half == 0) await_rows();
+      if (half == 0) {
+        if (e.R) await_rows();
+        else stage_free();
+      }
 #pragma unroll
       for (int q = 0; q < (OUT32 ? 8 : 4); ++q) {
         // the residual's piece of this lane's row makes way for the result's
@@ -228,9 +230,20 @@ __device__ __forceinline__ bool finish_tile(const Epilogue& e, uint4* stage, uin
         }
       }
     }
-    store_rows(stage, Y + c * 128, span_y, y_bytes);
-    if (e.R && c + 1 < chunks && whole(c + 1)) 
+    if (bulk) {
+      fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) {
+        tma_store_2d(tmY, smem_u32(stage), n, token0);
+        bulk_commit();
+      }
+    } else {
+      store_rows(stage, Y + c * 128, span_y, y_bytes);
+    }
+    if (e.R && c + 1 < chunks && whole(c + 1)) {
+      stage_free();
       fetch_rows(stage, R + (c + 1) * 128, span_r, r_bytes);
+    }
   }
   return true;
 }
@@ -262,22 +275,25 @@ __device__ __forceinline__ int row_token(const LinearParams& p, int r, int& fram
 struct RowMaps {
   const CUtensorMap *whole, *many, *unit;
 };
-// Issue the copies of one k block of a tile of n rows (the bytes are announced before; one thread).
+// Issue the copies of one k block of a tile's rows (the bytes are announced before; one thread).
+// Boxes are dealt to `of` threads; a whole tile's is the last one's.
 template <bool PAIR, int CAP>
 __device__ __forceinline__ void load_rows(const RowBoxes& x, const BoxList<CAP>& list,
-                                          const RowMaps& maps, uint32_t dst, uint32_t bar, int k0) {
+                                          const RowMaps& maps, uint32_t dst, uint32_t bar, int k0,
+                                          int who, int of) {
   auto load = [&](const CUtensorMap* m, int row, int tok) {
     if (PAIR) tma_load_2d_pair(dst + row * 128, m, bar, k0, tok);
     else tma_load_2d(dst + row * 128, m, bar, k0, tok);
   };
   if (x.n_many + x.n_unit == 0) {
-    load(maps.whole, 0, x.tok);
+    if (who == of - 1) load(maps.whole, 0, x.tok);
     return;
   }
 #pragma unroll 1
-  for (int i = 0; i < x.n_many; ++i) load(maps.many, list.row[i], list.tok[i]);
+  for (int i = who; i < x.n_many; i += of) load(maps.many, list.row[i], list.tok[i]);
 #pragma unroll 1
-  for (int i = CAP - x.n_unit; i < CAP; ++i) load(maps.unit, list.row[i], list.tok[i]);
+  for (int i = CAP - 1 - who; i >= CAP - x.n_unit; i -= of)
+    load(maps.unit, list.row[i], list.tok[i]);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -288,7 +304,7 @@ __device__ __forceinline__ void load_rows(const RowBoxes& x, const BoxList<CAP>&
 // That is what the pair is for: a CTA alone on 128 x 256 would have to bring 48 KB into shared
 // memory per 64 columns of K, in a pair it brings 32 KB.
 // Two accumulators in tensor memory: the epilogue of a tile runs during the products of the next.
-constexpr int kPairThreads = 384;  // warp 0 TMA, 1 MMA (first CTA), 2 tensor memory, 4-11 epilogue
+constexpr int kPairThreads = 384;  // warps 0, 3 TMA, 1 MMA (first CTA), 2 tensor memory, 4-11 epilogue
 constexpr int kEpiWarps = 8;
 
 template <int BN>
@@ -298,12 +314,11 @@ struct PairCfg {
   static constexpr int kStages = 196608 / kStageBytes;
   static constexpr int kBarFull = 0, kBarEmpty = kStages, kBarAccFull = 2 * kStages,
                        kBarAccEmpty = kBarAccFull + 2, kBars = kBarAccEmpty + 2;
-  static constexpr int kOffBar = kStages * kStageBytes;
+  static constexpr int kOffStage = kStages * kStageBytes;  // rows of results, per epilogue warp
+  static constexpr int kOffBar = kOffStage + kEpiWarps * kTurnBytes;
   static constexpr int kOffMisc = kOffBar + kBars * 8;
   static constexpr int kOffList = kOffMisc + 16;
-  static constexpr int kOffStage =
-      (kOffList + static_cast<int>(sizeof(BoxList<128>)) + 15) / 16 * 16;
-  static constexpr int kSmem = kOffStage + kEpiWarps * kTurnBytes + 1024;
+  static constexpr int kSmem = kOffList + 2 * static_cast<int>(sizeof(BoxList<128>)) + 1024;
   static constexpr uint32_t kTmemCols = 2 * BN;
 };
 
@@ -322,7 +337,7 @@ template <int BN>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
     pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmMany,
                 const __grid_constant__ CUtensorMap tmUnit, const __grid_constant__ CUtensorMap tmW,
-                const LinearParams p) {
+                const __grid_constant__ CUtensorMap tmY, const LinearParams p) {
   using C = PairCfg<BN>;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
@@ -365,9 +380,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
   const int tiles = m_tiles * p.n_tiles;
   const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
 
-  if (warp == 0) {
+  if (warp == 0 || warp == 3) {
+    // two warps: the boxes of a tile across frames are seven or more for each 64 columns of K, and
+    // one warp does not issue them in the 512 cycles that the products take
     const bool lead = elect_one();
-    BoxList<128>& list = *reinterpret_cast<BoxList<128>*>(smem + C::kOffList);
+    const int who = warp == 3;
+    BoxList<128>& list = reinterpret_cast<BoxList<128>*>(smem + C::kOffList)[who];
     int it = 0;
     bool ok = true;
     for (int t = pair; ok && t < tiles; t += pairs) {
@@ -389,15 +407,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
         const uint32_t full = map_to_rank(bar(C::kBarFull + s), 0);
         const uint32_t dst = sbase + s * C::kStageBytes;
         if (lead) {
-          if (rank == 0) mbar_arrive_expect_tx(bar(C::kBarFull + s), bytes);
-          tma_load_2d_pair(dst + C::kABytes, &tmW, full, kb * kBlockK, w0);
-          load_rows<true>(x, list, {&tmX, &tmMany, &tmUnit}, dst, full, kb * kBlockK);
+          if (who == 0) {
+            if (rank == 0) mbar_arrive_expect_tx(bar(C::kBarFull + s), bytes);
+            tma_load_2d_pair(dst + C::kABytes, &tmW, full, kb * kBlockK, w0);
+          }
+          load_rows<true>(x, list, {&tmX, &tmMany, &tmUnit}, dst, full, kb * kBlockK, who, 2);
         }
         __syncwarp();
       }
     }
     // every stage that was filled has been given back (so no arrival from the other CTA is still
     // to come) before this CTA may leave; after a wait that gave up, the copies in flight get time
+#pragma unroll 1
     for (int s = 0; s < C::kStages; ++s)
       if (it > s)
         mbar_drain(bar(C::kBarEmpty + s), ((it - 1 - s) / C::kStages) & 1, kDrainLimitNs);
@@ -464,10 +485,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
       const uint32_t acc = tmem + lane_base + b * BN + part * (BN / 2);
       const int n0 = n * BN + part * (BN / 2);
       if (!(p.epi.out_dtype == RF_FP32
-                ? finish_tile<true>(p.epi, stage, acc, n0, BN / 2, token, frame, ready, read)
-                : finish_tile<false>(p.epi, stage, acc, n0, BN / 2, token, frame, ready, read)))
+                ? finish_tile<true>(p.epi, &tmY, stage, acc, n0, BN / 2, token, frame, ready, read)
+                : finish_tile<false>(p.epi, &tmY, stage, acc, n0, BN / 2, token, frame, ready, read)))
         break;
     }
+    if (lane == 0) bulk_wait_all();
   }
   __syncwarp();
   tc_fence_before();
@@ -493,7 +515,7 @@ constexpr int kSplitRing = 212992;  // bytes for stages; the sums of a split tak
 constexpr int kSplitBarFull = 0, kSplitBarEmpty = kSplitMaxStages,
               kSplitBarAcc = 2 * kSplitMaxStages, kSplitBars = kSplitBarAcc + 1;
 constexpr int kSplitOffBar = kSplitRing, kSplitOffMisc = kSplitOffBar + kSplitBars * 8,
-              kSplitOffList = kSplitOffMisc + 16,
+              kSplitOffTok = kSplitOffMisc + 16, kSplitOffList = kSplitOffTok + 256 * 8,
               kSplitSmem = kSplitOffList + sizeof(BoxList<256>) + 1024;
 
 __global__ void __launch_bounds__(kSplitThreads, 1)
@@ -556,7 +578,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1)
         mbar_arrive_expect_tx(bar(kSplitBarFull + s), 16384 + x.rows * 128);
         tma_load_2d(dst, &tmW, bar(kSplitBarFull + s), kb * kBlockK, n * 128);
         load_rows<false>(x, list, {&tmX, &tmMany, &tmUnit}, dst + 16384,
-                         bar(kSplitBarFull + s), kb * kBlockK);
+                         bar(kSplitBarFull + s), kb * kBlockK, 0, 1);
       }
       __syncwarp();
     }
@@ -589,9 +611,15 @@ __global__ void __launch_bounds__(kSplitThreads, 1)
     mbar_drain(bar(kSplitBarAcc), 0, kDrainLimitNs);
   }
   float* sums = reinterpret_cast<float*>(smem);  // [BT][128]
+  int2* tokens = reinterpret_cast<int2*>(smem + kSplitOffTok);  // {token, frame}
   if (warp >= 4) {
     const int quarter = warp & 3;
-    const int col = n * 128 + quarter * 32 + lane;
+#pragma unroll 1
+    for (int j = threadIdx.x - 128; j < BT; j += 128) {
+      int2 t = make_int2(-1, 0);
+      if (r0 + j < R) t.x = row_token(p, r0 + j, t.y);
+      tokens[j] = t;
+    }
     const bool ok = warp_wait<false>(bar(kSplitBarAcc), 0, abort);
     if (!ok && lane == 0) flag_error(p, 2);
     tc_fence_after();
@@ -600,47 +628,58 @@ __global__ void __launch_bounds__(kSplitThreads, 1)
       uint32_t v[32];
       tmem_ld32(tmem + (static_cast<uint32_t>(quarter * 32) << 16) + c, v);
       tmem_wait_ld();
-      if (C > 1) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i)
-          if (c + i < BT) sums[(c + i) * 128 + quarter * 32 + lane] = __uint_as_float(v[i]);
-      } else {
+      for (int i = 0; i < 32; ++i)
+        if (c + i < BT) sums[(c + i) * 128 + quarter * 32 + lane] = __uint_as_float(v[i]);
+    }
+    tc_fence_before();
+  }
+  __syncthreads();
+  if (C > 1) {
+    cluster_arrive();
+    cluster_wait();
+  }
+  // A thread has one column, and kTok of the tokens of its half of the threads and its CTA at a
+  // time, with the loads of all of them in flight.
+  constexpr int kTok = 4;
+  const int col = threadIdx.x & 127, out = n * 128 + col;
+  const Epilogue& e = p.epi;
+  if (out < e.n_out) {
+    const float bias = e.bias ? load_elem(e.bias, out, e.in_dtype) : 0.f;
+    const int step = 2 * C;  // between a thread's tokens
+#pragma unroll 1
+    for (int j0 = 2 * rank + (threadIdx.x >> 7); j0 < BT && r0 + j0 < R; j0 += kTok * step) {
+      float sum[kTok], gate[kTok], res[kTok];
+      int2 t[kTok];
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
-          const int r = r0 + c + i;
-          if (c + i >= BT || r >= R) break;
-          int frame;
-          const int token = row_token(p, r, frame);
-          if (token >= 0 && col < p.epi.n_out)
-            finish_one(p.epi, token, frame, col, __uint_as_float(v[i]));
-        }
+      for (int u = 0; u < kTok; ++u) {
+        const int j = j0 + u * step;
+        t[u] = j < BT ? tokens[j] : make_int2(-1, 0);
+        sum[u] = 0.f;
+        gate[u] = e.gate && t[u].x >= 0 ? e.gate[t[u].y * e.gate_stride + out] : 1.f;
+        res[u] = e.R && t[u].x >= 0 ? load_elem(e.R, t[u].x * e.r_stride + out, e.out_dtype) : 0.f;
+      }
+#pragma unroll 2
+      for (int c = 0; c < C; ++c) {
+        const uint32_t at = sbase + (j0 * 128 + col) * 4;
+        const uint32_t base = C > 1 ? map_to_rank(at, c) : at;
+#pragma unroll
+        for (int u = 0; u < kTok; ++u)
+          if (t[u].x >= 0) sum[u] += ld_cluster_f(base + u * step * 512);
+      }
+#pragma unroll
+      for (int u = 0; u < kTok; ++u) sum[u] += bias;
+      activate(e.act, sum);
+#pragma unroll
+      for (int u = 0; u < kTok; ++u) {
+        if (e.gate) sum[u] *= gate[u];
+        if (e.R) sum[u] += res[u];
+        if (t[u].x >= 0) store_elem(e.Y, t[u].x * e.y_stride + out, e.out_dtype, sum[u]);
       }
     }
   }
   __syncwarp();
   if (C > 1) {
-    cluster_arrive();
-    cluster_wait();
-    // two tokens at a time (half of the threads each), every C-th pair of them
-    const int col = threadIdx.x & 127;
-    if (n * 128 + col < p.epi.n_out) {
-      for (int j = 2 * rank + (threadIdx.x >> 7); j < BT; j += 2 * C) {
-        const int r = r0 + j;
-        if (r >= R) break;
-        int frame;
-        const int token = row_token(p, r, frame);
-        if (token < 0) continue;
-        const uint32_t at = sbase + (j * 128 + col) * 4;
-        float part[8];
-#pragma unroll
-        for (int c = 0; c < 8; ++c) part[c] = c < C ? ld_cluster_f(map_to_rank(at, c)) : 0.f;
-        float sum = part[0];
-#pragma unroll
-        for (int c = 1; c < 8; ++c) sum += part[c];
-        finish_one(p.epi, token, frame, n * 128 + col, sum);
-      }
-    }
-    __syncwarp();
     cluster_arrive();  // every CTA has read the others' sums
     cluster_wait();
   }
@@ -683,7 +722,7 @@ int split_ranges(int64_t tiles, int kblocks, int sms) {
 }
 
 struct Maps {
-  CUtensorMap x, many, unit, w;
+  CUtensorMap x, many, unit, w, y;
 };
 // The maps of a launch with tiles of `tile` rows of X; w_rows rows of W per box.  Boxes of part of a
 // tile are made where a tile can lie across frames.
@@ -719,7 +758,7 @@ rf_status launch_pair(const Maps& t, const LinearParams& p, int64_t tiles, const
   }
   const int64_t pairs = std::min<int64_t>(tiles, most);
   pair_kernel<BN><<<static_cast<unsigned>(2 * pairs), kPairThreads, PairCfg<BN>::kSmem, s>>>(
-      t.x, t.many, t.unit, t.w, p);
+      t.x, t.many, t.unit, t.w, t.y, p);
   return launch_status("rf_linear pair_kernel launch");
 }
 
@@ -816,6 +855,13 @@ extern "C" rf_status rf_linear(void* d_Y, int64_t y_row_stride, int out_dtype, c
   if (rows > 256 && pair_tiles >= di.sm_count / 4) {
     p.n_tiles = static_cast<int>(n256);
     if (rf_status st = make_maps(&t, p, d_X, x_row_stride, d_W, w_row_stride, d_in, 128, 128)) return st;
+    t.y = t.x;
+    if (e.vec) {  // 128 bytes of 32 rows
+      const uint64_t dims[2] = {static_cast<uint64_t>(d_out), static_cast<uint64_t>(T)};
+      const uint64_t strides[1] = {static_cast<uint64_t>(y_row_stride) * es_out};
+      const uint32_t box[2] = {128u / es_out, 32};
+      if (rf_status st = make_tensor_map(&t.y, out_dtype, d_Y, 2, dims, strides, box)) return st;
+    }
     return launch_pair<256>(t, p, pair_tiles, di, s);
   }
   int BT = 16;

@@ -31,8 +31,9 @@ rf_status make_tensor_map(CUtensorMap* m, int dtype, const void* base, int rank,
     if (i > 0) s[i - 1] = strides[i - 1];
   }
   const CUresult r =
-      encode(m, dtype == RF_FP16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16
-                                 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
+      encode(m, dtype == RF_FP32   ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                : dtype == RF_FP16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16
+                                   : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
              static_cast<cuuint32_t>(rank), const_cast<void*>(base), d, s, b, e,
              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
