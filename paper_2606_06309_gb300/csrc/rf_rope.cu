@@ -9,9 +9,11 @@
 //
 // The work is one read and one write of the active rows.  A thread keeps its place in the head
 // (16 bytes of it, or 16 bytes of each half) and loads the (cos, sin) of its pairs once per token,
-// for kHeads heads whose loads are all in flight together; blocks of a fixed grid walk the active
+// for four heads whose loads are all in flight together; blocks of a fixed grid walk the active
 // tokens, since their number is known on the device only (a grid for all F frames would launch
-// F/A times the blocks).
+// F/A times the blocks).  Blocks that run together cover all heads of the same tokens, so that rows are
+// read and written whole.  A pair's place in the tables is found again for every token, from three
+// pointers: kept per pair it took 115 registers, and 720p x 40 heads in halves 756 us.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -25,6 +27,7 @@ namespace rf {
 namespace {
 
 constexpr int kRopeThreads = 256;
+constexpr int kHeads = 4;  // of a thread: 64 bytes in flight, 128 in halves
 
 struct RopeSide {  // queries or keys
   char* y;
@@ -73,43 +76,27 @@ struct __align__(sizeof(T) * E) Vec {
 template <typename T, int E, bool HALF>
 __global__ void __launch_bounds__(kRopeThreads)
     rope_kernel(const RopeParams p) {
-  constexpr int kHeads = HALF ? 2 : 4;          // heads per thread: 64 bytes in flight
-  constexpr int kPairs = HALF ? E : E / 2;      // pairs of a unit
+  constexpr int kPairs = HALF ? E : E / 2;  // pairs of a unit
   constexpr int kVecs = HALF ? 2 : 1;
   using V = Vec<T, E>;
-  const bool keys = static_cast<int>(blockIdx.y) >= p.side[0].groups;
+  const bool keys = static_cast<int>(blockIdx.x) >= p.side[0].groups;
   const RopeSide s = p.side[keys];
-  const int h0 = (blockIdx.y - (keys ? p.side[0].groups : 0)) * kHeads;
+  const int h0 = (blockIdx.x - (keys ? p.side[0].groups : 0)) * kHeads;
   const int nh = min(kHeads, s.heads - h0);
   const int slots = kRopeThreads / p.units;  // tokens of a block at a time
   const int slot = threadIdx.x / p.units, u = threadIdx.x - slot * p.units;
   if (slot >= slots) return;
 
-  // this unit's place in the head and its pairs' places in the tables
+  // this unit's place in the head
   const int pair0 = u * kPairs;
   const bool through = HALF && pair0 >= p.pairs;  // whole units only (host: pairs % kPairs == 0)
   const int at = (through ? p.pairs * 2 + (u - p.pairs / kPairs) * E : u * E) * sizeof(T);
   const int to_other = p.pairs * static_cast<int>(sizeof(T));  // HALF: from i to i + R/2
-  const float2* tab[kPairs];
-  int axis[kPairs];
-#pragma unroll
-  for (int i = 0; i < kPairs; ++i) {
-    int j = pair0 + i, a = 0;
-    if (j >= p.half[0]) {
-      j -= p.half[0];
-      a = 1;
-      if (j >= p.half[1]) {
-        j -= p.half[1];
-        a = 2;
-      }
-    }
-    axis[i] = pair0 + i < p.pairs ? a : -1;
-    tab[i] = p.table[a] + j;
-  }
+  const int end_t = p.half[0], end_h = end_t + p.half[1];      // the axes' pairs end here
 
   const int A = p.active ? min(max(p.counts[0], 0), p.F) : p.F;
-  const uint32_t rows = static_cast<uint32_t>(A) * p.N, step = gridDim.x * slots;
-  for (uint32_t r = blockIdx.x * slots + slot; r < rows; r += step) {
+  const uint32_t rows = static_cast<uint32_t>(A) * p.N, step = gridDim.y * slots;
+  for (uint32_t r = blockIdx.y * slots + slot; r < rows; r += step) {
     uint32_t f, t, y, x;
     p.by_N.divmod(r, f, t);
     p.by_gw.divmod(t, y, x);
@@ -125,13 +112,17 @@ __global__ void __launch_bounds__(kRopeThreads)
         if (HALF && !through)
           v[h][kVecs - 1] = *reinterpret_cast<const V*>(src + h * p.head_bytes + to_other);
       }
-    const int64_t row[3] = {static_cast<int64_t>(f) * p.half[0], static_cast<int64_t>(y) * p.half[1],
-                            static_cast<int64_t>(x) * p.half[2]};
+    // the token's rows of the tables, as if each began with the first pair of all
+    const float2* tab_t = p.table[0] + static_cast<int64_t>(f) * p.half[0];
+    const float2* tab_h = p.table[1] + (static_cast<int64_t>(y) * p.half[1] - end_t);
+    const float2* tab_w = p.table[2] + (static_cast<int64_t>(x) * p.half[2] - end_h);
     float2 cs[kPairs];
 #pragma unroll
-    for (int i = 0; i < kPairs; ++i)
-      cs[i] = axis[i] < 0 ? make_float2(1.f, 0.f)
-                          : __ldg(tab[i] + (axis[i] == 0 ? row[0] : axis[i] == 1 ? row[1] : row[2]));
+    for (int i = 0; i < kPairs; ++i) {
+      const int g = pair0 + i;
+      const float2* tab = g < end_t ? tab_t : g < end_h ? tab_h : tab_w;
+      cs[i] = g < p.pairs ? __ldg(tab + g) : make_float2(1.f, 0.f);
+    }
 #pragma unroll
     for (int h = 0; h < kHeads; ++h) {
       if (h >= nh) break;
@@ -141,7 +132,7 @@ __global__ void __launch_bounds__(kRopeThreads)
         T& e1 = v[h][kVecs - 1].e[HALF ? i : 2 * i + 1];
         const float x0 = to_f(e0), x1 = to_f(e1), sn = p.sign * cs[i].y;
         const float y0 = fmaf(x0, cs[i].x, -(x1 * sn)), y1 = fmaf(x0, sn, x1 * cs[i].x);
-        if (axis[i] >= 0) {  // elements past R keep their bits
+        if (pair0 + i < p.pairs) {  // elements past R keep their bits
           e0 = from_f<T>(y0);
           e1 = from_f<T>(y1);
         }
@@ -155,7 +146,6 @@ __global__ void __launch_bounds__(kRopeThreads)
 
 template <typename T, int E, bool HALF>
 rf_status launch_rope(RopeParams p, int sm_count, cudaStream_t stream) {
-  constexpr int kHeads = HALF ? 2 : 4;
   const int d = p.head_bytes / static_cast<int>(sizeof(T));
   p.units = HALF ? p.pairs / E + (d - 2 * p.pairs) / E : d / E;
   for (RopeSide& s : p.side) s.groups = (s.heads + kHeads - 1) / kHeads;
@@ -163,7 +153,7 @@ rf_status launch_rope(RopeParams p, int sm_count, cudaStream_t stream) {
   const int64_t blocks = (static_cast<int64_t>(p.F) * p.N + slots - 1) / slots;
   // eight blocks of 256 threads fill an SM; four times that many even out the blocks' ends
   const int64_t most = std::max<int64_t>(1, static_cast<int64_t>(sm_count) * 32 / groups);
-  const dim3 grid(static_cast<unsigned>(std::min(blocks, most)), groups);
+  const dim3 grid(groups, static_cast<unsigned>(std::min(blocks, most)));
   rope_kernel<T, E, HALF><<<grid, kRopeThreads, 0, stream>>>(p);
   return launch_status("rope_kernel launch");
 }
