@@ -8,7 +8,7 @@
 // ones.  Products and sums in 32 bits, one rounding to the stored type.
 //
 // The work is one read and one write of the active rows.  A thread keeps its place in the head
-// (16 bytes of it, or 16 bytes of each half) and loads the (cos, sin) of its pairs once per token,
+// (16 bytes of it, or 8 to 16 bytes of each half) and loads the (cos, sin) of its pairs once per token,
 // for four heads whose loads are all in flight together; blocks of a fixed grid walk the active
 // tokens, since their number is known on the device only (a grid for all F frames would launch
 // F/A times the blocks).  Blocks that run together cover all heads of the same tokens, so that rows are
@@ -27,7 +27,7 @@ namespace rf {
 namespace {
 
 constexpr int kRopeThreads = 256;
-constexpr int kHeads = 4;  // of a thread: 64 bytes in flight, 128 in halves
+constexpr int kHeads = 4;  // of a thread: 64 bytes in flight
 
 struct RopeSide {  // queries or keys
   char* y;
@@ -160,11 +160,11 @@ rf_status launch_rope(RopeParams p, int sm_count, cudaStream_t stream) {
 
 template <typename T>
 rf_status launch_rope_type(const RopeParams& p, bool half, int sm_count, cudaStream_t stream) {
-  constexpr int E = 16 / sizeof(T);
-  if (!half) return launch_rope<T, E, false>(p, sm_count, stream);
-  // the second half of the pairs, and what passes through behind it, start on 16 bytes only
-  // where R/2 is a multiple of a vector
-  if (p.pairs % E == 0) return launch_rope<T, E, true>(p, sm_count, stream);
+  if (!half) return launch_rope<T, 16 / sizeof(T), false>(p, sm_count, stream);
+  // Halves: four elements of each at a time.  With eight of a 16-bit type the pairs' angles take 116
+  // registers, two blocks per SM: 720p x 40 heads 656 us.  The second half of the pairs, and what
+  // passes through behind it, start on a vector's boundary only where R/2 is a multiple of four.
+  if (p.pairs % 4 == 0) return launch_rope<T, 4, true>(p, sm_count, stream);
   return launch_rope<T, 1, true>(p, sm_count, stream);
 }
 
