@@ -1,0 +1,106 @@
+"""A transformer block of a video diffusion model, run for the active frames of a step.
+
+The step core's attention with the operators around it, on one stream with no host synchronisation:
+
+  1. rf_linear   queries, keys and values of the active frames' tokens, one product
+  2. rf_rope     rotary positions over time, height and width, in place
+  3. rf_project_kv, rf_attn   (StepCore) skipped frames' keys and values from the layer's rolling cache,
+                 which holds rotated keys; active queries over the whole sequence
+  4. rf_linear   output projection, gated, onto the stream of hidden states
+  5. rf_linear, rf_cross_attn, rf_linear   attention to the encoder's states, onto the stream
+  6. rf_linear   feed-forward pair: activation in the first, gate and stream in the second
+
+The hidden states are [F*N, D] for all frames; only the active frames' rows are read and written.
+Normalisations stay the model's: each of the three is a callable on the hidden states.
+"""
+from __future__ import annotations
+
+from dataclasses import dataclass
+from typing import Callable, Optional, Tuple
+
+import numpy as np
+import torch
+
+from . import rf_cross_attn, rf_linear, rf_rope, rf_rope_table
+from .stepcore import StepCore
+
+Linear = Tuple[torch.Tensor, Optional[torch.Tensor]]  # weight [out, in], bias [out] or None
+
+
+@dataclass
+class BlockWeights:
+    qkv: Linear      # [3 H d, D]: queries, keys, values
+    out: Linear      # [D, H d]
+    cross_q: Linear  # [H d, D]
+    cross_kv: Linear  # [2 Hkv d, De]: keys, values of the encoder's states
+    cross_out: Linear  # [D, H d]
+    up: Linear       # [Df, D]
+    down: Linear     # [D, Df]
+
+
+class ActiveBlock:
+    """Buffers and tables of one block over `core`'s frames, whose N tokens are a grid gh x gw.
+
+    dims: rotated elements of a head per axis (time, height, width).  positions: the axes' positions,
+    0, 1, 2, ... where None.  core's key/value cache is this layer's."""
+
+    def __init__(self, core: StepCore, gh: int, gw: int, weights: BlockWeights, dims, heads_kv: int,
+                 positions=None, base: float = 10000.0, pairing: str = "interleaved",
+                 act: str = "gelu_tanh"):
+        if gh * gw != core.N:
+            raise ValueError(f"a grid of {gh} x {gw} is not {core.N} tokens")
+        self.core, self.gh, self.gw, self.w = core, gh, gw, weights
+        self.dims, self.heads_kv, self.pairing, self.act = tuple(dims), heads_kv, pairing, act
+        T, H, d = core.F * core.N, core.H, core.d
+        wt = weights.qkv[0]
+        pos = positions or [np.arange(n) for n in (core.F, gh, gw)]
+        self.tables = [torch.from_numpy(rf_rope_table(p, dim, base)).to(wt.device) if dim else None
+                       for p, dim in zip(pos, self.dims)]
+        self.qkv = torch.zeros(T, 3, H, d, dtype=wt.dtype, device=wt.device)
+        self.rows = torch.zeros(T, H, d, dtype=wt.dtype, device=wt.device)  # attention's results
+        self.ffn = torch.zeros(T, weights.up[0].shape[0], dtype=wt.dtype, device=wt.device)
+        self.enc = None        # [L, 2, Hkv, d]
+        self.enc_mask = self.enc_range = None
+
+    def encode(self, states: torch.Tensor, mask=None, ranges=None, stream=None):
+        """Keys and values of an encoder's states [L, De], kept until the next call: once per prompt.
+        mask [L]: zero = padding; ranges int32 [F, 2]: the states each frame sees."""
+        L = states.shape[0]
+        w, b = self.w.cross_kv
+        self.enc = torch.empty(L, 2, self.heads_kv, self.core.d, dtype=w.dtype, device=w.device)
+        rf_linear(self.enc.view(L, -1), states, w, 1, L, bias=b, status=self.core.status,
+                  stream=stream)
+        self.enc_mask, self.enc_range = mask, ranges
+
+    def run(self, s: int, x: torch.Tensor, scale: float, norms=(None, None, None), gates=(None, None),
+            stream=None):
+        """Step s: x [F*N, D], rows of the active frames updated in place.  norms: callables in front
+        of the attention, the attention to the encoder and the feed-forward pair (None: none);
+        gates: fp32 [D] or [F, D] of the attention and of the feed-forward pair (None: 1).
+
+        core.compact(s) has been called for the step (once, for all blocks)."""
+        c, w = self.core, self.w
+        T, F, N, H, d = c.F * c.N, c.F, c.N, c.H, c.d
+        on = dict(active=c.active, counts=c.counts, stream=stream)
+        lin = dict(on, status=c.status)
+        n1, n2, n3 = (n or (lambda h: h) for n in norms)
+        q, k, v = self.qkv.unbind(1)
+
+        rf_linear(self.qkv.view(T, -1), n1(x), w.qkv[0], F, N, bias=w.qkv[1], **lin)
+        rf_rope(q, q, k, k, F, self.gh, self.gw, self.dims, self.tables, pairing=self.pairing, **on)
+        if c.Kc is not None:
+            c.project_kv(s, k, v, stream)
+        c.attn(self.rows, q, k, v, scale, None, stream)
+        rf_linear(x, self.rows.view(T, H * d), w.out[0], F, N, bias=w.out[1], gate=gates[0],
+                  residual=x, **lin)
+
+        if self.enc is not None:
+            qc = self.qkv[:, 0]
+            rf_linear(qc.view(T, H * d), n2(x), w.cross_q[0], F, N, bias=w.cross_q[1], **lin)
+            rf_cross_attn(self.rows, None, qc, self.enc[:, 0], self.enc[:, 1], F, N, scale,
+                          kv_range=self.enc_range, key_mask=self.enc_mask, **lin)
+            rf_linear(x, self.rows.view(T, H * d), w.cross_out[0], F, N, bias=w.cross_out[1],
+                      residual=x, **lin)
+
+        rf_linear(self.ffn, n3(x), w.up[0], F, N, bias=w.up[1], act=self.act, **lin)
+        rf_linear(x, self.ffn, w.down[0], F, N, bias=w.down[1], gate=gates[1], residual=x, **lin)
