@@ -515,7 +515,8 @@ constexpr int kSplitRing = 212992;  // bytes for stages; the sums of a split tak
 constexpr int kSplitBarFull = 0, kSplitBarEmpty = kSplitMaxStages,
               kSplitBarAcc = 2 * kSplitMaxStages, kSplitBars = kSplitBarAcc + 1;
 constexpr int kSplitOffBar = kSplitRing, kSplitOffMisc = kSplitOffBar + kSplitBars * 8,
-              kSplitOffTok = kSplitOffMisc + 16, kSplitOffList = kSplitOffTok + 256 * 8,
+              kSplitOffBoxes = kSplitOffMisc + 16,
+              kSplitOffTok = kSplitOffBoxes + 16, kSplitOffList = kSplitOffTok + 256 * 8,
               kSplitSmem = kSplitOffList + sizeof(BoxList<256>) + 1024;
 
 __global__ void __launch_bounds__(kSplitThreads, 1)
@@ -552,9 +553,14 @@ __global__ void __launch_bounds__(kSplitThreads, 1)
     tma_prefetch_desc(&tmX);
     tma_prefetch_desc(&tmW);
   }
+  BoxList<256>& list = *reinterpret_cast<BoxList<256>*>(smem + kSplitOffList);
+  RowBoxes* boxes = reinterpret_cast<RowBoxes*>(smem + kSplitOffBoxes);
   if (warp == 2) {
     tmem_alloc(smem_u32(tmem_slot), tmem_cols);
     tmem_relinquish();
+  } else if (warp == 3) {
+    const RowBoxes x = list_boxes(p.rows, R, r0, BT, list);
+    if (lane == 0) *boxes = x;
   }
   tc_fence_before();
   __syncthreads();
@@ -562,11 +568,15 @@ __global__ void __launch_bounds__(kSplitThreads, 1)
   const uint32_t tmem = *tmem_slot;
   const int kb0 = p.kblocks * rank / C, kb1 = p.kblocks * (rank + 1) / C;
 
-  if (warp == 0) {
+  const RowBoxes x = *boxes;
+  // rows loaded one by one are dealt to all warps but the MMA warp: one warp would take a hundred
+  // cycles for each (33 frames of one token, 1536 -> 6144: 29 us)
+  const int loaders = x.n_unit > 8 ? kSplitThreads / 32 - 1 : 1;
+  const int who = warp == 0 ? 0 : warp - 1;
+  if (warp != 1 && who < loaders) {
     const bool lead = elect_one();
-    BoxList<256>& list = *reinterpret_cast<BoxList<256>*>(smem + kSplitOffList);
-    const RowBoxes x = list_boxes(p.rows, R, r0, BT, list);
     int it = 0;
+#pragma unroll 1
     for (int kb = kb0; kb < kb1; ++kb, ++it) {
       const int s = it % p.stages;
       if (!warp_wait<false>(bar(kSplitBarEmpty + s), ((it / p.stages) & 1) ^ 1, abort)) {
@@ -575,15 +585,19 @@ __global__ void __launch_bounds__(kSplitThreads, 1)
       }
       const uint32_t dst = sbase + s * stage_bytes;
       if (lead) {
-        mbar_arrive_expect_tx(bar(kSplitBarFull + s), 16384 + x.rows * 128);
-        tma_load_2d(dst, &tmW, bar(kSplitBarFull + s), kb * kBlockK, n * 128);
+        if (who == 0) {
+          mbar_arrive_expect_tx(bar(kSplitBarFull + s), 16384 + x.rows * 128);
+          tma_load_2d(dst, &tmW, bar(kSplitBarFull + s), kb * kBlockK, n * 128);
+        }
         load_rows<false>(x, list, {&tmX, &tmMany, &tmUnit}, dst + 16384,
-                         bar(kSplitBarFull + s), kb * kBlockK, 0, 1);
+                         bar(kSplitBarFull + s), kb * kBlockK, who, loaders);
       }
       __syncwarp();
     }
-    for (int s = 0; s < p.stages; ++s)  // every copy has landed
-      if (it > s) mbar_drain(bar(kSplitBarFull + s), ((it - 1 - s) / p.stages) & 1, kDrainLimitNs);
+    if (who == 0)
+#pragma unroll 1
+      for (int s = 0; s < p.stages; ++s)  // every copy has landed
+        if (it > s) mbar_drain(bar(kSplitBarFull + s), ((it - 1 - s) / p.stages) & 1, kDrainLimitNs);
   } else if (warp == 1) {
     const bool lead = elect_one();
     const uint32_t idesc = idesc_f16(p.fp16, 128, BT, 0);
@@ -714,11 +728,35 @@ rf_status map_2d(CUtensorMap* m, int dtype, const void* base, int cols, int64_t 
   return make_tensor_map(m, dtype, base, 2, dims, strides, box);
 }
 
-// CTAs per cluster of a split launch: as many ranges of K as fill the SMs, of at least two blocks.
-int split_ranges(int64_t tiles, int kblocks, int sms) {
-  int c = 1;
-  while (c < 8 && tiles * c * 2 <= sms && kblocks >= c * 4) c *= 2;
-  return c;
+// Tokens per tile and CTAs per cluster of a split launch: the pair with the least to do for the busiest
+// SM, in cycles.  Per 64 columns of K a CTA loads its tile of W and of X at about 50 bytes per cycle
+// (its products take 2 cycles per token, less); start and end cost about 5000, a cluster's two barriers
+// 1500, and each four tokens of a thread one round trip per CTA of the cluster, 600 cycles and 150 for
+// every further CTA.  Clusters of 4 and 8 do not fill the GPCs: 36 and 15 of them run together.
+// (333 rows 1000 -> 777: tiles of 256 tokens in clusters of eight 14.5 us.)
+struct SplitPlan {
+  int tokens, cluster;
+};
+SplitPlan split_plan(int64_t rows, int64_t n128, int kblocks, int sms) {
+  SplitPlan best{256, 1};
+  double least = 0;
+  for (int bt = 16; bt <= 256; bt *= 2) {
+    for (int c = 1; c <= 8 && c <= kblocks; c *= 2) {
+      const int64_t ctas = (rows + bt - 1) / bt * n128 * c;
+      const int64_t at_once = c == 8 ? sms * 120 / 152 : c == 4 ? sms * 144 / 152 : sms;
+      const int64_t rounds = (ctas + at_once - 1) / at_once;
+      const int join = (bt / 2 + 4 * c - 1) / (4 * c);  // groups of four tokens of a thread
+      const double one = 5000.0 + (kblocks + c - 1) / c * ((16384.0 + 128.0 * bt) / 50) +
+                         join * (600.0 + 150.0 * (c - 1)) + (c > 1 ? 1500 : 0);
+      const double cost = static_cast<double>(rounds) * one;
+      if (least == 0 || cost < least) {
+        least = cost;
+        best = {bt, c};
+      }
+    }
+    if (bt >= rows) break;
+  }
+  return best;
 }
 
 struct Maps {
@@ -864,12 +902,12 @@ extern "C" rf_status rf_linear(void* d_Y, int64_t y_row_stride, int out_dtype, c
     }
     return launch_pair<256>(t, p, pair_tiles, di, s);
   }
-  int BT = 16;
-  while (BT < 256 && BT < rows) BT *= 2;
+  const SplitPlan plan = split_plan(rows, n128, p.kblocks, di.sm_count);
+  const int BT = plan.tokens;
   const int64_t tiles = (rows + BT - 1) / BT * n128;
   p.n_tiles = static_cast<int>(n128);
   p.tile_tokens = BT;
-  p.cluster = split_ranges(tiles, p.kblocks, di.sm_count);
+  p.cluster = plan.cluster;
   p.stages = std::min(kSplitMaxStages, kSplitRing / (16384 + BT * 128));
   if (rf_status st = make_maps(&t, p, d_X, x_row_stride, d_W, w_row_stride, d_in, BT, 128)) return st;
   return launch_split(t, p, tiles, di, s);
