@@ -97,6 +97,54 @@ __device__ __forceinline__ void add2(uint32_t w, int dtype, float& lo, float& hi
   hi += b;
 }
 
+// Gate, residual and store of four columns of a row: VEC: from n on, as vectors; otherwise n, n + 32, ...
+template <bool VEC>
+__device__ __forceinline__ void finish4(const Epilogue& e, int64_t token, int frame, int n, float* v) {
+  constexpr int kApart = VEC ? 1 : 32;
+  const int64_t at = token * e.y_stride + n, at_r = token * e.r_stride + n;
+  const float* g = e.gate ? e.gate + frame * e.gate_stride + n : nullptr;
+  if (!VEC || n + 4 > e.n_out) {
+    float res[4] = {};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (n + i * kApart < e.n_out) {
+        if (g) v[i] *= g[i * kApart];
+        if (e.R) res[i] = load_elem(e.R, at_r + i * kApart, e.out_dtype);
+      }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (n + i * kApart < e.n_out)
+        store_elem(e.Y, at + i * kApart, e.out_dtype, e.R ? v[i] + res[i] : v[i]);
+    return;
+  }
+  if (g) {
+    const float4 x = *reinterpret_cast<const float4*>(g);
+    v[0] *= x.x;
+    v[1] *= x.y;
+    v[2] *= x.z;
+    v[3] *= x.w;
+  }
+  if (e.out_dtype == RF_FP32) {
+    if (e.R) {
+      const float4 x = *reinterpret_cast<const float4*>(static_cast<const float*>(e.R) + at_r);
+      v[0] += x.x;
+      v[1] += x.y;
+      v[2] += x.z;
+      v[3] += x.w;
+    }
+    *reinterpret_cast<float4*>(static_cast<float*>(e.Y) + at) = make_float4(v[0], v[1], v[2], v[3]);
+  } else {
+    if (e.R) {
+      const uint2 x = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(e.R) + at_r);
+      add2(x.x, e.out_dtype, v[0], v[1]);
+      add2(x.y, e.out_dtype, v[2], v[3]);
+    }
+    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(e.Y) + at) =
+        e.out_dtype == RF_FP16 ? make_uint2(pack_f16x2(v[0], v[1]), pack_f16x2(v[2], v[3]))
+                               : make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+  }
+}
+
 // Columns n .. n + 31 of a row, element by element: the last columns of a result, and rows off the
 // 16-byte boundaries.
 static __device__ __noinline__ void finish_row(const Epilogue& e, int64_t token, int frame, int n,
@@ -519,6 +567,59 @@ constexpr int kSplitOffBar = kSplitRing, kSplitOffMisc = kSplitOffBar + kSplitBa
               kSplitOffTok = kSplitOffBoxes + 16, kSplitOffList = kSplitOffTok + 256 * 8,
               kSplitSmem = kSplitOffList + sizeof(BoxList<256>) + 1024;
 
+// Results of a CTA's share of a tile's tokens from the sums of all CTAs: a warp has kTok tokens at a time,
+// a lane four columns of each, with the loads of all of them in flight.  VEC: neighbouring columns, moved
+// as vectors; otherwise every 32nd, so that a warp's accesses are of consecutive elements either way.
+template <bool VEC>
+__device__ __forceinline__ void finish_tokens(const Epilogue& e, const int2* tokens, uint32_t sums,
+                                              int n0, int BT, int rows, int rank, int C) {
+  constexpr int kTok = 4, kApart = VEC ? 1 : 32;
+  const int lane = threadIdx.x & 31, col = VEC ? 4 * lane : lane, out = n0 + col;
+  if (out >= e.n_out) return;
+  float bias[4] = {};
+  if (e.bias)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (out + i * kApart < e.n_out) bias[i] = load_elem(e.bias, out + i * kApart, e.in_dtype);
+  const int step = kSplitThreads / 32 * C;  // between a warp's tokens
+#pragma unroll 1
+  for (int j0 = kSplitThreads / 32 * rank + (threadIdx.x >> 5); j0 < rows; j0 += kTok * step) {
+    int2 t[kTok];
+    float v[kTok * 4];
+#pragma unroll
+    for (int u = 0; u < kTok; ++u) {
+      const int j = j0 + u * step;
+      t[u] = j < BT ? tokens[j] : make_int2(-1, 0);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[4 * u + i] = bias[i];
+    }
+    const uint32_t at = sums + (j0 * 128 + col) * 4;
+#pragma unroll 2
+    for (int c = 0; c < C; ++c) {
+      const uint32_t base = C > 1 ? map_to_rank(at, c) : at;
+#pragma unroll
+      for (int u = 0; u < kTok; ++u)
+        if (t[u].x >= 0) {
+          const uint32_t from = base + u * step * 512;
+          if (VEC) {
+            const float4 x = ld_cluster_f4(from);
+            v[4 * u] += x.x;
+            v[4 * u + 1] += x.y;
+            v[4 * u + 2] += x.z;
+            v[4 * u + 3] += x.w;
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[4 * u + i] += ld_cluster_f(from + 128 * i);
+          }
+        }
+    }
+    activate(e.act, v);
+#pragma unroll
+    for (int u = 0; u < kTok; ++u)
+      if (t[u].x >= 0) finish4<VEC>(e, t[u].x, t[u].y, out, v + 4 * u);
+  }
+}
+
 __global__ void __launch_bounds__(kSplitThreads, 1)
     split_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmMany,
                  const __grid_constant__ CUtensorMap tmUnit, const __grid_constant__ CUtensorMap tmW,
@@ -653,45 +754,8 @@ __global__ void __launch_bounds__(kSplitThreads, 1)
     cluster_arrive();
     cluster_wait();
   }
-  // A thread has one column, and kTok of the tokens of its half of the threads and its CTA at a
-  // time, with the loads of all of them in flight.
-  constexpr int kTok = 4;
-  const int col = threadIdx.x & 127, out = n * 128 + col;
-  const Epilogue& e = p.epi;
-  if (out < e.n_out) {
-    const float bias = e.bias ? load_elem(e.bias, out, e.in_dtype) : 0.f;
-    const int step = 2 * C;  // between a thread's tokens
-#pragma unroll 1
-    for (int j0 = 2 * rank + (threadIdx.x >> 7); j0 < BT && r0 + j0 < R; j0 += kTok * step) {
-      float sum[kTok], gate[kTok], res[kTok];
-      int2 t[kTok];
-#pragma unroll
-      for (int u = 0; u < kTok; ++u) {
-        const int j = j0 + u * step;
-        t[u] = j < BT ? tokens[j] : make_int2(-1, 0);
-        sum[u] = 0.f;
-        gate[u] = e.gate && t[u].x >= 0 ? e.gate[t[u].y * e.gate_stride + out] : 1.f;
-        res[u] = e.R && t[u].x >= 0 ? load_elem(e.R, t[u].x * e.r_stride + out, e.out_dtype) : 0.f;
-      }
-#pragma unroll 2
-      for (int c = 0; c < C; ++c) {
-        const uint32_t at = sbase + (j0 * 128 + col) * 4;
-        const uint32_t base = C > 1 ? map_to_rank(at, c) : at;
-#pragma unroll
-        for (int u = 0; u < kTok; ++u)
-          if (t[u].x >= 0) sum[u] += ld_cluster_f(base + u * step * 512);
-      }
-#pragma unroll
-      for (int u = 0; u < kTok; ++u) sum[u] += bias;
-      activate(e.act, sum);
-#pragma unroll
-      for (int u = 0; u < kTok; ++u) {
-        if (e.gate) sum[u] *= gate[u];
-        if (e.R) sum[u] += res[u];
-        if (t[u].x >= 0) store_elem(e.Y, t[u].x * e.y_stride + out, e.out_dtype, sum[u]);
-      }
-    }
-  }
+  if (p.epi.vec) finish_tokens<true>(p.epi, tokens, sbase, n * 128, BT, min(BT, R - r0), rank, C);
+  else finish_tokens<false>(p.epi, tokens, sbase, n * 128, BT, min(BT, R - r0), rank, C);
   __syncwarp();
   if (C > 1) {
     cluster_arrive();  // every CTA has read the others' sums
@@ -730,10 +794,10 @@ rf_status map_2d(CUtensorMap* m, int dtype, const void* base, int cols, int64_t 
 
 // Tokens per tile and CTAs per cluster of a split launch: the pair with the least to do for the busiest
 // SM, in cycles.  Per 64 columns of K a CTA loads its tile of W and of X at about 50 bytes per cycle
-// (its products take 2 cycles per token, less); start and end cost about 5000, a cluster's two barriers
-// 1500, and each four tokens of a thread one round trip per CTA of the cluster, 600 cycles and 150 for
+// (its products take 2 cycles per token, less); start and end cost about 5000, a cluster's start and its
+// two barriers 750 per CTA, and each four tokens of a warp one round trip per CTA of the cluster, 700 cycles and 150 for
 // every further CTA.  Clusters of 4 and 8 do not fill the GPCs: 36 and 15 of them run together.
-// (333 rows 1000 -> 777: tiles of 256 tokens in clusters of eight 14.5 us.)
+// (333 rows 1000 -> 777: 10.8 us in tiles of 16 tokens, 14.0 in tiles of 256 and clusters of eight.)
 struct SplitPlan {
   int tokens, cluster;
 };
@@ -745,9 +809,9 @@ SplitPlan split_plan(int64_t rows, int64_t n128, int kblocks, int sms) {
       const int64_t ctas = (rows + bt - 1) / bt * n128 * c;
       const int64_t at_once = c == 8 ? sms * 120 / 152 : c == 4 ? sms * 144 / 152 : sms;
       const int64_t rounds = (ctas + at_once - 1) / at_once;
-      const int join = (bt / 2 + 4 * c - 1) / (4 * c);  // groups of four tokens of a thread
+      const int join = (bt + 32 * c - 1) / (32 * c);  // groups of four tokens of a warp
       const double one = 5000.0 + (kblocks + c - 1) / c * ((16384.0 + 128.0 * bt) / 50) +
-                         join * (600.0 + 150.0 * (c - 1)) + (c > 1 ? 1500 : 0);
+                         join * (700.0 + 150.0 * (c - 1)) + (c > 1 ? 750 * c : 0);
       const double cost = static_cast<double>(rounds) * one;
       if (least == 0 || cost < least) {
         least = cost;
