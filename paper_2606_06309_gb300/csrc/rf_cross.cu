@@ -91,7 +91,7 @@ struct CrossParams {
   int tile_frames;     // packed: frames of a tile
   int cluster;
   float scale_log2;
-  FastDiv by_g, by_frame_rows;
+  FastDiv by_g, by_frame_rows, by_units;
 };
 
 __device__ __forceinline__ void flag_error(const CrossParams& p, int where) {
@@ -102,13 +102,20 @@ __device__ __forceinline__ bool all_wait(uint32_t bar, uint32_t parity, volatile
 }
 
 // The work of a launch, from the active count on the device.
+constexpr int kMaxSorted = 256, kSortRounds = 8;
 struct Work {
   int A, groups, tiles, pairs, items;  // groups of tiles with keys of their own (frames, or one)
-  int first, step;  // this CTA's items
-  FastDiv by_pairs, by_groups;
+  int first, step[2];  // this CTA's items: the steps to the next one, in turn
+  FastDiv by_pairs;
+  // Launches with ranges and a few items per CTA: the frames by falling length.  The items are dealt
+  // to the CTAs from the first to the last, then from the last to the first, and so on, so that who
+  // has a long one of a round has a short one of the next (16 sequences of 1000, 2000 and 3000 states x
+  // 12 heads, in their own order 48 K/V tiles for the busiest CTA, this way 24: 66 us -> 46; with many
+  // rounds lengths even out, and the order costs 2 us at the start).
+  bool sorted;
+  uint8_t order[kMaxSorted];
 };
-__device__ __forceinline__ Work make_work(const CrossParams& p) {
-  Work w;
+__device__ __forceinline__ void make_work(const CrossParams& p, Work& w) {
   w.A = p.rows.frames();
   w.groups = p.kv_range ? w.A : 1;
   if (p.packed)
@@ -117,11 +124,33 @@ __device__ __forceinline__ Work make_work(const CrossParams& p) {
     w.tiles = ((p.kv_range ? p.rows.N : w.A * p.rows.Np) + kBM - 1) / kBM;
   w.pairs = (w.tiles + 1) / 2;
   w.items = p.units * w.groups * w.pairs;
+  const int ctas = gridDim.x / p.cluster;  // (or clusters)
   w.first = blockIdx.x / p.cluster;
-  w.step = gridDim.x / p.cluster;
+  w.sorted = p.kv_range && w.groups > 1 && w.groups <= kMaxSorted && w.items > ctas &&
+             w.items <= kSortRounds * ctas;
+  w.step[0] = w.sorted ? 2 * (ctas - 1 - w.first) + 1 : ctas;
+  w.step[1] = w.sorted ? 2 * w.first + 1 : ctas;
   w.by_pairs = FastDiv(max(w.pairs, 1));
-  w.by_groups = FastDiv(max(w.groups, 1));
-  return w;
+}
+// K/V tiles of a range.
+__device__ __forceinline__ int range_tiles(const CrossParams& p, int frame, int& begin, int& end) {
+  const int2 r = p.kv_range[frame];
+  begin = min(max(r.x, 0), p.L);
+  end = min(max(r.y, begin), p.L);
+  return (end - begin + kBN - 1) / kBN;
+}
+// All threads of the block; `tiles`: room for kMaxSorted numbers.
+__device__ __forceinline__ void sort_frames(const CrossParams& p, Work& w, int* tiles) {
+  const int i = threadIdx.x;
+  int begin, end, mine = 0, rank = 0;
+  if (i < w.groups) tiles[i] = mine = range_tiles(p, p.rows.frame(i), begin, end);
+  __syncthreads();
+  if (i < w.groups) {
+    for (int j = 0; j < w.groups; ++j)
+      rank += tiles[j] > mine || (tiles[j] == mine && j < i);
+    w.order[rank] = static_cast<uint8_t>(i);
+  }
+  __syncthreads();
 }
 
 // One item, or a cluster CTA's share of it: a pair of query tiles of a head over key rows
@@ -134,16 +163,13 @@ __device__ __forceinline__ Item get_item(const CrossParams& p, const Work& w, in
   Item t;
   const int gp = w.by_pairs.div(i);
   t.pair = i - gp * w.pairs;
-  t.unit = w.by_groups.div(gp);
-  t.group = gp - t.unit * w.groups;
+  const int slot = p.by_units.div(gp);
+  t.unit = gp - slot * p.units;
+  t.group = w.sorted ? w.order[slot] : slot;
   t.begin = 0;
   t.end = p.L;
-  if (p.kv_range) {
-    const int2 r = p.kv_range[p.rows.frame(t.group)];
-    t.begin = min(max(r.x, 0), p.L);
-    t.end = min(max(r.y, t.begin), p.L);
-  }
-  const int nt = (t.end - t.begin + kBN - 1) / kBN;  // below 2^24
+  int nt = (p.L + kBN - 1) / kBN;  // below 2^24
+  if (p.kv_range) nt = range_tiles(p, p.rows.frame(t.group), t.begin, t.end);
   t.j0 = 0;
   t.j1 = nt;
   if (p.cluster > 1) {
@@ -278,7 +304,7 @@ __device__ __forceinline__ void producer(const QueryMaps& maps, const CUtensorMa
   int it = 0;
   bool ok = true;
   Load n;
-  int i = w.first;
+  int i = w.first, turn = 0;
   if (i < w.items) prepare_load<D>(maps, p, w, i, rank, list, lead, n);
   while (ok && i < w.items) {
     const Item t = n.t;
@@ -313,7 +339,8 @@ __device__ __forceinline__ void producer(const QueryMaps& maps, const CUtensorMa
         (X ? q_cnt1 : q_cnt0) += 1;
       }
     }
-    i += w.step;
+    i += w.step[turn];
+    turn ^= 1;
     if (ok && i < w.items) prepare_load<D>(maps, p, w, i, rank, list, lead, n);
   }
   if (!ok && lead) flag_error(p, 0);
@@ -336,7 +363,7 @@ __device__ __forceinline__ void cleaner(const CrossParams& p, const Work& w, int
   const int lane = threadIdx.x & 31;
   int it = 1;  // V follows K in the ring
 #pragma unroll 1
-  for (int i = w.first; i < w.items; i += w.step) {
+  for (int i = w.first, turn = 0; i < w.items; i += w.step[turn], turn ^= 1) {
     const Item t = get_item(p, w, i, rank);
 #pragma unroll 1
     for (int j = t.j0; j < t.j1; ++j, it += 2) {
@@ -400,7 +427,7 @@ __device__ __forceinline__ bool mma_issuer(const CrossParams& p, const Work& w, 
   bool my_turn = X == 0;    // the first turn is tile A's
   bool ok = true;
 #pragma unroll 1
-  for (int i = w.first; ok && i < w.items; i += w.step) {
+  for (int i = w.first, turn = 0; ok && i < w.items; i += w.step[turn], turn ^= 1) {
     const Item t = get_item(p, w, i, rank);
     const int nt = t.j1 - t.j0;
     if (nt <= 0) continue;
@@ -596,9 +623,10 @@ __device__ __forceinline__ bool softmax_group(const CUtensorMap* tmO, const Cros
   Item next;
   if (w.first < w.items) next = get_item(p, w, w.first, rank);
 #pragma unroll 1
-  for (int i = w.first; i < w.items;) {
+  for (int i = w.first, turn = 0; i < w.items;) {
     const Item t = next;
-    i += w.step;
+    i += w.step[turn];
+    turn ^= 1;
     const int tile = 2 * t.pair + X;
     if (tile >= w.tiles) {
       if (i < w.items) next = get_item(p, w, i, rank);
@@ -777,7 +805,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int rank = p.cluster > 1 ? static_cast<int>(cluster_rank()) : 0;
 
   __shared__ Work work;
-  if (threadIdx.x == 64) work = make_work(p);
+  if (threadIdx.x == 64) make_work(p, work);
   if (threadIdx.x == 0) {
     for (int X = 0; X < 2; ++X) {
       mbar_init(bar0 + 8 * (C::kQFull + X), 1);
@@ -807,6 +835,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
   const Work& w = work;
+  if (CLEAN && w.sorted) sort_frames(p, work, reinterpret_cast<int*>(smem + C::kOffStage));
 
   // Every warp of warpgroup 0 gives registers back before any softmax warp asks for more, so the
   // increase below always finds them.
@@ -988,6 +1017,7 @@ extern "C" rf_status rf_cross_attn(void* d_O, float* d_lse, const void* d_Q, con
   p.frame_rows = packed ? N * g : 0;
   p.tile_frames = packed ? (d_kv_range ? 1 : kBM / p.frame_rows) : 0;
   p.by_g = FastDiv(static_cast<uint32_t>(g));
+  p.by_units = FastDiv(static_cast<uint32_t>(p.units));
   p.by_frame_rows = FastDiv(static_cast<uint32_t>(std::max(p.frame_rows, 1)));
   p.scale_log2 = static_cast<float>(static_cast<double>(softmax_scale) * 1.4426950408889634);
 
@@ -997,7 +1027,9 @@ extern "C" rf_status rf_cross_attn(void* d_O, float* d_lse, const void* d_Q, con
                                : ((d_kv_range ? Nr : Fr * Np) + kBM - 1) / kBM;
   const int64_t items = p.units * groups * ((tiles + 1) / 2);
   if (items > 0x7FFFFFFF / 16) return fail(RF_ERR_INVALID_ARG, "rf_cross_attn: too many rows");
-  const int kv_tiles = (L + kBN - 1) / kBN;
+  // (the ranges are on the device: taken as shares of the states)
+  const int64_t share = d_kv_range ? (static_cast<int64_t>(L) + F - 1) / F : L;
+  const int64_t kv_tiles = (share + kBN - 1) / kBN;
   p.cluster = cluster_size(items, kv_tiles, di.sm_count);
   const int grid = p.cluster > 1 ? static_cast<int>(items) * p.cluster
                                  : static_cast<int>(std::min<int64_t>(items, di.sm_count));
