@@ -89,6 +89,7 @@ struct CrossParams {
   int packed;          // rows of a tile are (frame, token, query head of the key head)
   int frame_rows;      // packed: rows of a frame, N * g
   int tile_frames;     // packed: frames of a tile
+  int tile_rows;       // not packed: rows of a tile
   int cluster;
   float scale_log2;
   FastDiv by_g, by_frame_rows, by_units;
@@ -104,6 +105,7 @@ __device__ __forceinline__ bool all_wait(uint32_t bar, uint32_t parity, volatile
 // The work of a launch, from the active count on the device.
 constexpr int kMaxSorted = 256, kSortRounds = 8;
 struct Work {
+  int rows;  // of a tile
   int A, groups, tiles, pairs, items;  // groups of tiles with keys of their own (frames, or one)
   int first, step[2];  // this CTA's items: the steps to the next one, in turn
   FastDiv by_pairs;
@@ -116,12 +118,13 @@ struct Work {
   uint8_t order[kMaxSorted];
 };
 __device__ __forceinline__ void make_work(const CrossParams& p, Work& w) {
+  w.rows = p.tile_rows;
   w.A = p.rows.frames();
   w.groups = p.kv_range ? w.A : 1;
   if (p.packed)
     w.tiles = p.kv_range ? 1 : (w.A + p.tile_frames - 1) / p.tile_frames;
   else
-    w.tiles = ((p.kv_range ? p.rows.N : w.A * p.rows.Np) + kBM - 1) / kBM;
+    w.tiles = ((p.kv_range ? p.rows.N : w.A * p.rows.Np) + w.rows - 1) / w.rows;
   w.pairs = (w.tiles + 1) / 2;
   w.items = p.units * w.groups * w.pairs;
   const int ctas = gridDim.x / p.cluster;  // (or clusters)
@@ -191,7 +194,8 @@ __device__ __forceinline__ int row_of(const CrossParams& p, const Work& w, const
     head = t.unit * p.g + (rem - q * p.g);
     return p.rows.frame(a) * p.rows.N + q;
   }
-  const int r = tile * kBM + row;
+  const int r = tile * w.rows + row;
+  if (row >= w.rows) return -1;
   if (p.kv_range) return r < p.rows.N ? p.rows.frame(t.group) * p.rows.N + r : -1;
   if (r >= w.A * p.rows.Np) return -1;
   const int a = p.rows.by_Np.div(r), q = r - a * p.rows.Np;
@@ -202,7 +206,7 @@ __device__ __forceinline__ int row_of(const CrossParams& p, const Work& w, const
 // frames or heads, or fewer than 128.
 __device__ __forceinline__ int whole_tile(const CrossParams& p, const Work& w, const Item& t, int tile) {
   const int r = tile * kBM;
-  if (p.packed) return -1;
+  if (p.packed || w.rows < kBM) return -1;
   if (p.kv_range) return r + kBM <= p.rows.N ? p.rows.frame(t.group) * p.rows.N + r : -1;
   const int a = p.rows.by_Np.div(r), q = r - a * p.rows.Np;
   return a < w.A && q + kBM <= p.rows.N ? p.rows.frame(a) * p.rows.N + q : -1;
@@ -250,7 +254,7 @@ __device__ __forceinline__ void prepare_load(const QueryMaps& maps, const CrossP
     if (tile >= w.tiles) break;
     const RowBoxes x =
         p.kv_range ? RowBoxes{kBM, 0, 0, p.rows.frame(n.t.group) * p.rows.N + tile * kBM}
-                   : list_boxes(p.rows, w.A * p.rows.Np, tile * kBM, kBM, list[X]);
+                   : list_boxes(p.rows, w.A * p.rows.Np, tile * w.rows, w.rows, kBM, list[X]);
     (X ? n.x1 : n.x0) = x;
     // on their way to L2 while the item before is worked on: the queries' own buffer is free only
     // when that item's last Q K^T is done
@@ -1014,6 +1018,7 @@ extern "C" rf_status rf_cross_attn(void* d_O, float* d_lse, const void* d_Q, con
   p.g = g;
   p.packed = packed;
   p.units = packed ? Hkv : H;
+  p.tile_rows = d_kv_range ? kBM : tile_rows(unit, kBM);
   p.frame_rows = packed ? N * g : 0;
   p.tile_frames = packed ? (d_kv_range ? 1 : kBM / p.frame_rows) : 0;
   p.by_g = FastDiv(static_cast<uint32_t>(g));
@@ -1024,7 +1029,7 @@ extern "C" rf_status rf_cross_attn(void* d_O, float* d_lse, const void* d_Q, con
   // at most, with every frame active
   const int64_t groups = d_kv_range ? F : 1;
   const int64_t tiles = packed ? (d_kv_range ? 1 : (Fr + p.tile_frames - 1) / p.tile_frames)
-                               : ((d_kv_range ? Nr : Fr * Np) + kBM - 1) / kBM;
+                               : ((d_kv_range ? Nr : Fr * Np) + p.tile_rows - 1) / p.tile_rows;
   const int64_t items = p.units * groups * ((tiles + 1) / 2);
   if (items > 0x7FFFFFFF / 16) return fail(RF_ERR_INVALID_ARG, "rf_cross_attn: too many rows");
   // (the ranges are on the device: taken as shares of the states)

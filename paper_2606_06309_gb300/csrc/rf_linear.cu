@@ -304,6 +304,7 @@ struct LinearParams {
   int32_t* status;
   // split_kernel
   int tile_tokens, cluster, stages;
+  int tile_rows;  // rows of a tile of split_kernel, or of a CTA's half of a pair's
 };
 
 __device__ __forceinline__ void flag_error(const LinearParams& p, int where) {
@@ -424,7 +425,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
   const uint32_t tmem = *tmem_slot;
 
   const int R = p.rows.frames() * p.rows.Np;
-  const int m_tiles = (R + 255) / 256;
+  const int half = p.tile_rows;  // rows of a CTA's half of a tile
+  const int m_tiles = (R + 2 * half - 1) / (2 * half);
   const int tiles = m_tiles * p.n_tiles;
   const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
 
@@ -439,11 +441,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
     for (int t = pair; ok && t < tiles; t += pairs) {
       int m, n;
       tile_at(t, m_tiles, p.n_tiles, m, n);
-      const RowBoxes x = list_boxes(p.rows, R, m * 256 + rank * 128, 128, list);
+      const RowBoxes x = list_boxes(p.rows, R, (2 * m + rank) * half, half, 128, list);
       const int w0 = n * BN + rank * (BN / 2);
       // of both CTAs, the other one's rows included
       const int bytes = 2 * C::kBBytes +
-                        (x.rows + (rank == 0 ? boxed_rows(p.rows, R, m * 256 + 128, 128) : 0)) * 128;
+                        (x.rows + (rank == 0 ? boxed_rows(p.rows, R, (2 * m + 1) * half, half, 128)
+                                             : 0)) * 128;
       for (int kb = 0; kb < p.kblocks; ++kb, ++it) {
         const int s = it % C::kStages;
         if (!warp_wait<true>(bar(C::kBarEmpty + s), ((it / C::kStages) & 1) ^ 1, abort)) {
@@ -515,9 +518,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
       int m, n;
       tile_at(t, m_tiles, p.n_tiles, m, n);
       const int b = n_acc & 1;
-      const int r = m * 256 + rank * 128 + quarter * 32 + lane;
+      const int row = quarter * 32 + lane, r = (2 * m + rank) * half + row;
       int frame = 0;
-      const int token = r < R ? row_token(p, r, frame) : -1;
+      const int token = row < half && r < R ? row_token(p, r, frame) : -1;
       auto ready = [&]() -> bool {
         const bool ok = warp_wait<true>(bar(C::kBarAccFull + b),
                                                                   (n_acc >> 1) & 1, abort);
@@ -638,7 +641,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1)
   const int tile = blockIdx.x / C;
   const int m = tile / p.n_tiles, n = tile - m * p.n_tiles;
   const int R = p.rows.frames() * p.rows.Np;
-  const int r0 = m * BT;
+  const int r0 = m * p.tile_rows, rows = min(p.tile_rows, R - r0);
   if (r0 >= R) return;  // the whole cluster
   const int stage_bytes = 16384 + BT * 128;
   const uint32_t tmem_cols = BT < 32 ? 32 : BT;
@@ -660,7 +663,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1)
     tmem_alloc(smem_u32(tmem_slot), tmem_cols);
     tmem_relinquish();
   } else if (warp == 3) {
-    const RowBoxes x = list_boxes(p.rows, R, r0, BT, list);
+    const RowBoxes x = list_boxes(p.rows, R, r0, p.tile_rows, BT, list);
     if (lane == 0) *boxes = x;
   }
   tc_fence_before();
@@ -670,9 +673,9 @@ __global__ void __launch_bounds__(kSplitThreads, 1)
   const int kb0 = p.kblocks * rank / C, kb1 = p.kblocks * (rank + 1) / C;
 
   const RowBoxes x = *boxes;
-  // rows loaded one by one are dealt to all warps but the MMA warp: one warp would take a hundred
-  // cycles for each (33 frames of one token, 1536 -> 6144: 29 us)
-  const int loaders = x.n_unit > 8 ? kSplitThreads / 32 - 1 : 1;
+  // the boxes of a tile across frames are dealt to all warps but the MMA warp: one warp would take a
+  // hundred cycles for each (33 frames of one token, 1536 -> 6144: 29 us, this way 16)
+  const int loaders = x.n_many + x.n_unit > 2 ? kSplitThreads / 32 - 1 : 1;
   const int who = warp == 0 ? 0 : warp - 1;
   if (warp != 1 && who < loaders) {
     const bool lead = elect_one();
@@ -732,7 +735,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1)
 #pragma unroll 1
     for (int j = threadIdx.x - 128; j < BT; j += 128) {
       int2 t = make_int2(-1, 0);
-      if (r0 + j < R) t.x = row_token(p, r0 + j, t.y);
+      if (j < rows) t.x = row_token(p, r0 + j, t.y);
       tokens[j] = t;
     }
     const bool ok = warp_wait<false>(bar(kSplitBarAcc), 0, abort);
@@ -754,8 +757,8 @@ __global__ void __launch_bounds__(kSplitThreads, 1)
     cluster_arrive();
     cluster_wait();
   }
-  if (p.epi.vec) finish_tokens<true>(p.epi, tokens, sbase, n * 128, BT, min(BT, R - r0), rank, C);
-  else finish_tokens<false>(p.epi, tokens, sbase, n * 128, BT, min(BT, R - r0), rank, C);
+  if (p.epi.vec) finish_tokens<true>(p.epi, tokens, sbase, n * 128, BT, rows, rank, C);
+  else finish_tokens<false>(p.epi, tokens, sbase, n * 128, BT, rows, rank, C);
   __syncwarp();
   if (C > 1) {
     cluster_arrive();  // every CTA has read the others' sums
@@ -801,12 +804,13 @@ rf_status map_2d(CUtensorMap* m, int dtype, const void* base, int cols, int64_t 
 struct SplitPlan {
   int tokens, cluster;
 };
-SplitPlan split_plan(int64_t rows, int64_t n128, int kblocks, int sms) {
+SplitPlan split_plan(int64_t rows, int unit, int64_t n128, int kblocks, int sms) {
   SplitPlan best{256, 1};
   double least = 0;
   for (int bt = 16; bt <= 256; bt *= 2) {
     for (int c = 1; c <= 8 && c <= kblocks; c *= 2) {
-      const int64_t ctas = (rows + bt - 1) / bt * n128 * c;
+      const int tile = tile_rows(unit, bt);
+      const int64_t ctas = (rows + tile - 1) / tile * n128 * c;
       const int64_t at_once = c == 8 ? sms * 120 / 152 : c == 4 ? sms * 144 / 152 : sms;
       const int64_t rounds = (ctas + at_once - 1) / at_once;
       const int join = (bt + 32 * c - 1) / (32 * c);  // groups of four tokens of a warp
@@ -818,7 +822,7 @@ SplitPlan split_plan(int64_t rows, int64_t n128, int kblocks, int sms) {
         best = {bt, c};
       }
     }
-    if (bt >= rows) break;
+    if (tile_rows(unit, bt) >= rows) break;
   }
   return best;
 }
@@ -952,10 +956,12 @@ extern "C" rf_status rf_linear(void* d_Y, int64_t y_row_stride, int out_dtype, c
 
   const int64_t rows = Fr * Np;  // at most: the active count is known on the device only
   const int64_t n256 = (d_out + 255) / 256, n128 = (d_out + 127) / 128;
-  const int64_t pair_tiles = (rows + 255) / 256 * n256;
+  const int half = tile_rows(unit, 128);
+  const int64_t pair_tiles = (rows + 2 * half - 1) / (2 * half) * n256;
   Maps t;
   if (rows > 256 && pair_tiles >= di.sm_count / 4) {
     p.n_tiles = static_cast<int>(n256);
+    p.tile_rows = half;
     if (rf_status st = make_maps(&t, p, d_X, x_row_stride, d_W, w_row_stride, d_in, 128, 128)) return st;
     t.y = t.x;
     if (e.vec) {  // 128 bytes of 32 rows
@@ -966,9 +972,10 @@ extern "C" rf_status rf_linear(void* d_Y, int64_t y_row_stride, int out_dtype, c
     }
     return launch_pair<256>(t, p, pair_tiles, di, s);
   }
-  const SplitPlan plan = split_plan(rows, n128, p.kblocks, di.sm_count);
+  const SplitPlan plan = split_plan(rows, unit, n128, p.kblocks, di.sm_count);
   const int BT = plan.tokens;
-  const int64_t tiles = (rows + BT - 1) / BT * n128;
+  p.tile_rows = tile_rows(unit, BT);
+  const int64_t tiles = (rows + p.tile_rows - 1) / p.tile_rows * n128;
   p.n_tiles = static_cast<int>(n128);
   p.tile_tokens = BT;
   p.cluster = plan.cluster;

@@ -22,8 +22,10 @@ struct RowMap {
   __device__ __forceinline__ int frame(int a) const { return active ? active[a] : a; }
 };
 // Frames of 8 tokens or more are padded to 8 rows, a swizzle atom of shared memory; shorter ones
-// not at all (their rows are loaded one by one, which the atom's address-based swizzle allows).
-constexpr int row_unit(int64_t N) { return N < 8 ? 1 : 8; }
+// not at all, and are loaded whole (the swizzle goes by address, so a box may begin at any row): their
+// tiles have whole frames, tile_rows of the rows that a tile could have.
+constexpr int row_unit(int64_t N) { return N < 8 ? static_cast<int>(N) : 8; }
+constexpr int tile_rows(int unit, int most) { return most / unit * unit; }
 
 // How a tile of rows is loaded: in one TMA box where its rows lie in one frame, else in boxes of
 // kBoxRows and of `unit` rows, listed in shared memory {first token, first row of the tile}: the
@@ -41,13 +43,13 @@ struct RowBoxes {
   int n_many, n_unit; // both 0: one box of the whole tile, from token tok
   int tok;
 };
-// Rows [r0, r0 + n) of R, r0 a multiple of the unit; with room for n / unit
+// Rows [r0, r0 + n) of R, r0 and n multiples of the unit, a whole tile's box of `box` >= n rows; with room for n / unit
 // boxes.  Warp-collective; the same in
 // every lane.  Rows past R are not loaded, except that a tile with none at all gets a box of zeros.
 template <int CAP>
-__device__ __forceinline__ RowBoxes list_boxes(const RowMap& m, int R, int r0, int n,
+__device__ __forceinline__ RowBoxes list_boxes(const RowMap& m, int R, int r0, int n, int box,
                                                BoxList<CAP>& list) {
-  RowBoxes x{n, 0, 0, 0};
+  RowBoxes x{box, 0, 0, 0};
   const int lane = threadIdx.x & 31;
   const int end = min(r0 + n, R);
   const int a0 = m.by_Np.div(r0);
@@ -58,13 +60,12 @@ __device__ __forceinline__ RowBoxes list_boxes(const RowMap& m, int R, int r0, i
   }
   x.rows = end - r0;
   __syncwarp();  // the list's last use is over
-  if (m.unit == 1) {
-    x.n_unit = x.rows;
+  if (m.unit < 8) {  // frames of `unit` tokens
+    x.n_unit = x.rows / m.unit;
 #pragma unroll 1
-    for (int i = lane; i < x.rows; i += 32) {
-      const int r = r0 + i, a = m.by_Np.div(r);
-      list.tok[CAP - 1 - i] = m.frame(a) * m.N + (r - a * m.Np);
-      list.row[CAP - 1 - i] = static_cast<uint8_t>(i);
+    for (int i = lane; i < x.n_unit; i += 32) {
+      list.tok[CAP - 1 - i] = m.frame(a0 + i) * m.N;
+      list.row[CAP - 1 - i] = static_cast<uint8_t>(i * m.unit);
     }
   } else {
 #pragma unroll 1
@@ -91,9 +92,9 @@ __device__ __forceinline__ RowBoxes list_boxes(const RowMap& m, int R, int r0, i
   return x;
 }
 // list_boxes(...).rows, without the list.
-__device__ __forceinline__ int boxed_rows(const RowMap& m, int R, int r0, int n) {
+__device__ __forceinline__ int boxed_rows(const RowMap& m, int R, int r0, int n, int box) {
   const int end = min(r0 + n, R);
-  return r0 >= R || m.by_Np.div(r0) == m.by_Np.div(end - 1) ? n : end - r0;
+  return r0 >= R || m.by_Np.div(r0) == m.by_Np.div(end - 1) ? box : end - r0;
 }
 
 }  // namespace rf

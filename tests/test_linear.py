@@ -31,6 +31,8 @@ SHAPES = [
     (3, 1560, (0, 2), 200, 2500),
     (2, 40, (), 64, 64),                 # nothing active
     (300, 2, tuple(range(0, 300, 3)), 64, 1600),
+    (300, 5, tuple(range(1, 300, 2)), 72, 3000),  # pairs of CTAs on frames of five tokens
+    (40, 7, tuple(range(40)), 520, 300),          # tiles of whole frames of seven tokens
 ]
 OPTIONS = [  # bias, act, gate, residual, out32
     (False, None, None, False, False),
