@@ -41,6 +41,7 @@ struct Epilogue {
   int act, in_dtype, out_dtype;
   int n_out;
   int vec;              // Y and R rows, bias and gate can be moved in 16-byte vectors
+  int vec_cols;         // bias and gate alone
 };
 
 __device__ __forceinline__ float ex2_neg_log2e(float x) { return ex2_approx(-1.4426950408889634f * x); }
@@ -145,21 +146,28 @@ __device__ __forceinline__ void finish4(const Epilogue& e, int64_t token, int fr
   }
 }
 
-// Columns n .. n + 31 of a row, element by element: the last columns of a result, and rows off the
-// 16-byte boundaries.
-static __device__ __noinline__ void finish_row(const Epilogue& e, int64_t token, int frame, int n,
-                                           float (&v)[32]) {
+// 32 columns from n, element by element: bias, activation, gate.  Out of line: the last columns of a
+// result, and bias or gate rows off the 16-byte boundaries.
+static __device__ __noinline__ void finish_cols_each(const Epilogue& e, int frame, int n, float (&v)[32]) {
+  const int mine = n + (threadIdx.x & 31);  // a column per lane, then handed round
+  if (e.bias) {
+    const float b = mine < e.n_out ? load_elem(e.bias, mine, e.in_dtype) : 0.f;
 #pragma unroll
-  for (int i = 0; i < 32; ++i)
-    if (n + i < e.n_out && e.bias) v[i] += load_elem(e.bias, n + i, e.in_dtype);
+    for (int i = 0; i < 32; ++i) v[i] += __shfl_sync(0xffffffffu, b, i);
+  }
   activate(e.act, v);
+  if (e.gate) {
+    const int frame0 = __shfl_sync(0xffffffffu, frame, 0);
+    if (__all_sync(0xffffffffu, frame == frame0)) {
+      const float g = mine < e.n_out ? e.gate[frame0 * e.gate_stride + mine] : 0.f;
 #pragma unroll
-  for (int i = 0; i < 32; ++i)
-    if (n + i < e.n_out) {
-      if (e.gate) v[i] *= e.gate[frame * e.gate_stride + n + i];
-      if (e.R) v[i] += load_elem(e.R, token * e.r_stride + n + i, e.out_dtype);
-      store_elem(e.Y, token * e.y_stride + n + i, e.out_dtype, v[i]);
+      for (int i = 0; i < 32; ++i) v[i] *= __shfl_sync(0xffffffffu, g, i);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (n + i < e.n_out) v[i] *= e.gate[frame * e.gate_stride + n + i];
     }
+  }
 }
 
 // 32 columns from n: bias, activation, gate.
@@ -205,43 +213,42 @@ __device__ __forceinline__ bool finish_tile(const Epilogue& e, const CUtensorMap
   char* Y = static_cast<char*>(e.Y) + static_cast<int64_t>(n0) * kBytes;
   const char* R = static_cast<const char*>(e.R) + static_cast<int64_t>(n0) * kBytes;
   const int lane = threadIdx.x & 31;
-  auto whole = [&](int c) { return e.vec && n0 + (c + 1) * kCols <= e.n_out; };
-  // 32 consecutive tokens leave through TMA, in the background
-  const bool bulk = span_y.regular && span_y.n == 32;
-  const int token0 = __shfl_sync(0xffffffffu, static_cast<int>(token), 0);
   auto stage_free = [&]() {
     if (lane == 0) bulk_wait_read();
     __syncwarp();
   };
-  if (e.R && chunks > 0 && whole(0)) {
+  auto in_full = [&](int c) { return n0 + (c + 1) * kCols <= e.n_out; };
+  auto whole = [&](int c) { return e.vec && in_full(c); };
+  auto fetch = [&](int c) {  // the residual's rows, ahead of their use
     stage_free();
-    fetch_rows(stage, R, span_r, r_bytes);
-  }
+    if (whole(c)) fetch_rows(stage, R + c * 128, span_r, r_bytes);
+    else fetch_elems<kBytes>(stage, R + c * 128, span_r.at, e.n_out - n0 - c * kCols);
+  };
+  // 32 consecutive tokens leave through TMA, in the background
+  const bool bulk = span_y.regular && span_y.n == 32;
+  const int token0 = __shfl_sync(0xffffffffu, static_cast<int>(token), 0);
+  if (e.R && chunks > 0) fetch(0);
   if (!ready()) return false;
   if (chunks == 0) read();
 #pragma unroll 1
   for (int c = 0; c < chunks; ++c) {
     const int n = n0 + c * kCols;
-    if (!whole(c)) {
-#pragma unroll 1
-      for (int half = 0; half < kCols; half += 32) {
-        uint32_t v[32];
-        tmem_ld32(acc + c * kCols + half, v);
-        tmem_wait_ld();
-        if (token >= 0 && n + half < e.n_out)
-          finish_row(e, token, frame, n + half, *reinterpret_cast<float(*)[32]>(&v));
-        __syncwarp();
-      }
-      if (c == chunks - 1) read();
-      continue;
-    }
 #pragma unroll 1
     for (int half = 0; half < kCols / 32; ++half) {
       float v[32];
       tmem_ld32(acc + c * kCols + half * 32, reinterpret_cast<uint32_t(&)[32]>(v));
       tmem_wait_ld();
       if (half == kCols / 32 - 1 && c == chunks - 1) read();
-      finish_cols(e, frame, n + half * 32, v);
+      if (e.vec_cols && in_full(c)) {
+        finish_cols(e, frame, n + half * 32, v);
+      } else {
+        float t[32];  // its address is taken: v stays in registers
+#pragma unroll
+        for (int i = 0; i < 32; ++i) t[i] = v[i];
+        finish_cols_each(e, frame, n + half * 32, t);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] = t[i];
+      }
       if (half == 0) {
         if (e.R) await_rows();
         else stage_free();
@@ -278,7 +285,9 @@ __device__ __forceinline__ bool finish_tile(const Epilogue& e, const CUtensorMap
         }
       }
     }
-    if (bulk) {
+    if (!whole(c)) {
+      store_elems<kBytes>(stage, Y + c * 128, span_y.at, e.n_out - n);
+    } else if (bulk) {
       fence_proxy_async();
       __syncwarp();
       if (lane == 0) {
@@ -288,10 +297,7 @@ __device__ __forceinline__ bool finish_tile(const Epilogue& e, const CUtensorMap
     } else {
       store_rows(stage, Y + c * 128, span_y, y_bytes);
     }
-    if (e.R && c + 1 < chunks && whole(c + 1)) {
-      stage_free();
-      fetch_rows(stage, R + (c + 1) * 128, span_r, r_bytes);
-    }
+    if (e.R && c + 1 < chunks) fetch(c + 1);
   }
   return true;
 }
@@ -316,8 +322,9 @@ __device__ __forceinline__ int row_token(const LinearParams& p, int r, int& fram
   const int a = p.rows.by_Np.div(r), q = r - a * p.rows.Np;
   const int f = p.rows.frame(a);
   const int token = f * p.rows.N + q;
-  frame = p.by_N.div(token);
-  return q < p.rows.N ? token : -1;
+  const bool valid = q < p.rows.N;
+  frame = valid ? p.by_N.div(token) : 0;  // the padding behind the last frame is in none
+  return valid ? token : -1;
 }
 
 // The maps of X: boxes of a whole tile, of kBoxRows rows and of rows.unit rows.
@@ -945,9 +952,9 @@ extern "C" rf_status rf_linear(void* d_Y, int64_t y_row_stride, int out_dtype, c
   e.in_dtype = dtype;
   e.out_dtype = out_dtype;
   e.n_out = d_out;
-  e.vec = aligned16(d_Y) && y_row_stride * es_out % 16 == 0 &&
-          (!d_R || (aligned16(d_R) && r_row_stride * es_out % 16 == 0)) && aligned16(d_bias) &&
-          (!d_gate || (aligned16(d_gate) && gate_frame_stride % 4 == 0));
+  e.vec_cols = aligned16(d_bias) && (!d_gate || (aligned16(d_gate) && gate_frame_stride % 4 == 0));
+  e.vec = e.vec_cols && aligned16(d_Y) && y_row_stride * es_out % 16 == 0 &&
+          (!d_R || (aligned16(d_R) && r_row_stride * es_out % 16 == 0));
   p.by_N = FastDiv(static_cast<uint32_t>(N));
   p.kblocks = (d_in + kBlockK - 1) / kBlockK;
   p.fp16 = dtype == RF_FP16;

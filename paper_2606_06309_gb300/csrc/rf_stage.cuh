@@ -13,6 +13,15 @@
 
 namespace rf {
 
+template <int BYTES>
+struct ElemBits {
+  using type = uint16_t;
+};
+template <>
+struct ElemBits<4> {
+  using type = uint32_t;
+};
+
 constexpr int kTurnBytes = 4096;  // per warp: 32 rows of 128 bytes, 16-byte pieces swizzled by row (TMA's 128-byte swizzle)
 
 __device__ __forceinline__ uint4& stage_at(uint4* stage, int row, int piece) {
@@ -83,6 +92,65 @@ __device__ __forceinline__ void fetch_rows(uint4* stage, const char* base, const
 }
 __device__ __forceinline__ void await_rows() {
   asm volatile("cp.async.wait_all;" ::: "memory");
+  __syncwarp();
+}
+
+// The same element by element, for rows off the 16-byte boundaries and columns that end within the
+// 128 bytes: the first `cols` elements of BYTES (2 or 4) each.  A warp's accesses are of consecutive
+// elements of a row; pairs of 16-bit ones are stored together where the row is on their boundary.
+template <int BYTES>
+__device__ __forceinline__ char* stage_elem(uint4* stage, int row, int col) {
+  const int byte = col * BYTES;
+  return reinterpret_cast<char*>(&stage_at(stage, row, byte >> 4)) + (byte & 15);
+}
+template <int BYTES>
+static __device__ __noinline__ void store_elems(uint4* stage, char* base, int64_t at, int cols) {
+  const int lane = threadIdx.x & 31;
+  __syncwarp();
+#pragma unroll 4
+  for (int r = 0; r < 32; ++r) {
+    const int64_t o = shfl64(at, r);
+    if (o < 0) continue;
+    char* row = base + o;
+    if (BYTES == 4) {
+      if (lane < cols)
+        *reinterpret_cast<uint32_t*>(row + 4 * lane) =
+            *reinterpret_cast<const uint32_t*>(stage_elem<4>(stage, r, lane));
+    } else if ((reinterpret_cast<uintptr_t>(row) & 3) == 0) {
+      const uint32_t two = *reinterpret_cast<const uint32_t*>(stage_elem<2>(stage, r, 2 * lane));
+      if (2 * lane + 1 < cols) *reinterpret_cast<uint32_t*>(row + 4 * lane) = two;
+      else if (2 * lane < cols) *reinterpret_cast<uint16_t*>(row + 4 * lane) = static_cast<uint16_t>(two);
+    } else {
+#pragma unroll
+      for (int c = lane; c < 64; c += 32)
+        if (c < cols)
+          *reinterpret_cast<uint16_t*>(row + 2 * c) =
+              *reinterpret_cast<const uint16_t*>(stage_elem<2>(stage, r, c));
+    }
+  }
+  __syncwarp();
+}
+template <int BYTES>
+static __device__ __noinline__ void fetch_elems(uint4* stage, const char* base, int64_t at, int cols) {
+  const int lane = threadIdx.x & 31;
+  using T = typename ElemBits<BYTES>::type;
+#pragma unroll 1
+  for (int r0 = 0; r0 < 32; r0 += 4) {
+    T v[4][4 / BYTES];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int64_t o = shfl64(at, r0 + k);
+#pragma unroll
+      for (int i = 0; i < 4 / BYTES; ++i)
+        v[k][i] = o >= 0 && lane + 32 * i < cols
+                      ? reinterpret_cast<const T*>(base + o)[lane + 32 * i] : T(0);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int i = 0; i < 4 / BYTES; ++i)
+        *reinterpret_cast<T*>(stage_elem<BYTES>(stage, r0 + k, lane + 32 * i)) = v[k][i];
+  }
   __syncwarp();
 }
 

@@ -29,6 +29,7 @@ SHAPES = [
     (3, 700, (0, 2), 192, 1536),         # more rows than a tile
     (6, 1003, (0, 1, 2, 4, 5), 77, 3000),  # many tiles: pairs of CTAs, K within one block
     (3, 1560, (0, 2), 200, 2500),
+    (4, 1100, (0, 1, 3), 72, 2501),      # many tiles, rows of results off every vector's boundary
     (2, 40, (), 64, 64),                 # nothing active
     (300, 2, tuple(range(0, 300, 3)), 64, 1600),
     (300, 5, tuple(range(1, 300, 2)), 72, 3000),  # pairs of CTAs on frames of five tokens
@@ -96,7 +97,9 @@ def test_linear_matches_oracle(cuda_lib, shape, option, dtype):
     X, W, b, ga, R = _inputs(F, N, K, O, dt, out, 7 + shape, bias, gate, residual,
                              pad=3 if option == 3 else 8)
     act_l, cnt = lists(frames, F, N)
-    Y = torch.full((F * N, _pad(O)), SENTINEL, dtype=out, device=DEV)
+    # options 1 and 4: result rows off the 16-byte boundaries (1: of an odd number of elements)
+    ld = {1: O | 1, 4: O + 2 + O % 2}.get(option, _pad(O))
+    Y = torch.full((F * N, ld), SENTINEL, dtype=out, device=DEV)
     st = torch.zeros(1, dtype=torch.int32, device=DEV)
     rf.rf_linear(Y[:, :O], X, W, F, N, bias=b, act=act, gate=ga, residual=R, active=act_l,
                  counts=cnt, status=st)
