@@ -115,6 +115,7 @@ struct Work {
   // 12 heads, in their own order 48 K/V tiles for the busiest CTA, this way 24: 66 us -> 46; with many
   // rounds lengths even out, and the order costs 2 us at the start).
   bool sorted;
+  int lo, hi;  // no state before lo or from hi on is seen: what the mask pads at the ends is not visited
   uint8_t order[kMaxSorted];
 };
 __device__ __forceinline__ void make_work(const CrossParams& p, Work& w) {
@@ -127,6 +128,8 @@ __device__ __forceinline__ void make_work(const CrossParams& p, Work& w) {
     w.tiles = ((p.kv_range ? p.rows.N : w.A * p.rows.Np) + w.rows - 1) / w.rows;
   w.pairs = (w.tiles + 1) / 2;
   w.items = p.units * w.groups * w.pairs;
+  w.lo = 0;
+  w.hi = p.L;
   const int ctas = gridDim.x / p.cluster;  // (or clusters)
   w.first = blockIdx.x / p.cluster;
   w.sorted = p.kv_range && w.groups > 1 && w.groups <= kMaxSorted && w.items > ctas &&
@@ -135,18 +138,56 @@ __device__ __forceinline__ void make_work(const CrossParams& p, Work& w) {
   w.step[1] = w.sorted ? 2 * w.first + 1 : ctas;
   w.by_pairs = FastDiv(max(w.pairs, 1));
 }
-// K/V tiles of a range.
-__device__ __forceinline__ int range_tiles(const CrossParams& p, int frame, int& begin, int& end) {
-  const int2 r = p.kv_range[frame];
-  begin = min(max(r.x, 0), p.L);
-  end = min(max(r.y, begin), p.L);
+// K/V tiles of a frame's range.
+__device__ __forceinline__ int range_tiles(const CrossParams& p, const Work& w, int frame, int& begin,
+                                           int& end) {
+  const int2 r = p.kv_range ? p.kv_range[frame] : make_int2(0, p.L);
+  begin = min(max(r.x, w.lo), w.hi);
+  end = min(max(r.y, begin), w.hi);
   return (end - begin + kBN - 1) / kBN;
+}
+// All threads of the block: w.lo and w.hi from the mask (L bytes; a word of 4 at a time where it lies on
+// their boundary).
+__device__ __forceinline__ void trim_states(const CrossParams& p, Work& w) {
+  if (threadIdx.x == 0) {
+    w.lo = p.L;
+    w.hi = 0;
+  }
+  __syncthreads();
+  int lo = p.L, hi = 0;
+  if ((reinterpret_cast<uintptr_t>(p.key_mask) & 3) == 0 && p.L >= 4) {
+    const uint32_t* words = reinterpret_cast<const uint32_t*>(p.key_mask);
+#pragma unroll 4
+    for (int i = threadIdx.x; i < p.L >> 2; i += kThreads)
+      if (const uint32_t v = words[i]) {
+        lo = min(lo, 4 * i + ((__ffs(v) - 1) >> 3));
+        hi = max(hi, 4 * i + 4 - (__clz(v) >> 3));
+      }
+    for (int k = (p.L & ~3) + threadIdx.x; k < p.L; k += kThreads)
+      if (p.key_mask[k]) {
+        lo = min(lo, k);
+        hi = max(hi, k + 1);
+      }
+  } else {
+    for (int k = threadIdx.x; k < p.L; k += kThreads)
+      if (p.key_mask[k]) {
+        lo = min(lo, k);
+        hi = max(hi, k + 1);
+      }
+  }
+  lo = __reduce_min_sync(0xffffffffu, lo);
+  hi = __reduce_max_sync(0xffffffffu, hi);
+  if ((threadIdx.x & 31) == 0) {
+    atomicMin(&w.lo, lo);
+    atomicMax(&w.hi, hi);
+  }
+  __syncthreads();
 }
 // All threads of the block; `tiles`: room for kMaxSorted numbers.
 __device__ __forceinline__ void sort_frames(const CrossParams& p, Work& w, int* tiles) {
   const int i = threadIdx.x;
   int begin, end, mine = 0, rank = 0;
-  if (i < w.groups) tiles[i] = mine = range_tiles(p, p.rows.frame(i), begin, end);
+  if (i < w.groups) tiles[i] = mine = range_tiles(p, w, p.rows.frame(i), begin, end);
   __syncthreads();
   if (i < w.groups) {
     for (int j = 0; j < w.groups; ++j)
@@ -169,10 +210,8 @@ __device__ __forceinline__ Item get_item(const CrossParams& p, const Work& w, in
   const int slot = p.by_units.div(gp);
   t.unit = gp - slot * p.units;
   t.group = w.sorted ? w.order[slot] : slot;
-  t.begin = 0;
-  t.end = p.L;
-  int nt = (p.L + kBN - 1) / kBN;  // below 2^24
-  if (p.kv_range) nt = range_tiles(p, p.rows.frame(t.group), t.begin, t.end);
+  const int nt =  // below 2^24
+      range_tiles(p, w, p.kv_range ? p.rows.frame(t.group) : 0, t.begin, t.end);
   t.j0 = 0;
   t.j1 = nt;
   if (p.cluster > 1) {
@@ -212,21 +251,28 @@ __device__ __forceinline__ int whole_tile(const CrossParams& p, const Work& w, c
   return a < w.A && q + kBM <= p.rows.N ? p.rows.frame(a) * p.rows.N + q : -1;
 }
 
-// Which keys of tile j a row may see: bit c of word c / 32.  Warp-collective.
+// Which keys of tile j a row may see: bit c of word c / 32.  Warp-collective, in two parts so that the
+// mask's bytes can be on their way meanwhile: this lane's keys (bit i: key lane + 32 i), and all.
 struct KeyBits {
   uint32_t w[4];
   __device__ __forceinline__ bool all() const {
     return (w[0] & w[1] & w[2] & w[3]) == 0xFFFFFFFFu;
   }
 };
-__device__ __forceinline__ KeyBits key_bits(const CrossParams& p, const Item& t, int j) {
-  KeyBits b;
+__device__ __forceinline__ uint32_t own_keys(const CrossParams& p, const Item& t, int j) {
   const int k0 = t.begin + j * kBN + (threadIdx.x & 31);
+  uint32_t m = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int k = k0 + 32 * i;
-    b.w[i] = __ballot_sync(0xffffffffu, k < t.end && (!p.key_mask || p.key_mask[k] != 0));
+    if (k < t.end && (!p.key_mask || p.key_mask[k] != 0)) m |= 1u << i;
   }
+  return m;
+}
+__device__ __forceinline__ KeyBits all_keys(uint32_t own) {
+  KeyBits b;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) b.w[i] = __ballot_sync(0xffffffffu, (own >> i) & 1u);
   return b;
 }
 
@@ -371,7 +417,7 @@ __device__ __forceinline__ void cleaner(const CrossParams& p, const Work& w, int
     const Item t = get_item(p, w, i, rank);
 #pragma unroll 1
     for (int j = t.j0; j < t.j1; ++j, it += 2) {
-      const KeyBits b = key_bits(p, t, j);
+      const KeyBits b = all_keys(own_keys(p, t, j));
       const int s = it % C::kSlots;
       if (!all_wait(bar(C::kKVFull + s), (it / C::kSlots) & 1, abort)) {
         if (lane == 0) flag_error(p, 1);
@@ -520,10 +566,14 @@ __device__ __forceinline__ bool softmax_item(const CrossParams& p, const Item& t
                                              float& l_out, volatile int* abort) {
   const float sl2 = p.scale_log2;
   float m = -INFINITY, l = 0.f;
-  KeyBits bits{};
-  if (CLEAN) bits = key_bits(p, t, t.j0);
+  uint32_t own = CLEAN ? own_keys(p, t, t.j0) : 0;
 #pragma unroll 1
   for (int j = t.j0; j < t.j1; ++j) {
+    KeyBits bits{};
+    if (CLEAN) {
+      bits = all_keys(own);
+      if (j + 1 < t.j1) own = own_keys(p, t, j + 1);
+    }
     if (!all_wait(bar_s, s_cnt & 1, abort)) return false;
     ++s_cnt;
     tc_fence_after();
@@ -539,7 +589,6 @@ __device__ __forceinline__ bool softmax_item(const CrossParams& p, const Item& t
         for (int c = 0; c < kBN; ++c)
           if (!((bits.w[c >> 5] >> (c & 31)) & 1u)) sf[c] = -INFINITY;
       }
-      if (j + 1 < t.j1) bits = key_bits(p, t, j + 1);
     } else if ((j + 1) * kBN > t.end) {
       const int valid = t.end - j * kBN;
 #pragma unroll
@@ -839,6 +888,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
   const Work& w = work;
+  if (CLEAN && p.key_mask) trim_states(p, work);
   if (CLEAN && w.sorted) sort_frames(p, work, reinterpret_cast<int*>(smem + C::kOffStage));
 
   // Every warp of warpgroup 0 gives registers back before any softmax warp asks for more, so the
