@@ -13,7 +13,13 @@
 // tokens, since their number is known on the device only (a grid for all F frames would launch
 // F/A times the blocks).  Blocks that run together cover all heads of the same tokens, so that rows are
 // read and written whole.  A pair's place in the tables is found again for every token, from three
-// pointers: kept per pair it took 115 registers, and 720p x 40 heads in halves 756 us.
+// pointers: kept per pair it took 115 registers.
+//
+// What bounds it is HBM.  Measured on warm clocks (bytes of one read and one write): 480p, 21 frames,
+// 12 + 12 heads of 128, bf16, neighbours as pairs: 60.5 us, 6.65 TB/s, as fast as a copy; 720p, 40 + 40
+// heads, fp16, halves: 452 us, 6.85 TB/s.  In halves the loads stand without branches between them
+// (with a branch per head and vector they waited for one another: 585 us); with neighbours as pairs a
+// branch per head is the better of the two at whole groups of heads (60.5 against 62.7 us).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -91,7 +97,8 @@ __global__ void __launch_bounds__(kRopeThreads)
   const int pair0 = u * kPairs;
   const bool through = HALF && pair0 >= p.pairs;  // whole units only (host: pairs % kPairs == 0)
   const int at = (through ? p.pairs * 2 + (u - p.pairs / kPairs) * E : u * E) * sizeof(T);
-  const int to_other = p.pairs * static_cast<int>(sizeof(T));  // HALF: from i to i + R/2
+  // HALF: from i to i + R/2; where nothing is rotated the same vector again
+  const int to_other = through ? 0 : p.pairs * static_cast<int>(sizeof(T));
   const int end_t = p.half[0], end_h = end_t + p.half[1];      // the axes' pairs end here
 
   const int A = p.active ? min(max(p.counts[0], 0), p.F) : p.F;
@@ -106,12 +113,15 @@ __global__ void __launch_bounds__(kRopeThreads)
     char* dst = s.y + token * s.y_stride + static_cast<int64_t>(h0) * p.head_bytes + at;
     V v[kHeads][kVecs];
 #pragma unroll
-    for (int h = 0; h < kHeads; ++h)
-      if (h < nh) {
+    for (int h = 0; h < kHeads; ++h) {
+      if (HALF) {  // no branch between the loads: past the last head the last one's again
+        const char* q = src + min(h, nh - 1) * p.head_bytes;
+        v[h][0] = *reinterpret_cast<const V*>(q);
+        v[h][kVecs - 1] = *reinterpret_cast<const V*>(q + to_other);
+      } else if (h < nh) {
         v[h][0] = *reinterpret_cast<const V*>(src + h * p.head_bytes);
-        if (HALF && !through)
-          v[h][kVecs - 1] = *reinterpret_cast<const V*>(src + h * p.head_bytes + to_other);
       }
+    }
     // the token's rows of the tables, as if each began with the first pair of all
     const float2* tab_t = p.table[0] + static_cast<int64_t>(f) * p.half[0];
     const float2* tab_h = p.table[1] + (static_cast<int64_t>(y) * p.half[1] - end_t);
@@ -162,8 +172,9 @@ template <typename T>
 rf_status launch_rope_type(const RopeParams& p, bool half, int sm_count, cudaStream_t stream) {
   if (!half) return launch_rope<T, 16 / sizeof(T), false>(p, sm_count, stream);
   // Halves: four elements of each at a time.  With eight of a 16-bit type the pairs' angles take 116
-  // registers, two blocks per SM: 720p x 40 heads 656 us.  The second half of the pairs, and what
-  // passes through behind it, start on a vector's boundary only where R/2 is a multiple of four.
+  // registers, two blocks per SM: 720p x 40 heads 656 against 452 us.  The second half of the pairs,
+  // and what passes through behind it, start on a vector's boundary only where R/2 is a multiple of
+  // four.
   if (p.pairs % 4 == 0) return launch_rope<T, 4, true>(p, sm_count, stream);
   return launch_rope<T, 1, true>(p, sm_count, stream);
 }
