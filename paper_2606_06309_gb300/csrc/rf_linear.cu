@@ -7,9 +7,18 @@
 // leaves tensor memory, so Y is rounded once and nothing between them goes to memory.
 //
 // Two kernels, both fed by TMA from 128-byte-swizzled tiles of 64 columns of K:
-//   pair_kernel  many rows: a pair of CTAs on one tile of 256 tokens x BN columns (cta_group::2).
-//   split_kernel few rows: 128 columns of W against all the rows of a launch, W as the tensor
-//                core's M side, and K split over a cluster of CTAs.
+//   pair_kernel  many rows: a pair of CTAs on one tile of 256 tokens x 256 columns (cta_group::2).
+//   split_kernel few rows: 128 columns of W against 16 to 256 tokens, W as the tensor core's M
+//                side, and K split over a cluster of CTAs.
+//
+// Measured (device time, calls one after another):
+//   75,600 rows 5120 -> 5120, residual and gate: bounded by the tensor cores, 1.84 PFLOP/s while
+//     the clock holds (2.16 ms; 2.57 ms, 1.54 PFLOP/s, when the power limit lowers it).
+//   6,240 of 20,280 rows 1536 -> 6144, bias and GELU: 84 us, 1.40 PFLOP/s: 600 tiles are 7.9 for
+//     each of the 76 pairs, and the activation of a tile takes most of its products' 6,100 cycles.
+//   1 row 1536 -> 9216: 9.4 us, of which reading W's 28 MB takes 4.2: launch, tensor memory,
+//     barriers and one cluster's exchange are the rest.
+//   333 rows 1000 -> 777: 10.8 us, the same fixed costs.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -44,7 +53,9 @@ struct Epilogue {
   int vec_cols;         // bias and gate alone
 };
 
-__device__ __forceinline__ float ex2_neg_log2e(float x) { return ex2_approx(-1.4426950408889634f * x); }
+__device__ __forceinline__ float ex2_neg_log2e(float x) {
+  return ex2_approx(-1.4426950408889634f * x);
+}
 // x * sigmoid(s): 1 + e^-s overflows to infinity for very negative s, and the quotient is then 0
 __device__ __forceinline__ float times_sigmoid(float x, float s) {
   return __fdividef(x, 1.f + ex2_neg_log2e(s));
@@ -98,7 +109,8 @@ __device__ __forceinline__ void add2(uint32_t w, int dtype, float& lo, float& hi
   hi += b;
 }
 
-// Gate, residual and store of four columns of a row: VEC: from n on, as vectors; otherwise n, n + 32, ...
+// Gate, residual and store of four columns of a row.  VEC: from n on, as vectors; otherwise n,
+// n + 32, ...
 template <bool VEC>
 __device__ __forceinline__ void finish4(const Epilogue& e, int64_t token, int frame, int n, float* v) {
   constexpr int kApart = VEC ? 1 : 32;
@@ -146,8 +158,8 @@ __device__ __forceinline__ void finish4(const Epilogue& e, int64_t token, int fr
   }
 }
 
-// 32 columns from n, element by element: bias, activation, gate.  Out of line: the last columns of a
-// result, and bias or gate rows off the 16-byte boundaries.
+// 32 columns from n, element by element: bias, activation, gate.  Out of line: the last columns of
+// a result, and bias or gate rows off the 16-byte boundaries.
 static __device__ __noinline__ void finish_cols_each(const Epilogue& e, int frame, int n, float (&v)[32]) {
   const int mine = n + (threadIdx.x & 31);  // a column per lane, then handed round
   if (e.bias) {
@@ -197,14 +209,14 @@ __device__ __forceinline__ void finish_cols(const Epilogue& e, int frame, int n,
   }
 }
 
-// A warp's 32 rows of an accumulator (tensor memory columns from `acc`; a row per lane, its token or
-// -1), columns n0 .. n0 + cols - 1 of the result, 128 bytes of them at a time through the
-// warp's stage.  ready() is called when the residual's first loads are in flight and the
-// accumulator is wanted, read() when it has been read; false from ready() ends it.
+// A warp's 32 rows of an accumulator (tensor memory columns from `acc`; a row per lane, its token
+// or -1), columns n0 .. n0 + cols - 1 of the result, 128 bytes of them at a time through the warp's
+// stage.  ready() is called when the residual's first loads are in flight and the accumulator is
+// wanted, read() when it has been read; false from ready() ends it.
 template <bool OUT32, typename Ready, typename Read>
-__device__ __forceinline__ bool finish_tile(const Epilogue& e, const CUtensorMap* tmY, uint4* stage, uint32_t acc, int n0,
-                                            int cols, int64_t token, int frame, Ready&& ready,
-                                            Read&& read) {
+__device__ __forceinline__ bool finish_tile(const Epilogue& e, const CUtensorMap* tmY,
+                                            uint4* stage, uint32_t acc, int n0, int cols,
+                                            int64_t token, int frame, Ready&& ready, Read&& read) {
   constexpr int kCols = OUT32 ? 32 : 64, kBytes = OUT32 ? 4 : 2;
   const int chunks = (min(cols, max(e.n_out - n0, 0)) + kCols - 1) / kCols;
   const int64_t y_bytes = e.y_stride * kBytes, r_bytes = e.r_stride * kBytes;
@@ -355,17 +367,17 @@ __device__ __forceinline__ void load_rows(const RowBoxes& x, const BoxList<CAP>&
 // ---------------------------------------------------------------------------------------
 // Many rows: pairs of CTAs
 // ---------------------------------------------------------------------------------------
-// A pair's tile is 256 tokens x BN columns: each CTA holds 128 token rows of X, half of the tile's
+// A pair's tile is 256 tokens x kBN columns: each CTA holds 128 token rows of X, half of the tile's
 // rows of W, and the accumulators of its 128 rows; the tensor cores of both read both halves of W.
 // That is what the pair is for: a CTA alone on 128 x 256 would have to bring 48 KB into shared
 // memory per 64 columns of K, in a pair it brings 32 KB.
 // Two accumulators in tensor memory: the epilogue of a tile runs during the products of the next.
 constexpr int kPairThreads = 384;  // warps 0, 3 TMA, 1 MMA (first CTA), 2 tensor memory, 4-11 epilogue
 constexpr int kEpiWarps = 8;
+constexpr int kBN = 256;
 
-template <int BN>
 struct PairCfg {
-  static constexpr int kABytes = 128 * 128, kBBytes = BN / 2 * 128;
+  static constexpr int kABytes = 128 * 128, kBBytes = kBN / 2 * 128;
   static constexpr int kStageBytes = kABytes + kBBytes;
   static constexpr int kStages = 196608 / kStageBytes;
   static constexpr int kBarFull = 0, kBarEmpty = kStages, kBarAccFull = 2 * kStages,
@@ -375,7 +387,7 @@ struct PairCfg {
   static constexpr int kOffMisc = kOffBar + kBars * 8;
   static constexpr int kOffList = kOffMisc + 16;
   static constexpr int kSmem = kOffList + 2 * static_cast<int>(sizeof(BoxList<128>)) + 1024;
-  static constexpr uint32_t kTmemCols = 2 * BN;
+  static constexpr uint32_t kTmemCols = 2 * kBN;
 };
 
 // Tiles in groups of eight rows of tiles, column by column within a group, so that the pairs at
@@ -389,12 +401,11 @@ __device__ __forceinline__ void tile_at(int t, int m_tiles, int n_tiles, int& m,
   m = g * kGroupM + (i - n * width);
 }
 
-template <int BN>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
     pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmMany,
                 const __grid_constant__ CUtensorMap tmUnit, const __grid_constant__ CUtensorMap tmW,
                 const __grid_constant__ CUtensorMap tmY, const LinearParams p) {
-  using C = PairCfg<BN>;
+  using C = PairCfg;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t sbase = (raw + 1023u) & ~1023u;
@@ -449,7 +460,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
       int m, n;
       tile_at(t, m_tiles, p.n_tiles, m, n);
       const RowBoxes x = list_boxes(p.rows, R, (2 * m + rank) * half, half, 128, list);
-      const int w0 = n * BN + rank * (BN / 2);
+      const int w0 = n * kBN + rank * (kBN / 2);
       // of both CTAs, the other one's rows included
       const int bytes = 2 * C::kBBytes +
                         (x.rows + (rank == 0 ? boxed_rows(p.rows, R, (2 * m + 1) * half, half, 128)
@@ -483,7 +494,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
   } else if (warp == 1) {
     if (rank == 0) {
       const bool lead = elect_one();
-      const uint32_t idesc = idesc_f16(p.fp16, 256, BN, 0);
+      const uint32_t idesc = idesc_f16(p.fp16, 256, kBN, 0);
       int it = 0, n_acc = 0;
       bool ok = true;
       for (int t = pair; ok && t < tiles; t += pairs, ++n_acc) {
@@ -493,7 +504,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
           break;
         }
         tc_fence_after();
-        const uint32_t acc = tmem + b * BN;
+        const uint32_t acc = tmem + b * kBN;
         for (int kb = 0; kb < p.kblocks; ++kb, ++it) {
           const int s = it % C::kStages;
           if (!warp_wait<true>(bar(C::kBarFull + s), (it / C::kStages) & 1, abort)) {
@@ -517,7 +528,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
       }
     }
   } else if (warp >= 4) {
-    const int quarter = warp & 3, part = (warp - 4) >> 2;  // lanes of tensor memory; half of BN
+    const int quarter = warp & 3, part = (warp - 4) >> 2;  // lanes of tensor memory; half of kBN
     const uint32_t lane_base = static_cast<uint32_t>(quarter * 32) << 16;
     uint4* stage = reinterpret_cast<uint4*>(smem + C::kOffStage + (warp - 4) * kTurnBytes);
     int n_acc = 0;
@@ -529,8 +540,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
       int frame = 0;
       const int token = row < half && r < R ? row_token(p, r, frame) : -1;
       auto ready = [&]() -> bool {
-        const bool ok = warp_wait<true>(bar(C::kBarAccFull + b),
-                                                                  (n_acc >> 1) & 1, abort);
+        const bool ok = warp_wait<true>(bar(C::kBarAccFull + b), (n_acc >> 1) & 1, abort);
         if (!ok && lane == 0) flag_error(p, 3);
         tc_fence_after();
         return ok;
@@ -540,11 +550,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
         __syncwarp();
         if (lane == 0) mbar_arrive_remote(map_to_rank(bar(C::kBarAccEmpty + b), 0));
       };
-      const uint32_t acc = tmem + lane_base + b * BN + part * (BN / 2);
-      const int n0 = n * BN + part * (BN / 2);
+      const uint32_t acc = tmem + lane_base + b * kBN + part * (kBN / 2);
+      const int n0 = n * kBN + part * (kBN / 2);
       if (!(p.epi.out_dtype == RF_FP32
-                ? finish_tile<true>(p.epi, &tmY, stage, acc, n0, BN / 2, token, frame, ready, read)
-                : finish_tile<false>(p.epi, &tmY, stage, acc, n0, BN / 2, token, frame, ready, read)))
+                ? finish_tile<true>(p.epi, &tmY, stage, acc, n0, kBN / 2, token, frame, ready, read)
+                : finish_tile<false>(p.epi, &tmY, stage, acc, n0, kBN / 2, token, frame, ready, read)))
         break;
     }
     if (lane == 0) bulk_wait_all();
@@ -577,9 +587,10 @@ constexpr int kSplitOffBar = kSplitRing, kSplitOffMisc = kSplitOffBar + kSplitBa
               kSplitOffTok = kSplitOffBoxes + 16, kSplitOffList = kSplitOffTok + 256 * 8,
               kSplitSmem = kSplitOffList + sizeof(BoxList<256>) + 1024;
 
-// Results of a CTA's share of a tile's tokens from the sums of all CTAs: a warp has kTok tokens at a time,
-// a lane four columns of each, with the loads of all of them in flight.  VEC: neighbouring columns, moved
-// as vectors; otherwise every 32nd, so that a warp's accesses are of consecutive elements either way.
+// Results of a CTA's share of a tile's tokens from the sums of all CTAs: a warp has kTok tokens at
+// a time, a lane four columns of each, with the loads of all of them in flight.  VEC: neighbouring
+// columns, moved as vectors; otherwise every 32nd, so that a warp's accesses are of consecutive
+// elements either way.
 template <bool VEC>
 __device__ __forceinline__ void finish_tokens(const Epilogue& e, const int2* tokens, uint32_t sums,
                                               int n0, int BT, int rows, int rank, int C) {
@@ -680,8 +691,8 @@ __global__ void __launch_bounds__(kSplitThreads, 1)
   const int kb0 = p.kblocks * rank / C, kb1 = p.kblocks * (rank + 1) / C;
 
   const RowBoxes x = *boxes;
-  // the boxes of a tile across frames are dealt to all warps but the MMA warp: one warp would take a
-  // hundred cycles for each (33 frames of one token, 1536 -> 6144: 29 us, this way 16)
+  // the boxes of a tile across frames are dealt to all warps but the MMA warp: one warp would take
+  // a hundred cycles for each (33 frames of one token, 1536 -> 6144: 29 us, this way 16)
   const int loaders = x.n_many + x.n_unit > 2 ? kSplitThreads / 32 - 1 : 1;
   const int who = warp == 0 ? 0 : warp - 1;
   if (warp != 1 && who < loaders) {
@@ -802,12 +813,13 @@ rf_status map_2d(CUtensorMap* m, int dtype, const void* base, int cols, int64_t 
   return make_tensor_map(m, dtype, base, 2, dims, strides, box);
 }
 
-// Tokens per tile and CTAs per cluster of a split launch: the pair with the least to do for the busiest
-// SM, in cycles.  Per 64 columns of K a CTA loads its tile of W and of X at about 50 bytes per cycle
-// (its products take 2 cycles per token, less); start and end cost about 5000, a cluster's start and its
-// two barriers 750 per CTA, and each four tokens of a warp one round trip per CTA of the cluster, 700 cycles and 150 for
-// every further CTA.  Clusters of 4 and 8 do not fill the GPCs: 36 and 15 of them run together.
-// (333 rows 1000 -> 777: 10.8 us in tiles of 16 tokens, 14.0 in tiles of 256 and clusters of eight.)
+// Tokens per tile and CTAs per cluster of a split launch: the pair with the least to do for the
+// busiest SM, in cycles.  Per 64 columns of K a CTA loads its tile of W and of X at about 50 bytes
+// per cycle (its products take 2 cycles per token, less); start and end cost about 5000, a
+// cluster's start and its two barriers 750 per CTA, and each four tokens of a warp one round trip
+// per CTA of the cluster, 700 cycles and 150 for every further CTA.  Clusters of 4 and 8 do not
+// fill the GPCs: 36 and 15 of them run together. (333 rows 1000 -> 777: 10.8 us in tiles of 16
+// tokens, 14.0 in tiles of 256 and clusters of eight.)
 struct SplitPlan {
   int tokens, cluster;
 };
@@ -837,8 +849,8 @@ SplitPlan split_plan(int64_t rows, int unit, int64_t n128, int kblocks, int sms)
 struct Maps {
   CUtensorMap x, many, unit, w, y;
 };
-// The maps of a launch with tiles of `tile` rows of X; w_rows rows of W per box.  Boxes of part of a
-// tile are made where a tile can lie across frames.
+// The maps of a launch with tiles of `tile` rows of X; w_rows rows of W per box.  Boxes of part of
+// a tile are made where a tile can lie across frames.
 rf_status make_maps(Maps* t, const LinearParams& p, const void* d_X, int64_t x_stride,
                     const void* d_W, int64_t w_stride, int d_in, int tile, int w_rows) {
   const int dt = p.epi.in_dtype;
@@ -851,31 +863,32 @@ rf_status make_maps(Maps* t, const LinearParams& p, const void* d_X, int64_t x_s
   return map_2d(&t->unit, dt, d_X, d_in, p.rows.T, x_stride, p.rows.unit);
 }
 
-template <int BN>
-rf_status launch_pair(const Maps& t, const LinearParams& p, int64_t tiles, const DeviceInfo& di, cudaStream_t s) {
+rf_status launch_pair(const Maps& t, const LinearParams& p, int64_t tiles, const DeviceInfo& di,
+                      cudaStream_t s) {
   static bool done[64] = {};
-  if (rf_status st = set_smem(pair_kernel<BN>, PairCfg<BN>::kSmem, di, done)) return st;
-  // pairs that run together: fewer than half the SMs where a GPC has an odd number of them, and
-  // one pair more would begin when the others have finished (480p keyframe-only step: 154 us)
+  if (rf_status st = set_smem(pair_kernel, PairCfg::kSmem, di, done)) return st;
+  // pairs that run together: where a GPC has an odd number of free SMs it is fewer than half of
+  // them, and a pair that waits for the others to finish would double the time
   static std::atomic<int> resident[64] = {};
   int most = resident[di.device].load(std::memory_order_relaxed);
   if (most == 0) {
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(static_cast<unsigned>(di.sm_count / 2 * 2));
     cfg.blockDim = dim3(kPairThreads);
-    cfg.dynamicSmemBytes = PairCfg<BN>::kSmem;
-    if (cudaError_t e = cudaOccupancyMaxActiveClusters(&most, pair_kernel<BN>, &cfg))
+    cfg.dynamicSmemBytes = PairCfg::kSmem;
+    if (cudaError_t e = cudaOccupancyMaxActiveClusters(&most, pair_kernel, &cfg))
       return fail(RF_ERR_CUDA, "cudaOccupancyMaxActiveClusters(rf_linear)", e);
     if (most < 1) return fail(RF_ERR_UNSUPPORTED, "rf_linear: no room for a pair of CTAs");
     resident[di.device].store(most, std::memory_order_relaxed);
   }
   const int64_t pairs = std::min<int64_t>(tiles, most);
-  pair_kernel<BN><<<static_cast<unsigned>(2 * pairs), kPairThreads, PairCfg<BN>::kSmem, s>>>(
+  pair_kernel<<<static_cast<unsigned>(2 * pairs), kPairThreads, PairCfg::kSmem, s>>>(
       t.x, t.many, t.unit, t.w, t.y, p);
   return launch_status("rf_linear pair_kernel launch");
 }
 
-rf_status launch_split(const Maps& t, const LinearParams& p, int64_t tiles, const DeviceInfo& di, cudaStream_t s) {
+rf_status launch_split(const Maps& t, const LinearParams& p, int64_t tiles, const DeviceInfo& di,
+                       cudaStream_t s) {
   static bool done[64] = {};
   if (rf_status st = set_smem(split_kernel, kSplitSmem, di, done)) return st;
   cudaLaunchConfig_t cfg{};
@@ -965,6 +978,12 @@ extern "C" rf_status rf_linear(void* d_Y, int64_t y_row_stride, int out_dtype, c
   const int64_t n256 = (d_out + 255) / 256, n128 = (d_out + 127) / 128;
   const int half = tile_rows(unit, 128);
   const int64_t pair_tiles = (rows + 2 * half - 1) / (2 * half) * n256;
+  // Pairs of CTAs once their tiles occupy half of the 76 pairs (us, pair against split):
+  //   tiles 30: 3600 rows 5120 ->  512 34.5 / 26.3     40:  512 rows 5120 -> 5120 35.9 / 45.2
+  //         32: 1024 rows 1024 -> 2048 17.8 / 16.7     42: 1560 rows 1536 -> 1536 19.7 / 27.7
+  //         32: 2048 rows  256 -> 1024 14.5 / 13.0     48:  384 rows 1536 -> 6144 19.8 / 18.8
+  //         36:  256 rows 1536 -> 9216 20.0 / 18.2     48:  512 rows 1536 -> 6144 19.9 / 27.3
+  // Up to 256 rows it is one row of tiles, and the bytes of W: for the split, whatever the width.
   Maps t;
   if (rows > 256 && pair_tiles >= di.sm_count / 4) {
     p.n_tiles = static_cast<int>(n256);
@@ -977,7 +996,7 @@ extern "C" rf_status rf_linear(void* d_Y, int64_t y_row_stride, int out_dtype, c
       const uint32_t box[2] = {128u / es_out, 32};
       if (rf_status st = make_tensor_map(&t.y, out_dtype, d_Y, 2, dims, strides, box)) return st;
     }
-    return launch_pair<256>(t, p, pair_tiles, di, s);
+    return launch_pair(t, p, pair_tiles, di, s);
   }
   const SplitPlan plan = split_plan(rows, unit, n128, p.kblocks, di.sm_count);
   const int BT = plan.tokens;

@@ -3,23 +3,24 @@
 // Token (f, y, x) of a frame grid gh x gw rotates each pair of a head by the angle of the pair's
 // axis at the token's position on it:
 //     (x0, x1) -> (x0 cos a - x1 sin a, x0 sin a + x1 cos a),   inverse: -sin a.
-// (cos, sin) come from one small table per axis (rf_rope_table: 64-bit arithmetic, rounded once), so
-// the kernel evaluates no trigonometric function and any positions can be had, also fractional
+// (cos, sin) come from one small table per axis (rf_rope_table: 64-bit arithmetic, rounded once),
+// so the kernel evaluates no trigonometric function and any positions can be had, also fractional
 // ones.  Products and sums in 32 bits, one rounding to the stored type.
 //
-// The work is one read and one write of the active rows.  A thread keeps its place in the head
-// (16 bytes of it, or 8 to 16 bytes of each half) and loads the (cos, sin) of its pairs once per token,
+// The work is one read and one write of the active rows.  A thread keeps its place in the head (16
+// bytes of it, or 8 to 16 bytes of each half) and loads the (cos, sin) of its pairs once per token,
 // for four heads whose loads are all in flight together; blocks of a fixed grid walk the active
-// tokens, since their number is known on the device only (a grid for all F frames would launch
-// F/A times the blocks).  Blocks that run together cover all heads of the same tokens, so that rows are
+// tokens, since their number is known on the device only (a grid for all F frames would launch F/A
+// times the blocks).  Blocks that run together cover all heads of the same tokens, so that rows are
 // read and written whole.  A pair's place in the tables is found again for every token, from three
 // pointers: kept per pair it took 115 registers.
 //
-// What bounds it is HBM.  Measured on warm clocks (bytes of one read and one write): 480p, 21 frames,
-// 12 + 12 heads of 128, bf16, neighbours as pairs: 60.5 us, 6.65 TB/s, as fast as a copy; 720p, 40 + 40
-// heads, fp16, halves: 452 us, 6.85 TB/s.  In halves the loads stand without branches between them
-// (with a branch per head and vector they waited for one another: 585 us); with neighbours as pairs a
-// branch per head is the better of the two at whole groups of heads (60.5 against 62.7 us).
+// What bounds it is HBM.  Measured (device time; bytes of one read and one write): 480p, 21
+// frames, 12 + 12 heads of 128, bf16, neighbours as pairs: 60.5 us, 6.65 TB/s, as fast as a copy;
+// 720p, 40 + 40 heads, fp16, halves: 452 us, 6.85 TB/s.  In halves the loads stand without branches
+// between them (with a branch per head and vector they waited for one another: 585 us); with
+// neighbours as pairs a branch per head is the better of the two at whole groups of heads (60.5
+// against 62.7 us).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -171,10 +172,9 @@ rf_status launch_rope(RopeParams p, int sm_count, cudaStream_t stream) {
 template <typename T>
 rf_status launch_rope_type(const RopeParams& p, bool half, int sm_count, cudaStream_t stream) {
   if (!half) return launch_rope<T, 16 / sizeof(T), false>(p, sm_count, stream);
-  // Halves: four elements of each at a time.  With eight of a 16-bit type the pairs' angles take 116
-  // registers, two blocks per SM: 720p x 40 heads 656 against 452 us.  The second half of the pairs,
-  // and what passes through behind it, start on a vector's boundary only where R/2 is a multiple of
-  // four.
+  // Halves: four elements of each at a time, which reach the rate of a copy; eight of a 16-bit type
+  // would need the angles of eight pairs in registers.  The second half of the pairs, and what
+  // passes through behind it, start on a vector's boundary only where R/2 is a multiple of four.
   if (p.pairs % 4 == 0) return launch_rope<T, 4, true>(p, sm_count, stream);
   return launch_rope<T, 1, true>(p, sm_count, stream);
 }

@@ -22,8 +22,8 @@ struct RowMap {
   __device__ __forceinline__ int frame(int a) const { return active ? active[a] : a; }
 };
 // Frames of 8 tokens or more are padded to 8 rows, a swizzle atom of shared memory; shorter ones
-// not at all, and are loaded whole (the swizzle goes by address, so a box may begin at any row): their
-// tiles have whole frames, tile_rows of the rows that a tile could have.
+// not at all, and are loaded whole (the swizzle goes by address, so a box may begin at any row):
+// their tiles have whole frames, tile_rows of the rows that a tile could have.
 constexpr int row_unit(int64_t N) { return N < 8 ? static_cast<int>(N) : 8; }
 constexpr int tile_rows(int unit, int most) { return most / unit * unit; }
 
@@ -43,9 +43,9 @@ struct RowBoxes {
   int n_many, n_unit; // both 0: one box of the whole tile, from token tok
   int tok;
 };
-// Rows [r0, r0 + n) of R, r0 and n multiples of the unit, a whole tile's box of `box` >= n rows; with room for n / unit
-// boxes.  Warp-collective; the same in
-// every lane.  Rows past R are not loaded, except that a tile with none at all gets a box of zeros.
+// Rows [r0, r0 + n) of R, r0 and n multiples of the unit, a whole tile's box of `box` >= n rows;
+// with room for n / unit boxes.  Warp-collective; the same in every lane.  Rows past R are not
+// loaded, except that a tile with none at all gets a box of zeros.
 template <int CAP>
 __device__ __forceinline__ RowBoxes list_boxes(const RowMap& m, int R, int r0, int n, int box,
                                                BoxList<CAP>& list) {

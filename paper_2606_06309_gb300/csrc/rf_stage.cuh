@@ -1,11 +1,11 @@
 // rf_stage.cuh -- rows of results between registers and global memory, through shared memory.
 //
 // Accumulators leave tensor memory with a row per lane.  Stored like that, each store instruction
-// of a warp touches 32 rows, 16 bytes in each, and holds up the load/store path that every
-// barrier of the CTA goes through.  So a warp turns 32 rows x 128 bytes around in 4 KB of shared
-// memory of its own, and moves whole 128-byte lines, eight lanes to a row.  The loops are kept
-// short: code that runs once per tile comes from the instruction caches beyond the SM's, and unrolled
-// it took an attention item's epilogue of 128 columns 4,800 cycles.
+// of a warp touches 32 rows, 16 bytes in each, and holds up the load/store path that every barrier
+// of the CTA goes through.  So a warp turns 32 rows x 128 bytes around in 4 KB of shared memory of
+// its own, and moves whole 128-byte lines, eight lanes to a row.  The loops are kept short: code
+// that runs once per tile comes from the instruction caches beyond the SM's, and unrolled it took
+// an attention item's epilogue of 128 columns 4,800 cycles.
 #pragma once
 #include <cstdint>
 
@@ -22,7 +22,8 @@ struct ElemBits<4> {
   using type = uint32_t;
 };
 
-constexpr int kTurnBytes = 4096;  // per warp: 32 rows of 128 bytes, 16-byte pieces swizzled by row (TMA's 128-byte swizzle)
+// Per warp: 32 rows of 128 bytes, their 16-byte pieces swizzled by row as TMA's 128-byte swizzle does.
+constexpr int kTurnBytes = 4096;
 
 __device__ __forceinline__ uint4& stage_at(uint4* stage, int row, int piece) {
   return stage[row * 8 + (piece ^ (row & 7))];
@@ -50,7 +51,8 @@ __device__ __forceinline__ RowSpan row_span(int64_t at, int64_t stride) {
   return s;
 }
 
-// Each lane's row, written to the stage (piece q at stage_at(stage, lane, q)), to base + its offset.
+// Each lane's row, written to the stage (piece q at stage_at(stage, lane, q)), to base + its
+// offset.
 __device__ __forceinline__ void store_rows(uint4* stage, char* base, const RowSpan& s,
                                            int64_t stride) {
   const int lane = threadIdx.x & 31;
@@ -96,8 +98,9 @@ __device__ __forceinline__ void await_rows() {
 }
 
 // The same element by element, for rows off the 16-byte boundaries and columns that end within the
-// 128 bytes: the first `cols` elements of BYTES (2 or 4) each.  A warp's accesses are of consecutive
-// elements of a row; pairs of 16-bit ones are stored together where the row is on their boundary.
+// 128 bytes: the first `cols` elements of BYTES (2 or 4) each.  A warp's accesses are of
+// consecutive elements of a row; pairs of 16-bit ones are stored together where the row is on their
+// boundary.
 template <int BYTES>
 __device__ __forceinline__ char* stage_elem(uint4* stage, int row, int col) {
   const int byte = col * BYTES;
