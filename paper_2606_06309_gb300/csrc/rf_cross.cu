@@ -14,10 +14,12 @@
 // four K/V tiles long, so the next item's queries and keys are loaded, and its first product
 // issued, while the softmax warps still write the last one's rows.
 //
-// What masked keys hold must not matter, and 0 * NaN is NaN in a product: their scores are
-// replaced by -inf before anything is computed with them, and warp 3 sets their rows of V to zero
-// in shared memory before P V reads them (launches with ranges or a mask; past the last state TMA
-// fills in zeros by itself).
+// What masked keys hold must not matter, and 0 * NaN is NaN in a product: their scores are replaced
+// by -inf before anything is computed with them, and warp 3 sets their rows of V to zero in shared
+// memory before P V reads them (launches with ranges or a mask; past the last state TMA fills in
+// zeros by itself).  What a mask leaves out at the ends is not visited; where it leaves few states
+// between, and all rows see the same, only those are brought: K and V row by row (TMA gather, four
+// rows an instruction, K by warp 0, V by warp 3), so that an item is as long as what is seen.
 //
 // Query rows.  Without ranges the active tokens are one list of rows (a frame padded to a multiple
 // of 8, so that a tile across frames is gathered in boxes of 8 rows); with ranges a tile stays in
@@ -44,6 +46,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "rf_ops.h"
 #include "rf_rows.cuh"
@@ -53,6 +56,9 @@
 namespace rf {
 namespace {
 
+// Which keys a launch may leave out: none, some (ranges), or, under a mask without ranges, some
+// that are the same for all rows (they may be gathered).
+constexpr int kAllKeys = 0, kSomeKeys = 1, kSameKeys = 2;
 constexpr int kBM = 128, kBN = 128;  // rows of a query tile, keys of a K/V tile
 constexpr int kThreads = 384;        // three warpgroups
 // Registers after setmaxnreg: 128 * 104 + 256 * 200 = 64512 = 384 * 168, what the launch holds.
@@ -67,27 +73,6 @@ constexpr float kRescaleLog2 = 8.0f;
 constexpr int kPThreads = 128 + 32;
 __device__ __forceinline__ int p_barrier(int X, int part) { return 1 + 2 * X + part; }
 __device__ __forceinline__ int turn_barrier(int X) { return 5 + X; }
-
-template <int D>
-struct Cfg {
-  static constexpr int kHalves = D / 64;           // 128-byte swizzle atoms across the head dim
-  static constexpr int kTileBytes = 128 * D * 2;   // one tile of Q, K or V
-  static constexpr int kHalfBytes = 128 * 128;
-  static constexpr int kSlots = D == 128 ? 4 : 8;  // K in even slots, V in odd ones
-  static constexpr int kOffKV = 2 * kTileBytes;
-  static constexpr int kOffStage = kOffKV + kSlots * kTileBytes;  // rows of results, per softmax warp
-  static constexpr int kOffBar = kOffStage + 8 * kTurnBytes;
-  static constexpr int kQFull = 0, kQEmpty = 2, kKVFull = 4, kKVEmpty = 4 + kSlots,
-                       kVClean = 4 + 2 * kSlots, kSFull = 4 + 3 * kSlots, kODone = kSFull + 2,
-                       kDrain = kODone + 2, kBars = kDrain + 2;
-  static constexpr int kOffMisc = kOffBar + kBars * 8;  // tensor memory address, abort, MMA done [2]
-  static constexpr int kOffList = kOffMisc + 32;        // boxes of the query tiles
-  static constexpr int kSmem =                          // + slack to align the base
-      kOffList + 2 * static_cast<int>(sizeof(BoxList<kBM>)) + 1024;
-  // A split item's rows: [tile][D / 4][128] float4 over the K/V ring, {max, sum} [tile][128] over
-  // the queries
-  static_assert(2 * 128 * D * 4 <= kSlots * kTileBytes, "partial rows fit the ring");
-};
 
 struct CrossParams {
   uint16_t* O;
@@ -129,8 +114,38 @@ struct Work {
   // -> 46; with many rounds lengths even out, and the order costs 2 us at the start).
   bool sorted;
   int lo, hi;  // no state before lo or from hi on is seen: what the mask pads at the ends is not visited
+  // Masks without ranges that leave few states between: only those are brought, by their rows (TMA
+  // gather), and the keys of an item are the `seen` ones, numbered from 0.
+  bool gather;
+  int seen;
   uint8_t order[kMaxSorted];
 };
+template <int D>
+struct Cfg {
+  static constexpr int kHalves = D / 64;           // 128-byte swizzle atoms across the head dim
+  static constexpr int kTileBytes = 128 * D * 2;   // one tile of Q, K or V
+  static constexpr int kHalfBytes = 128 * 128;
+  static constexpr int kSlots = D == 128 ? 4 : 8;  // K in even slots, V in odd ones
+  static constexpr int kOffKV = 2 * kTileBytes;
+  static constexpr int kOffStage = kOffKV + kSlots * kTileBytes;  // rows of results, per softmax warp
+  static constexpr int kOffBar = kOffStage + 8 * kTurnBytes;
+  static constexpr int kQFull = 0, kQEmpty = 2, kKVFull = 4, kKVEmpty = 4 + kSlots,
+                       kVClean = 4 + 2 * kSlots, kSFull = 4 + 3 * kSlots, kODone = kSFull + 2,
+                       kDrain = kODone + 2, kBars = kDrain + 2;
+  static constexpr int kOffMisc = kOffBar + kBars * 8;  // tensor memory address, abort, MMA done [2]
+  static constexpr int kOffList = kOffMisc + 32;        // boxes of the query tiles
+  static constexpr int kOffKeys = kOffList + 2 * static_cast<int>(sizeof(BoxList<kBM>));
+  static constexpr int kOffWork = kOffKeys + 2 * kBN * 4;  // kOffKeys: keys of a gathered tile of K, of V
+  static constexpr int kSmem = kOffWork + static_cast<int>(sizeof(Work));
+  // A split item's rows: [tile][D / 4][128] float4 over the K/V ring, {max, sum} [tile][128] over
+  // the queries
+  static_assert(2 * 128 * D * 4 <= kSlots * kTileBytes, "partial rows fit the ring");
+};
+
+template <int KEYS>
+__device__ __forceinline__ bool gathers(const Work& w) {
+  return KEYS == kSameKeys && w.gather;
+}
 __device__ __forceinline__ void make_work(const CrossParams& p, Work& w) {
   w.rows = p.tile_rows;
   w.A = p.rows.frames();
@@ -143,6 +158,8 @@ __device__ __forceinline__ void make_work(const CrossParams& p, Work& w) {
   w.items = p.units * w.groups * w.pairs;
   w.lo = 0;
   w.hi = p.L;
+  w.gather = false;
+  w.seen = 0;
   const int ctas = gridDim.x / p.cluster;  // (or clusters)
   w.first = blockIdx.x / p.cluster;
   w.sorted = p.kv_range && w.groups > 1 && w.groups <= kMaxSorted && w.items > ctas &&
@@ -159,15 +176,16 @@ __device__ __forceinline__ int range_tiles(const CrossParams& p, const Work& w, 
   end = min(max(r.y, begin), w.hi);
   return (end - begin + kBN - 1) / kBN;
 }
-// All threads of the block: w.lo and w.hi from the mask (L bytes; a word of 4 at a time where it
-// lies on their boundary).
-__device__ __forceinline__ void trim_states(const CrossParams& p, Work& w) {
+// All threads of the block: w.lo, w.hi and the number of states seen from the mask (L bytes; a word
+// of 4 at a time where it lies on their boundary), and whether they are gathered.
+template <int KEYS>
+__device__ __forceinline__ void trim_states(const CrossParams& p, Work& w, int rank) {
   if (threadIdx.x == 0) {
     w.lo = p.L;
     w.hi = 0;
   }
   __syncthreads();
-  int lo = p.L, hi = 0;
+  int lo = p.L, hi = 0, seen = 0;
   if ((reinterpret_cast<uintptr_t>(p.key_mask) & 3) == 0 && p.L >= 4) {
     const uint32_t* words = reinterpret_cast<const uint32_t*>(p.key_mask);
 #pragma unroll 4
@@ -175,25 +193,56 @@ __device__ __forceinline__ void trim_states(const CrossParams& p, Work& w) {
       if (const uint32_t v = words[i]) {
         lo = min(lo, 4 * i + ((__ffs(v) - 1) >> 3));
         hi = max(hi, 4 * i + 4 - (__clz(v) >> 3));
+        seen += __popc((((v & 0x7F7F7F7Fu) + 0x7F7F7F7Fu) | v) & 0x80808080u);
       }
     for (int k = (p.L & ~3) + threadIdx.x; k < p.L; k += kThreads)
       if (p.key_mask[k]) {
         lo = min(lo, k);
         hi = max(hi, k + 1);
+        ++seen;
       }
   } else {
     for (int k = threadIdx.x; k < p.L; k += kThreads)
       if (p.key_mask[k]) {
         lo = min(lo, k);
         hi = max(hi, k + 1);
+        ++seen;
       }
   }
   lo = __reduce_min_sync(0xffffffffu, lo);
   hi = __reduce_max_sync(0xffffffffu, hi);
+  seen = __reduce_add_sync(0xffffffffu, seen);
   if ((threadIdx.x & 31) == 0) {
     atomicMin(&w.lo, lo);
     atomicMax(&w.hi, hi);
+    atomicAdd(&w.seen, seen);
   }
+  __syncthreads();
+  if (KEYS != kSameKeys || w.seen == 0) return;
+  lo = w.lo;
+  const int span = w.hi - lo;
+  // Gathered where that leaves half of the tiles or fewer; a tile by rows takes 1.4 (head dim 64)
+  // to 1.8 times (128) a whole one's time, in issuing.  Tiles, us gathered against us whole: 6240
+  // tokens, 12 heads of 128, 2048 states: 4 of 16 40.0 / 78.2, 8 54.4 / 64.3, 12 72.9 / 59.6; 20
+  // frames of 1003 tokens, 24 heads of 64, 1500 states: 6 of 12 189 / 252, 9 249 / 245.  The same
+  // in all CTAs of a cluster.
+  if ((w.seen + kBN - 1) / kBN * 2 > (span + kBN - 1) / kBN) return;
+  if (p.cluster > 1) {  // a CTA's share is one of all states, with what is seen of them
+    hi = lo + static_cast<int>(static_cast<int64_t>(span) * (rank + 1) / p.cluster);
+    lo += static_cast<int>(static_cast<int64_t>(span) * rank / p.cluster);
+    seen = 0;
+    for (int k = lo + threadIdx.x; k < hi; k += kThreads) seen += p.key_mask[k] != 0;
+    seen = __reduce_add_sync(0xffffffffu, seen);
+    __syncthreads();  // read by all
+    if (threadIdx.x == 0) {
+      w.lo = lo;
+      w.hi = hi;
+      w.seen = 0;
+    }
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) atomicAdd(&w.seen, seen);
+  }
+  if (threadIdx.x == 0) w.gather = true;
   __syncthreads();
 }
 // All threads of the block; `tiles`: room for kMaxSorted numbers.
@@ -216,6 +265,7 @@ struct Item {
   int unit, group, pair;
   int begin, end, j0, j1;
 };
+template <int KEYS>
 __device__ __forceinline__ Item get_item(const CrossParams& p, const Work& w, int i, int rank) {
   Item t;
   const int gp = w.by_pairs.div(i);
@@ -223,9 +273,15 @@ __device__ __forceinline__ Item get_item(const CrossParams& p, const Work& w, in
   const int slot = p.by_units.div(gp);
   t.unit = gp - slot * p.units;
   t.group = w.sorted ? w.order[slot] : slot;
+  t.j0 = 0;
+  if (gathers<KEYS>(w)) {
+    t.begin = 0;
+    t.end = w.seen;
+    t.j1 = (w.seen + kBN - 1) / kBN;
+    return t;
+  }
   const int nt =  // below 2^24
       range_tiles(p, w, p.kv_range ? p.rows.frame(t.group) : 0, t.begin, t.end);
-  t.j0 = 0;
   t.j1 = nt;
   if (p.cluster > 1) {
     t.j0 = nt * rank / p.cluster;
@@ -273,13 +329,15 @@ struct KeyBits {
     return (w[0] & w[1] & w[2] & w[3]) == 0xFFFFFFFFu;
   }
 };
-__device__ __forceinline__ uint32_t own_keys(const CrossParams& p, const Item& t, int j) {
+// gather: all keys of the item are seen.
+__device__ __forceinline__ uint32_t own_keys(const CrossParams& p, bool gather, const Item& t,
+                                             int j) {
   const int k0 = t.begin + j * kBN + (threadIdx.x & 31);
   uint32_t m = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int k = k0 + 32 * i;
-    if (k < t.end && (!p.key_mask || p.key_mask[k] != 0)) m |= 1u << i;
+    if (k < t.end && (gather || !p.key_mask || p.key_mask[k] != 0)) m |= 1u << i;
   }
   return m;
 }
@@ -293,6 +351,77 @@ __device__ __forceinline__ KeyBits all_keys(uint32_t own) {
 // ---------------------------------------------------------------------------------------
 // TMA producer
 // ---------------------------------------------------------------------------------------
+// The states that the mask lets through, in order, 128 at a time.  Warp-collective.
+struct KeyWalk {
+  const uint8_t* mask;
+  int hi, pos;          // pos: first of the 128 states at hand
+  uint32_t own, ahead;  // this lane's of them that are still to come (bit i: pos + lane + 32 i); the next 128
+  __device__ __forceinline__ uint32_t read(int k0) const {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int k = k0 + (threadIdx.x & 31) + 32 * i;
+      if (k < hi && mask[k] != 0) m |= 1u << i;
+    }
+    return m;
+  }
+  __device__ __forceinline__ void start(const CrossParams& p, const Work& w) {
+    mask = p.key_mask;
+    hi = w.hi;
+    pos = w.lo;
+    own = read(pos);
+    ahead = read(pos + kBN);
+  }
+  // The next 128 into `keys`; behind the last one the first of the tile again.
+  __device__ __forceinline__ void tile(int* keys) {
+    const int lane = threadIdx.x & 31;
+    const uint32_t below = (1u << lane) - 1;
+    const int from = pos;
+    int fill = 0;
+#pragma unroll 1
+    while (fill < kBN && pos < hi) {
+      const KeyBits b = all_keys(own);
+      uint32_t left = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if ((own >> i) & 1u) {
+          const int at = fill + __popc(b.w[i] & below);
+          if (at < kBN) keys[at] = pos + lane + 32 * i;
+          else left |= 1u << i;
+        }
+        fill += __popc(b.w[i]);
+      }
+      if (fill > kBN) {
+        own = left;
+      } else {
+        own = ahead;
+        pos += kBN;
+        ahead = read(pos + kBN);
+      }
+    }
+    __syncwarp();
+    const int first = fill > 0 ? keys[0] : min(from, hi - 1);
+    for (int i = fill + lane; i < kBN; i += 32) keys[i] = first;
+    __syncwarp();
+  }
+};
+// Their rows of K or V (one thread).
+template <int D>
+__device__ __forceinline__ void gather_tile(const CUtensorMap* map, const int* keys, int hk,
+                                            uint32_t dst, uint32_t bar) {
+#pragma unroll 1
+  for (int i = 0; i < kBN / 4; i += 8) {
+    int4 r[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) r[k] = reinterpret_cast<const int4*>(keys)[i + k];
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+#pragma unroll
+      for (int hb = 0; hb < Cfg<D>::kHalves; ++hb)
+        tma_gather4(dst + hb * Cfg<D>::kHalfBytes + (i + k) * 512, map, bar, hk * D + hb * 64, r[k]);
+  }
+}
+
 // The maps of Q: boxes of a tile, of kBoxRows rows, and of rows.unit rows or (packed) a frame.
 struct QueryMaps {
   const CUtensorMap *whole, *many, *unit;
@@ -302,11 +431,11 @@ struct Load {
   Item t;
   RowBoxes x0, x1;
 };
-template <int D>
+template <int D, int KEYS>
 __device__ __forceinline__ void prepare_load(const QueryMaps& maps, const CrossParams& p,
                                              const Work& w, int i, int rank, BoxList<kBM>* list, bool lead,
                                              Load& n) {
-  n.t = get_item(p, w, i, rank);
+  n.t = get_item<KEYS>(p, w, i, rank);
   if (p.packed || n.t.j0 >= n.t.j1) return;
 #pragma unroll 1
   for (int X = 0; X < 2; ++X) {
@@ -356,10 +485,12 @@ __device__ __forceinline__ void load_queries(const QueryMaps& maps, const CrossP
   for (int i = kBM - x.n_unit; i < kBM; ++i) load(maps.unit, list.row[i], t.unit, list.tok[i]);
 }
 
-template <int D>
+// GATHER: w.gather (two copies of the loop: with a branch in it, whole tiles took 4 to 10% longer).
+template <int D, int KEYS, bool GATHER>
 __device__ __forceinline__ void producer(const QueryMaps& maps, const CUtensorMap* tmK,
-                                         const CUtensorMap* tmV, const CrossParams& p,
-                                         const Work& w, int rank, BoxList<kBM>* list, uint32_t sQ0,
+                                         const CUtensorMap* tmV, const CUtensorMap* tmRowsK,
+                                         const CrossParams& p, const Work& w, int rank,
+                                         BoxList<kBM>* list, int* keys, uint32_t sQ0,
                                          uint32_t sKV0, uint32_t bar0, volatile int* abort) {
   using C = Cfg<D>;
   auto bar = [&](int i) { return bar0 + 8u * i; };
@@ -367,22 +498,34 @@ __device__ __forceinline__ void producer(const QueryMaps& maps, const CUtensorMa
   int q_cnt0 = 0, q_cnt1 = 0;
   int it = 0;
   bool ok = true;
+  KeyWalk walk;
   Load n;
   int i = w.first, turn = 0;
-  if (i < w.items) prepare_load<D>(maps, p, w, i, rank, list, lead, n);
+  if (i < w.items) prepare_load<D, KEYS>(maps, p, w, i, rank, list, lead, n);
   while (ok && i < w.items) {
     const Item t = n.t;
     const int hk = p.packed ? t.unit : p.by_g.div(t.unit);
     // K and V of the tiles in turn.  The first keys go before the queries: their slot is free
     // earlier
+    if (GATHER) walk.start(p, w);
 #pragma unroll 1
     for (int n2 = 2 * t.j0; ok && n2 < 2 * t.j1; ++n2) {
       const int s = it % C::kSlots;
+      if (GATHER) {
+        if (n2 & 1) {  // warp 3 brings V
+          ++it;
+          continue;
+        }
+        walk.tile(keys);
+      }
       ok = all_wait(bar(C::kKVEmpty + s), ((it / C::kSlots) & 1) ^ 1, abort);
       if (!ok) break;
       if (lead) {
         const CUtensorMap* m = (n2 & 1) ? tmV : tmK;
         mbar_arrive_expect_tx(bar(C::kKVFull + s), C::kTileBytes);
+        if (GATHER)
+          gather_tile<D>(tmRowsK, keys, hk, sKV0 + s * C::kTileBytes, bar(C::kKVFull + s));
+        else
 #pragma unroll
         for (int hb = 0; hb < C::kHalves; ++hb)
           tma_load_3d(sKV0 + s * C::kTileBytes + hb * C::kHalfBytes, m, bar(C::kKVFull + s),
@@ -406,7 +549,7 @@ __device__ __forceinline__ void producer(const QueryMaps& maps, const CUtensorMa
     }
     i += w.step[turn];
     turn ^= 1;
-    if (ok && i < w.items) prepare_load<D>(maps, p, w, i, rank, list, lead, n);
+    if (ok && i < w.items) prepare_load<D, KEYS>(maps, p, w, i, rank, list, lead, n);
   }
   if (!ok && lead) flag_error(p, 0);
   // every copy has landed
@@ -418,9 +561,67 @@ __device__ __forceinline__ void producer(const QueryMaps& maps, const CUtensorMa
 }
 
 // ---------------------------------------------------------------------------------------
-// V rows of keys that may not be seen (CLEAN; warp 3)
+// V rows of keys that may not be seen (warp 3)
 // ---------------------------------------------------------------------------------------
+// Rows of a tile of V whose keys are not in `seen`.
 template <int D>
+__device__ __forceinline__ void clear_rows(uint8_t* tile, const KeyBits& seen) {
+  const int lane = threadIdx.x & 31;
+  // a row is 128 bytes in each half: the swizzle moves 16-byte pieces within them
+#pragma unroll 1
+  for (int r = lane; r < kBN; r += 32)
+    if (!((seen.w[r >> 5] >> lane) & 1u))
+#pragma unroll
+      for (int hb = 0; hb < Cfg<D>::kHalves; ++hb)
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+          *reinterpret_cast<uint4*>(tile + hb * Cfg<D>::kHalfBytes + r * 128 + q * 16) =
+              make_uint4(0u, 0u, 0u, 0u);
+}
+// Gathered states: warp 3 brings the tiles of V, and clears what follows the last state.
+template <int D, int KEYS>
+__device__ __forceinline__ void gather_values(const CUtensorMap* tmRowsV, const CrossParams& p,
+                                              const Work& w, int rank, int* keys, uint32_t sKV0,
+                                              uint8_t* kv, uint32_t bar0, volatile int* abort) {
+  using C = Cfg<D>;
+  auto bar = [&](int i) { return bar0 + 8u * i; };
+  const bool lead = elect_one();
+  int it = 1;  // V follows K in the ring
+  bool ok = true;
+  KeyWalk walk;
+#pragma unroll 1
+  for (int i = w.first, turn = 0; ok && i < w.items; i += w.step[turn], turn ^= 1) {
+    const Item t = get_item<KEYS>(p, w, i, rank);
+    const int hk = p.packed ? t.unit : p.by_g.div(t.unit);
+    walk.start(p, w);
+#pragma unroll 1
+    for (int j = t.j0; ok && j < t.j1; ++j, it += 2) {
+      const int s = it % C::kSlots;
+      walk.tile(keys);
+      ok = all_wait(bar(C::kKVEmpty + s), ((it / C::kSlots) & 1) ^ 1, abort);
+      if (!ok) break;
+      if (lead) {
+        mbar_arrive_expect_tx(bar(C::kKVFull + s), C::kTileBytes);
+        gather_tile<D>(tmRowsV, keys, hk, sKV0 + s * C::kTileBytes, bar(C::kKVFull + s));
+      }
+      __syncwarp();
+      if (j + 1 == t.j1 && w.seen % kBN != 0) {
+        ok = all_wait(bar(C::kKVFull + s), (it / C::kSlots) & 1, abort);
+        if (!ok) break;
+        clear_rows<D>(kv + s * C::kTileBytes, all_keys(own_keys(p, true, t, j)));
+        fence_proxy_async();
+        __syncwarp();
+        if (lead) mbar_arrive(bar(C::kVClean + s));
+      }
+    }
+  }
+  if (!ok && lead) flag_error(p, 1);
+#pragma unroll 1
+  for (int s = 1; s < C::kSlots; s += 2)  // every copy has landed
+    if (it > s + 1)
+      mbar_drain(bar(C::kKVFull + s), ((it - 2 - s) / C::kSlots) & 1, kDrainLimitNs);
+}
+template <int D, int KEYS>
 __device__ __forceinline__ void cleaner(const CrossParams& p, const Work& w, int rank, uint32_t sKV0,
                                         uint8_t* kv, uint32_t bar0, volatile int* abort) {
   using C = Cfg<D>;
@@ -429,27 +630,17 @@ __device__ __forceinline__ void cleaner(const CrossParams& p, const Work& w, int
   int it = 1;  // V follows K in the ring
 #pragma unroll 1
   for (int i = w.first, turn = 0; i < w.items; i += w.step[turn], turn ^= 1) {
-    const Item t = get_item(p, w, i, rank);
+    const Item t = get_item<KEYS>(p, w, i, rank);
 #pragma unroll 1
     for (int j = t.j0; j < t.j1; ++j, it += 2) {
-      const KeyBits b = all_keys(own_keys(p, t, j));
+      const KeyBits b = all_keys(own_keys(p, false, t, j));
       const int s = it % C::kSlots;
       if (!all_wait(bar(C::kKVFull + s), (it / C::kSlots) & 1, abort)) {
         if (lane == 0) flag_error(p, 1);
         return;
       }
       if (!b.all()) {
-        // a row is 128 bytes in each half: the swizzle moves 16-byte pieces within them
-        uint8_t* tile = kv + s * C::kTileBytes;
-#pragma unroll 1
-        for (int r = lane; r < kBN; r += 32)
-          if (!((b.w[r >> 5] >> lane) & 1u))
-#pragma unroll
-            for (int hb = 0; hb < C::kHalves; ++hb)
-#pragma unroll
-              for (int q = 0; q < 8; ++q)
-                *reinterpret_cast<uint4*>(tile + hb * C::kHalfBytes + r * 128 + q * 16) =
-                    make_uint4(0u, 0u, 0u, 0u);
+        clear_rows<D>(kv + s * C::kTileBytes, b);
         fence_proxy_async();
       }
       __syncwarp();
@@ -479,7 +670,7 @@ __device__ __forceinline__ void mma_pv(uint32_t tO, uint32_t tP, uint64_t dV, in
     tc_mma_ts(tO, tP + part * 32 + k * 8, dV + part * 512 + ((k * 2048) >> 4), idesc, acc | k | part);
 }
 
-template <int D, bool F16, bool CLEAN>
+template <int D, bool F16, int KEYS, bool GATHER>
 __device__ __forceinline__ bool mma_issuer(const CrossParams& p, const Work& w, int rank, int X,
                                            uint32_t tmem, uint32_t sQ0, uint32_t sKV0,
                                            uint32_t bar0, volatile int* abort) {
@@ -489,11 +680,13 @@ __device__ __forceinline__ bool mma_issuer(const CrossParams& p, const Work& w, 
   const uint32_t tS = tmem + X * 128, tO = tmem + 256 + X * 128;
   const uint64_t dQ = smem_desc_sw128(sQ0 + X * C::kTileBytes, 16, 1024);
   int q_cnt = 0, it = 0;    // it: ring index of the item's first tile of keys
+  const bool tail = GATHER && w.seen % kBN != 0;
+  uint32_t cleared = 0;     // bit s: parity of the clearings of slot s (gathered values)
   bool my_turn = X == 0;    // the first turn is tile A's
   bool ok = true;
 #pragma unroll 1
   for (int i = w.first, turn = 0; ok && i < w.items; i += w.step[turn], turn ^= 1) {
-    const Item t = get_item(p, w, i, rank);
+    const Item t = get_item<KEYS>(p, w, i, rank);
     const int nt = t.j1 - t.j0;
     if (nt <= 0) continue;
     const bool both = 2 * t.pair + 1 < w.tiles, mine = X == 0 || both;
@@ -508,8 +701,15 @@ __device__ __forceinline__ bool mma_issuer(const CrossParams& p, const Work& w, 
       const int iV = it + 2 * j + 1, iK = iV + 1;
       const int sV = iV % C::kSlots, sK = iK % C::kSlots;
       // (V cleaned, where a launch has keys that may not be seen)
-      if (!first)
-        ok = all_wait(bar((CLEAN ? C::kVClean : C::kKVFull) + sV), (iV / C::kSlots) & 1, abort);
+      if (!first) {
+        if (GATHER && tail && !more) {
+          ok = all_wait(bar(C::kVClean + sV), (cleared >> sV) & 1, abort);
+          cleared ^= 1u << sV;
+        } else {
+          ok = all_wait(bar((KEYS != kAllKeys && !GATHER ? C::kVClean : C::kKVFull) + sV),
+                        (iV / C::kSlots) & 1, abort);
+        }
+      }
       if (ok && more) ok = all_wait(bar(C::kKVFull + sK), (iK / C::kSlots) & 1, abort);
       ok = __all_sync(0xffffffffu, ok && *abort == 0);
       if (!ok) break;
@@ -575,19 +775,20 @@ __device__ __forceinline__ uint4 pack8(const float* o, float scale) {
 
 // The running maximum (in units of log2, scaled) and sum of a row over a CTA's K/V tiles of an
 // item, with P left in tensor memory for the MMA warp.  False: a wait gave up.
-template <int D, bool F16, bool CLEAN>
-__device__ __forceinline__ bool softmax_item(const CrossParams& p, const Item& t, int X, uint32_t tS,
-                                             uint32_t tO, uint32_t bar_s, int& s_cnt, float& m_out,
+template <int D, bool F16, int KEYS>
+__device__ __forceinline__ bool softmax_item(const CrossParams& p, const Work& w, const Item& t,
+                                             int X, uint32_t tS, uint32_t tO, uint32_t bar_s, int& s_cnt, float& m_out,
                                              float& l_out, volatile int* abort) {
   const float sl2 = p.scale_log2;
+  const bool gather = gathers<KEYS>(w);
   float m = -INFINITY, l = 0.f;
-  uint32_t own = CLEAN ? own_keys(p, t, t.j0) : 0;
+  uint32_t own = KEYS != kAllKeys ? own_keys(p, gather, t, t.j0) : 0;
 #pragma unroll 1
   for (int j = t.j0; j < t.j1; ++j) {
     KeyBits bits{};
-    if (CLEAN) {
+    if (KEYS != kAllKeys) {
       bits = all_keys(own);
-      if (j + 1 < t.j1) own = own_keys(p, t, j + 1);
+      if (j + 1 < t.j1) own = own_keys(p, gather, t, j + 1);
     }
     if (!all_wait(bar_s, s_cnt & 1, abort)) return false;
     ++s_cnt;
@@ -598,7 +799,7 @@ __device__ __forceinline__ bool softmax_item(const CrossParams& p, const Item& t
       tmem_ld32(tS + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&s[c * 32]));
     tmem_wait_ld();
     float* sf = reinterpret_cast<float*>(s);
-    if (CLEAN) {
+    if (KEYS != kAllKeys) {
       if (!bits.all()) {
 #pragma unroll
         for (int c = 0; c < kBN; ++c)
@@ -675,7 +876,7 @@ __device__ __forceinline__ bool softmax_item(const CrossParams& p, const Item& t
   return true;
 }
 
-template <int D, bool F16, bool CLEAN>
+template <int D, bool F16, int KEYS>
 __device__ __forceinline__ bool softmax_group(const CUtensorMap* tmO, const CrossParams& p,
                                               const Work& w, int rank, int X,
                                               uint32_t tmem, uint8_t* smem, uint32_t bar0,
@@ -690,7 +891,7 @@ __device__ __forceinline__ bool softmax_group(const CUtensorMap* tmO, const Cros
   int64_t at = -1;  // byte offset of this thread's row in O
   int s_cnt = 0, o_cnt = 0;
   Item next;
-  if (w.first < w.items) next = get_item(p, w, w.first, rank);
+  if (w.first < w.items) next = get_item<KEYS>(p, w, w.first, rank);
 #pragma unroll 1
   for (int i = w.first, turn = 0; i < w.items;) {
     const Item t = next;
@@ -698,14 +899,14 @@ __device__ __forceinline__ bool softmax_group(const CUtensorMap* tmO, const Cros
     turn ^= 1;
     const int tile = 2 * t.pair + X;
     if (tile >= w.tiles) {
-      if (i < w.items) next = get_item(p, w, i, rank);
+      if (i < w.items) next = get_item<KEYS>(p, w, i, rank);
       continue;
     }
     float m = -INFINITY, l = 0.f;
     bool ok = t.j0 >= t.j1 ||
-              softmax_item<D, F16, CLEAN>(p, t, X, tS, tO, bar(C::kSFull + X), s_cnt, m, l, abort);
+              softmax_item<D, F16, KEYS>(p, w, t, X, tS, tO, bar(C::kSFull + X), s_cnt, m, l, abort);
     // found while the last P V runs: behind it every cycle counts
-    if (i < w.items) next = get_item(p, w, i, rank);
+    if (i < w.items) next = get_item<KEYS>(p, w, i, rank);
     const int first = whole_tile(p, w, t, tile);
     // no key: zeros, not 0 * accumulator, which may hold anything
     const bool none = l == 0.f;
@@ -784,13 +985,13 @@ __device__ __forceinline__ bool softmax_group(const CUtensorMap* tmO, const Cros
 
 // A split item's rows from all CTAs of the cluster: O = sum_c 2^(m_c - M) O_c / sum_c 2^(m_c - M)
 // l_c.  Each CTA takes its share of the columns of every row.
-template <int D, bool F16>
+template <int D, bool F16, int KEYS>
 __device__ __forceinline__ void join(const CrossParams& p, const Work& w, int rank, int X,
                                      uint32_t sbase) {
   using C = Cfg<D>;
   const int i = w.first;
   if (i >= w.items) return;
-  const Item t = get_item(p, w, i, rank);
+  const Item t = get_item<KEYS>(p, w, i, rank);
   const int tile = 2 * t.pair + X;
   if (tile >= w.tiles) return;
   const int row = threadIdx.x & 127;
@@ -855,17 +1056,20 @@ __device__ __forceinline__ void release_mma(const volatile int* done, int bar_a,
   }
 }
 
-template <int D, bool F16, bool CLEAN>
+template <int D, bool F16, int KEYS>
 __global__ void __launch_bounds__(kThreads, 1)
     cross_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmMany,
                  const __grid_constant__ CUtensorMap tmUnit, const __grid_constant__ CUtensorMap tmK,
                  const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmO,
-                 const CrossParams p) {
+                 const __grid_constant__ CUtensorMap tmRowsK,
+                 const __grid_constant__ CUtensorMap tmRowsV, const CrossParams p) {
   using C = Cfg<D>;
-  extern __shared__ uint8_t smem_raw[];
-  const uint32_t raw = smem_u32(smem_raw);
-  const uint32_t sbase = (raw + 1023u) & ~1023u;
-  uint8_t* smem = smem_raw + (sbase - raw);
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const uint32_t sbase = smem_u32(smem);
+  if (sbase & 1023u) {  // (swizzled tiles; no room to align it here)
+    if (threadIdx.x == 0) flag_error(p, 5);
+    return;
+  }
   const uint32_t sQ0 = sbase, sKV0 = sbase + C::kOffKV, bar0 = sbase + C::kOffBar;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::kOffMisc);
   volatile int* abort = reinterpret_cast<volatile int*>(smem + C::kOffMisc + 4);
@@ -873,7 +1077,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int warp = threadIdx.x >> 5;
   const int rank = p.cluster > 1 ? static_cast<int>(cluster_rank()) : 0;
 
-  __shared__ Work work;
+  Work& work = *reinterpret_cast<Work*>(smem + C::kOffWork);
   if (threadIdx.x == 64) make_work(p, work);
   if (threadIdx.x == 0) {
     for (int X = 0; X < 2; ++X) {
@@ -904,20 +1108,29 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
   const Work& w = work;
-  if (CLEAN && p.key_mask) trim_states(p, work);
-  if (CLEAN && w.sorted) sort_frames(p, work, reinterpret_cast<int*>(smem + C::kOffStage));
+  if (KEYS != kAllKeys && p.key_mask) trim_states<KEYS>(p, work, rank);
+  if (KEYS == kSomeKeys && w.sorted) sort_frames(p, work, reinterpret_cast<int*>(smem + C::kOffStage));
 
   // Every warp of warpgroup 0 gives registers back before any softmax warp asks for more, so the
   // increase below always finds them.
   if (warp < 4) {
     reg_dealloc<kRegsControl>();
     if (warp == 0) {
-      producer<D>({&tmQ, &tmMany, &tmUnit}, &tmK, &tmV, p, w, rank,
-                  reinterpret_cast<BoxList<kBM>*>(smem + C::kOffList), sQ0, sKV0, bar0, abort);
+      auto produce = [&](auto gather) {
+        producer<D, KEYS, gather.value>(
+            {&tmQ, &tmMany, &tmUnit}, &tmK, &tmV, &tmRowsK, p, w, rank,
+            reinterpret_cast<BoxList<kBM>*>(smem + C::kOffList),
+            reinterpret_cast<int*>(smem + C::kOffKeys), sQ0, sKV0, bar0, abort);
+      };
+      if (gathers<KEYS>(w)) produce(std::bool_constant<KEYS == kSameKeys>{});
+      else produce(std::false_type{});
     } else if (warp < 3) {
       const int X = warp - 1;
-      const bool ok =
-          mma_issuer<D, F16, CLEAN>(p, w, rank, X, tmem, sQ0, sKV0, bar0, abort);
+      auto issue = [&](auto gather) {
+        return mma_issuer<D, F16, KEYS, gather.value>(p, w, rank, X, tmem, sQ0, sKV0, bar0, abort);
+      };
+      const bool ok = gathers<KEYS>(w) ? issue(std::bool_constant<KEYS == kSameKeys>{})
+                                       : issue(std::false_type{});
       __syncwarp();
       mma_done[X] = 1;  // waits on no named barrier any more
       if (!ok) release_mma(mma_done + (X ^ 1), turn_barrier(X ^ 1), turn_barrier(X ^ 1), 64);
@@ -925,20 +1138,23 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (elect_one()) tc_commit(bar0 + 8 * (C::kDrain + X));
       __syncwarp();
       mbar_drain(bar0 + 8 * (C::kDrain + X), 0, kDrainLimitNs);
-    } else if (CLEAN) {
-      cleaner<D>(p, w, rank, sKV0, smem + C::kOffKV, bar0, abort);
+    } else if (gathers<KEYS>(w)) {
+      gather_values<D, KEYS>(&tmRowsV, p, w, rank, reinterpret_cast<int*>(smem + C::kOffKeys) + kBN, sKV0,
+                       smem + C::kOffKV, bar0, abort);
+    } else if (KEYS != kAllKeys) {
+      cleaner<D, KEYS>(p, w, rank, sKV0, smem + C::kOffKV, bar0, abort);
     }
   } else {
     reg_alloc<kRegsSoftmax>();
     const int X = (warp - 4) >> 2;
-    if (!softmax_group<D, F16, CLEAN>(&tmO, p, w, rank, X, tmem, smem, bar0, abort))
+    if (!softmax_group<D, F16, KEYS>(&tmO, p, w, rank, X, tmem, smem, bar0, abort))
       release_mma(mma_done + X, p_barrier(X, 0), p_barrier(X, 1), kPThreads);
   }
   __syncwarp();
   if (p.cluster > 1) {
     cluster_arrive();
     cluster_wait();
-    if (warp >= 4) join<D, F16>(p, w, rank, (warp - 4) >> 2, sbase);
+    if (warp >= 4) join<D, F16, KEYS>(p, w, rank, (warp - 4) >> 2, sbase);
     __syncwarp();
     cluster_arrive();  // every CTA has read the others' rows
     cluster_wait();
@@ -955,7 +1171,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 // Host side
 // ---------------------------------------------------------------------------------------
 struct Maps {
-  CUtensorMap q, many, unit, k, v, o;
+  CUtensorMap q, many, unit, k, v, o, rows_k, rows_v;
 };
 
 // [rows][heads][d] elements of 16 bits, boxes of 64 x box_heads x box_rows.
@@ -968,14 +1184,23 @@ rf_status map_heads(CUtensorMap* m, int dtype, const void* base, int d, int head
   return make_tensor_map(m, dtype, base, 3, dims, strides, box);
 }
 
-template <int D, bool F16, bool CLEAN>
+// [rows][cols] elements of 16 bits, boxes of 64 x 1.
+rf_status map_rows(CUtensorMap* m, int dtype, const void* base, int cols, int64_t rows,
+                   int64_t row_stride) {
+  const uint64_t dims[2] = {static_cast<uint64_t>(cols), static_cast<uint64_t>(rows)};
+  const uint64_t strides[1] = {static_cast<uint64_t>(row_stride) * 2};
+  const uint32_t box[2] = {64, 1};
+  return make_tensor_map(m, dtype, base, 2, dims, strides, box);
+}
+
+template <int D, bool F16, int KEYS>
 rf_status launch(const Maps& m, const CrossParams& p, int grid, const DeviceInfo& di,
                  cudaStream_t s) {
   constexpr int smem = Cfg<D>::kSmem;
   static bool done[64] = {};
   if (smem > di.max_smem_optin) return fail(RF_ERR_UNSUPPORTED, "rf_cross_attn: shared memory");
   if (!done[di.device]) {
-    if (cudaError_t e = cudaFuncSetAttribute(cross_kernel<D, F16, CLEAN>,
+    if (cudaError_t e = cudaFuncSetAttribute(cross_kernel<D, F16, KEYS>,
                                              cudaFuncAttributeMaxDynamicSharedMemorySize, smem))
       return fail(RF_ERR_CUDA, "cudaFuncSetAttribute(rf_cross_attn)", e);
     done[di.device] = true;
@@ -991,20 +1216,28 @@ rf_status launch(const Maps& m, const CrossParams& p, int grid, const DeviceInfo
   attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = p.cluster > 1 ? 1 : 0;
-  if (cudaError_t e = cudaLaunchKernelEx(&cfg, cross_kernel<D, F16, CLEAN>, m.q, m.many, m.unit, m.k,
-                                         m.v, m.o, p)) {
+  if (cudaError_t e = cudaLaunchKernelEx(&cfg, cross_kernel<D, F16, KEYS>, m.q, m.many, m.unit, m.k,
+                                         m.v, m.o, m.rows_k, m.rows_v, p)) {
     cudaGetLastError();
     return fail(RF_ERR_CUDA, "rf_cross_attn launch", e);
   }
   return RF_OK;
 }
 
+template <int D, bool F16>
+rf_status launch_type(int keys, const Maps& m, const CrossParams& p, int grid,
+                      const DeviceInfo& di, cudaStream_t s) {
+  switch (keys) {
+    case kAllKeys: return launch<D, F16, kAllKeys>(m, p, grid, di, s);
+    case kSomeKeys: return launch<D, F16, kSomeKeys>(m, p, grid, di, s);
+    default: return launch<D, F16, kSameKeys>(m, p, grid, di, s);
+  }
+}
 template <int D>
-rf_status launch_dim(bool f16, bool clean, const Maps& m, const CrossParams& p, int grid,
+rf_status launch_dim(bool f16, int keys, const Maps& m, const CrossParams& p, int grid,
                      const DeviceInfo& di, cudaStream_t s) {
-  if (f16)
-    return clean ? launch<D, true, true>(m, p, grid, di, s) : launch<D, true, false>(m, p, grid, di, s);
-  return clean ? launch<D, false, true>(m, p, grid, di, s) : launch<D, false, false>(m, p, grid, di, s);
+  return f16 ? launch_type<D, true>(keys, m, p, grid, di, s)
+             : launch_type<D, false>(keys, m, p, grid, di, s);
 }
 
 // CTAs per item: the number whose busiest SM has the least to do, in K/V tiles.  A further round of
@@ -1120,9 +1353,15 @@ extern "C" rf_status rf_cross_attn(void* d_O, float* d_lse, const void* d_Q, con
   }
   if (rf_status st = map_heads(&m.k, dtype, K, d, Hkv, rows_kv, k_row_stride, 1, kBN)) return st;
   if (rf_status st = map_heads(&m.v, dtype, V, d, Hkv, rows_kv, v_row_stride, 1, kBN)) return st;
+  m.rows_k = m.k;
+  m.rows_v = m.v;
+  if (d_key_mask && !d_kv_range && L > 0) {  // single rows, where the mask leaves few
+    if (rf_status st = map_rows(&m.rows_k, dtype, d_K, Hkv * d, L, k_row_stride)) return st;
+    if (rf_status st = map_rows(&m.rows_v, dtype, d_V, Hkv * d, L, v_row_stride)) return st;
+  }
   if (rf_status st = map_heads(&m.o, dtype, d_O, d, H, T, o_row_stride, 1, 32)) return st;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  const bool clean = d_kv_range || d_key_mask;
-  return d == 128 ? launch_dim<128>(dtype == RF_FP16, clean, m, p, grid, di, s)
-                  : launch_dim<64>(dtype == RF_FP16, clean, m, p, grid, di, s);
+  const int keys = d_kv_range ? kSomeKeys : d_key_mask ? kSameKeys : kAllKeys;
+  return d == 128 ? launch_dim<128>(dtype == RF_FP16, keys, m, p, grid, di, s)
+                  : launch_dim<64>(dtype == RF_FP16, keys, m, p, grid, di, s);
 }
