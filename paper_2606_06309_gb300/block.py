@@ -15,6 +15,7 @@ Normalisations stay the model's: each of the three is a callable on the hidden s
 """
 from __future__ import annotations
 
+from contextlib import nullcontext
 from dataclasses import dataclass
 from typing import Callable, Optional, Tuple
 
@@ -36,6 +37,13 @@ class BlockWeights:
     cross_out: Linear  # [D, H d]
     up: Linear       # [Df, D]
     down: Linear     # [D, Df]
+
+
+def _on(stream):
+    """What torch allocates and runs inside (the norms, too) is ordered on `stream`."""
+    if stream is None:
+        return nullcontext()
+    return torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream)
 
 
 class ActiveBlock:
@@ -67,9 +75,9 @@ class ActiveBlock:
         mask [L]: zero = padding; ranges int32 [F, 2]: the states each frame sees."""
         L = states.shape[0]
         w, b = self.w.cross_kv
-        self.enc = torch.empty(L, 2, self.heads_kv, self.core.d, dtype=w.dtype, device=w.device)
-        rf_linear(self.enc.view(L, -1), states, w, 1, L, bias=b, status=self.core.status,
-                  stream=stream)
+        with _on(stream):
+            self.enc = torch.empty(L, 2, self.heads_kv, self.core.d, dtype=w.dtype, device=w.device)
+            rf_linear(self.enc.view(L, -1), states, w, 1, L, bias=b, status=self.core.status)
         self.enc_mask, self.enc_range = mask, ranges
 
     def run(self, s: int, x: torch.Tensor, scale: float, norms=(None, None, None), gates=(None, None),
@@ -79,9 +87,13 @@ class ActiveBlock:
         gates: fp32 [D] or [F, D] of the attention and of the feed-forward pair (None: 1).
 
         core.compact(s) has been called for the step (once, for all blocks)."""
+        with _on(stream):
+            self._run(s, x, scale, norms, gates)
+
+    def _run(self, s, x, scale, norms, gates):
         c, w = self.core, self.w
         T, F, N, H, d = c.F * c.N, c.F, c.N, c.H, c.d
-        on = dict(active=c.active, counts=c.counts, stream=stream)
+        on = dict(active=c.active, counts=c.counts)
         lin = dict(on, status=c.status)
         n1, n2, n3 = (n or (lambda h: h) for n in norms)
         q, k, v = self.qkv.unbind(1)
@@ -89,8 +101,8 @@ class ActiveBlock:
         rf_linear(self.qkv.view(T, -1), n1(x), w.qkv[0], F, N, bias=w.qkv[1], **lin)
         rf_rope(q, q, k, k, F, self.gh, self.gw, self.dims, self.tables, pairing=self.pairing, **on)
         if c.Kc is not None:
-            c.project_kv(s, k, v, stream)
-        c.attn(self.rows, q, k, v, scale, None, stream)
+            c.project_kv(s, k, v)
+        c.attn(self.rows, q, k, v, scale)
         rf_linear(x, self.rows.view(T, H * d), w.out[0], F, N, bias=w.out[1], gate=gates[0],
                   residual=x, **lin)
 
