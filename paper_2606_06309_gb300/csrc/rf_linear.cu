@@ -14,8 +14,9 @@
 // Measured (device time, calls one after another):
 //   75,600 rows 5120 -> 5120, residual and gate: bounded by the tensor cores, 1.84 PFLOP/s while
 //     the clock holds (2.16 ms; 2.57 ms, 1.54 PFLOP/s, when the power limit lowers it).
-//   6,240 of 20,280 rows 1536 -> 6144, bias and GELU: 84 us, 1.40 PFLOP/s: 600 tiles are 7.9 for
-//     each of the 76 pairs, and the activation of a tile takes most of its products' 6,100 cycles.
+//   6,240 of 20,280 rows 1536 -> 6144, bias and GELU: 82 us, 1.44 PFLOP/s: 600 tiles are 7.9 for
+//     each of the 76 pairs, a tile's products take 12,300 cycles, and the last tile's activation,
+//     5 us, has none to hide behind.
 //   1 row 1536 -> 9216: 9.4 us, of which reading W's 28 MB takes 4.2: launch, tensor memory,
 //     barriers and one cluster's exchange are the rest.
 //   333 rows 1000 -> 777: 10.8 us, the same fixed costs.
