@@ -276,8 +276,10 @@ def _rows(fn: str, name: str, t, shape) -> int:
     """Row stride of t [rows, n] or [rows, heads, d], whose rows have to be contiguous."""
     if t.shape != shape:
         raise ValueError(f"{fn}: {name} has shape {tuple(t.shape)}, not {shape}")
-    st = t.stride()
     n = shape[-1]
+    if t.is_contiguous():
+        return n * shape[1] if len(shape) == 3 else n
+    st = t.stride()
     ok = st[-1] == 1 or n <= 1
     if len(shape) == 3:
         ok = ok and (st[1] == n or shape[1] <= 1)
@@ -288,11 +290,27 @@ def _rows(fn: str, name: str, t, shape) -> int:
     return st[0] if shape[0] > 1 or st[0] > n else n
 
 
+def _row(fn: str, name: str, t, n: int) -> int:
+    """Address of a row [n] or [1, n]."""
+    if t.dim() != 1:
+        _rows(fn, name, t, (1, n))
+    elif t.shape[0] != n or (n > 1 and t.stride(0) != 1):
+        raise ValueError(f"{fn}: {name} is not a contiguous row of {n} ({tuple(t.shape)}, "
+                         f"strides {t.stride()})")
+    return t.data_ptr()
+
+
+_NAMES: dict = {}  # torch types -> their names: str() of one takes as long as the whole check
+
+
 def _whole(fn: str, name: str, t, shape, kinds) -> Optional[int]:
     """Address of an optional contiguous tensor of a given shape and type."""
     if t is None:
         return None
-    if t.shape != shape or str(t.dtype) not in kinds or not t.is_contiguous():
+    kind = t.dtype
+    if kind not in _NAMES:
+        _NAMES[kind] = str(kind)
+    if t.shape != shape or _NAMES[kind] not in kinds or not t.is_contiguous():
         raise ValueError(f"{fn}: {name} is not a contiguous {shape} of {' or '.join(kinds)}")
     return t.data_ptr()
 
@@ -367,16 +385,14 @@ def rf_linear(Y, X, W, F: int, N: int, bias=None, act=None, gate=None, residual=
     b = g = r = None
     gate_stride = r_stride = 0
     if bias is not None:
-        _rows(fn, "bias", bias[None] if bias.dim() == 1 else bias, (1, d_out))
-        b = bias.data_ptr()
+        b = _row(fn, "bias", bias, d_out)
     if gate is not None:
         if _dtype(fn, gate) != _F32:
             raise ValueError(f"{fn}: gate is not fp32")
         if gate.dim() == 1:
-            _rows(fn, "gate", gate[None], (1, d_out))
+            g = _row(fn, "gate", gate, d_out)
         else:
-            gate_stride = _rows(fn, "gate", gate, (F, d_out))
-        g = gate.data_ptr()
+            gate_stride, g = _rows(fn, "gate", gate, (F, d_out)), gate.data_ptr()
     if residual is not None:
         r, r_stride = residual.data_ptr(), _rows(fn, "residual", residual, (T, d_out))
     _check(fn, load().rf_linear(
