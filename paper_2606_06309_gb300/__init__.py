@@ -277,7 +277,7 @@ def _rows(fn: str, name: str, t, shape) -> int:
     if t.shape != shape:
         raise ValueError(f"{fn}: {name} has shape {tuple(t.shape)}, not {shape}")
     n = shape[-1]
-    if t.is_contiguous():
+    if shape[0] > 1 and t.is_contiguous():  # (a single row counts as contiguous at any stride)
         return n * shape[1] if len(shape) == 3 else n
     st = t.stride()
     ok = st[-1] == 1 or n <= 1
