@@ -109,21 +109,33 @@ def _check(fn: str, st: int):
 def _ptr(t) -> Optional[int]:
     if t is None:
         return None
+    address = getattr(t, "data_ptr", None)  # most are tensors
+    if address is not None:
+        return address()
     if isinstance(t, int):
         return t
-    if isinstance(t, np.ndarray):
-        return t.ctypes.data
-    return t.data_ptr()
+    return t.ctypes.data
+
+
+_CURRENT = None  # () -> handle of the current stream
+
+
+def _current_stream():
+    """That function; torch is imported with the first call that needs it."""
+    global _CURRENT
+    import torch
+    raw, device = (getattr(torch._C, n, None) for n in ("_cuda_getCurrentRawStream",
+                                                        "_cuda_getDevice"))
+    if raw is None or device is None:
+        _CURRENT = lambda: torch.cuda.current_stream().cuda_stream  # noqa: E731
+    else:  # the same handle without a Stream object: 0.2 us of host time instead of 2.9
+        _CURRENT = lambda: raw(device())  # noqa: E731
+    return _CURRENT
 
 
 def _stream(stream) -> Optional[int]:
     if stream is None:
-        import torch
-        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-        if raw is None:
-            return torch.cuda.current_stream().cuda_stream
-        # the same handle without a Stream object: 0.2 us of host time instead of 2.9
-        return raw(torch._C._cuda_getDevice())
+        return (_CURRENT or _current_stream())()
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -332,21 +344,25 @@ def rf_rope(Yq, Xq, Yk, Xk, F: int, gh: int, gw: int, dims, tables, pairing: str
     shape = (F * gh * gw, *Xq.shape[1:])
     dim_t, dim_h, dim_w = dims
     t, h, w = tables
-    yq, xq = _rows(fn, "Yq", Yq, shape), _rows(fn, "Xq", Xq, shape)
+    yq = _rows(fn, "Yq", Yq, shape)
+    xq = yq if Xq is Yq else _rows(fn, "Xq", Xq, shape)
     kp = (None, None, 0, 0, 0)
     if Xk is not None:
         ks = (shape[0], Xk.shape[1], shape[2])
-        kp = (Yk.data_ptr(), Xk.data_ptr(), _rows(fn, "Yk", Yk, ks), _rows(fn, "Xk", Xk, ks), ks[1])
+        yk = _rows(fn, "Yk", Yk, ks)
+        kp = (Yk.data_ptr(), Xk.data_ptr(), yk, yk if Xk is Yk else _rows(fn, "Xk", Xk, ks), ks[1])
     elif Yk is not None:
         raise ValueError(f"{fn}: Yk without Xk")
     dt = _dtype(fn, Xq, Yq, Xk, Yk)
     f32 = ("torch.float32",)
-    _check(fn, load().rf_rope(
+    st = (_LIB or load()).rf_rope(
         Yq.data_ptr(), Xq.data_ptr(), yq, xq, shape[1], *kp, dt, F, gh, gw, shape[2], dim_t, dim_h,
         dim_w, _whole(fn, "time's table", t, (F, dim_t // 2, 2), f32),
         _whole(fn, "height's table", h, (gh, dim_h // 2, 2), f32),
         _whole(fn, "width's table", w, (gw, dim_w // 2, 2), f32), _PAIRINGS[pairing], inverse,
-        _ptr(active), _ptr(counts), _stream(stream)))
+        _ptr(active), _ptr(counts), _stream(stream))
+    if st:
+        raise RFError(fn, st)
 
 
 def rf_cross_attn(O, lse, Q, K, V, F: int, N: int, softmax_scale: float, kv_range=None,
@@ -362,13 +378,15 @@ def rf_cross_attn(O, lse, Q, K, V, F: int, N: int, softmax_scale: float, kv_rang
     rows = (F * N, H, d)
     if kv[2] != d:
         raise ValueError(f"{fn}: head dim {d} of Q, {kv[2]} of K")
-    _check(fn, load().rf_cross_attn(
+    st = (_LIB or load()).rf_cross_attn(
         O.data_ptr(), _whole(fn, "lse", lse, (H, F * N), ("torch.float32",)), Q.data_ptr(),
         K.data_ptr(), V.data_ptr(), _rows(fn, "O", O, rows), _rows(fn, "Q", Q, rows),
         _rows(fn, "K", K, kv), _rows(fn, "V", V, kv), _dtype(fn, Q, O, K, V), F, N, H, Hkv, d, L,
         _whole(fn, "kv_range", kv_range, (F, 2), ("torch.int32",)),
         _whole(fn, "key_mask", key_mask, (L,), ("torch.uint8", "torch.bool")), _ptr(active),
-        _ptr(counts), softmax_scale, _ptr(status), _stream(stream)))
+        _ptr(counts), softmax_scale, _ptr(status), _stream(stream))
+    if st:
+        raise RFError(fn, st)
 
 
 def rf_linear(Y, X, W, F: int, N: int, bias=None, act=None, gate=None, residual=None, active=None,
@@ -395,10 +413,12 @@ def rf_linear(Y, X, W, F: int, N: int, bias=None, act=None, gate=None, residual=
             gate_stride, g = _rows(fn, "gate", gate, (F, d_out)), gate.data_ptr()
     if residual is not None:
         r, r_stride = residual.data_ptr(), _rows(fn, "residual", residual, (T, d_out))
-    _check(fn, load().rf_linear(
+    st = (_LIB or load()).rf_linear(
         Y.data_ptr(), _rows(fn, "Y", Y, (T, d_out)), out, X.data_ptr(), _rows(fn, "X", X, (T, d_in)),
         W.data_ptr(), _rows(fn, "W", W, (d_out, d_in)), dt, F, N, d_in, d_out, b, _ACTS[act], g,
-        gate_stride, r, r_stride, _ptr(active), _ptr(counts), _ptr(status), _stream(stream)))
+        gate_stride, r, r_stride, _ptr(active), _ptr(counts), _ptr(status), _stream(stream))
+    if st:
+        raise RFError(fn, st)
 
 
 def rf_pipeline_create(F: int, N: int, H: int, d: int, E: int, plan: dict, z2, K0, V0,
