@@ -1078,7 +1078,10 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int rank = p.cluster > 1 ? static_cast<int>(cluster_rank()) : 0;
 
   Work& work = *reinterpret_cast<Work*>(smem + C::kOffWork);
-  if (threadIdx.x == 64) make_work(p, work);
+  if (threadIdx.x == 64) {
+    cudaGridDependencySynchronize();
+    make_work(p, work);
+  }
   if (threadIdx.x == 0) {
     for (int X = 0; X < 2; ++X) {
       mbar_init(bar0 + 8 * (C::kQFull + X), 1);
@@ -1108,6 +1111,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
   const Work& w = work;
+  cudaGridDependencySynchronize();  // what was launched before is done (launch_early)
   if (KEYS != kAllKeys && p.key_mask) trim_states<KEYS>(p, work, rank);
   if (KEYS == kSomeKeys && w.sorted) sort_frames(p, work, reinterpret_cast<int*>(smem + C::kOffStage));
 
@@ -1210,18 +1214,8 @@ rf_status launch(const Maps& m, const CrossParams& p, int grid, const DeviceInfo
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = static_cast<unsigned>(p.cluster);
-  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = p.cluster > 1 ? 1 : 0;
-  if (cudaError_t e = cudaLaunchKernelEx(&cfg, cross_kernel<D, F16, KEYS>, m.q, m.many, m.unit, m.k,
-                                         m.v, m.o, m.rows_k, m.rows_v, p)) {
-    cudaGetLastError();
-    return fail(RF_ERR_CUDA, "rf_cross_attn launch", e);
-  }
-  return RF_OK;
+  return launch_early(cfg, p.cluster, "rf_cross_attn launch", cross_kernel<D, F16, KEYS>, m.q, m.many,
+                      m.unit, m.k, m.v, m.o, m.rows_k, m.rows_v, p);
 }
 
 template <int D, bool F16>

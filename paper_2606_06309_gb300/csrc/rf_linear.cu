@@ -442,6 +442,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
   cluster_wait();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
+  cudaGridDependencySynchronize();  // what was launched before is done (launch_early)
 
   const int R = p.rows.frames() * p.rows.Np;
   const int half = p.tile_rows;  // rows of a CTA's half of a tile
@@ -659,9 +660,6 @@ __global__ void __launch_bounds__(kSplitThreads, 1)
   const int rank = C > 1 ? static_cast<int>(cluster_rank()) : 0;
   const int tile = blockIdx.x / C;
   const int m = tile / p.n_tiles, n = tile - m * p.n_tiles;
-  const int R = p.rows.frames() * p.rows.Np;
-  const int r0 = m * p.tile_rows, rows = min(p.tile_rows, R - r0);
-  if (r0 >= R) return;  // the whole cluster
   const int stage_bytes = 16384 + BT * 128;
   const uint32_t tmem_cols = BT < 32 ? 32 : BT;
 
@@ -676,6 +674,10 @@ __global__ void __launch_bounds__(kSplitThreads, 1)
     tma_prefetch_desc(&tmX);
     tma_prefetch_desc(&tmW);
   }
+  cudaGridDependencySynchronize();  // what was launched before is done (launch_early)
+  const int R = p.rows.frames() * p.rows.Np;
+  const int r0 = m * p.tile_rows, rows = min(p.tile_rows, R - r0);
+  if (r0 >= R) return;  // the whole cluster
   BoxList<256>& list = *reinterpret_cast<BoxList<256>*>(smem + kSplitOffList);
   RowBoxes* boxes = reinterpret_cast<RowBoxes*>(smem + kSplitOffBoxes);
   if (warp == 2) {
@@ -883,9 +885,13 @@ rf_status launch_pair(const Maps& t, const LinearParams& p, int64_t tiles, const
     resident[di.device].store(most, std::memory_order_relaxed);
   }
   const int64_t pairs = std::min<int64_t>(tiles, most);
-  pair_kernel<<<static_cast<unsigned>(2 * pairs), kPairThreads, PairCfg::kSmem, s>>>(
-      t.x, t.many, t.unit, t.w, t.y, p);
-  return launch_status("rf_linear pair_kernel launch");
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(static_cast<unsigned>(2 * pairs));
+  cfg.blockDim = dim3(kPairThreads);
+  cfg.dynamicSmemBytes = PairCfg::kSmem;
+  cfg.stream = s;
+  return launch_early(cfg, 1, "rf_linear pair_kernel launch", pair_kernel, t.x, t.many, t.unit, t.w,
+                      t.y, p);
 }
 
 rf_status launch_split(const Maps& t, const LinearParams& p, int64_t tiles, const DeviceInfo& di,
@@ -897,17 +903,8 @@ rf_status launch_split(const Maps& t, const LinearParams& p, int64_t tiles, cons
   cfg.blockDim = dim3(kSplitThreads);
   cfg.dynamicSmemBytes = kSplitSmem;
   cfg.stream = s;
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = static_cast<unsigned>(p.cluster);
-  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = p.cluster > 1 ? 1 : 0;
-  if (cudaError_t e = cudaLaunchKernelEx(&cfg, split_kernel, t.x, t.many, t.unit, t.w, p)) {
-    cudaGetLastError();
-    return fail(RF_ERR_CUDA, "rf_linear split_kernel launch", e);
-  }
-  return RF_OK;
+  return launch_early(cfg, p.cluster, "rf_linear split_kernel launch", split_kernel, t.x, t.many,
+                      t.unit, t.w, p);
 }
 
 }  // namespace

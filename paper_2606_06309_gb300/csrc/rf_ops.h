@@ -21,4 +21,29 @@ inline int dtype_bytes(int dtype) {
 rf_status make_tensor_map(CUtensorMap* m, int dtype, const void* base, int rank,
                           const uint64_t* dims, const uint64_t* strides, const uint32_t* box);
 
+#ifdef __CUDACC__
+// A launch that may begin when the last blocks before it on the stream have left, with its own start
+// (barriers, tensor memory, addresses) while what they wrote is made visible.  Every block of the
+// kernel calls cudaGridDependencySynchronize before it reads or writes global memory or leaves, so the
+// order of the stream is kept, and of whatever follows.  Calls one after another: 1 row 1536 -> 9216
+// 12.3 -> 10 us, 4 of 13 x 1560 tokens over 512 states 24.3 -> 21.7 us.
+template <typename... P, typename... A>
+rf_status launch_early(cudaLaunchConfig_t cfg, int cluster, const char* what, void (*kernel)(P...),
+                       const A&... args) {
+  cudaLaunchAttribute attr[2] = {};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = static_cast<unsigned>(cluster);
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  if (cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, args...)) {
+    cudaGetLastError();
+    return fail(RF_ERR_CUDA, what, e);
+  }
+  return RF_OK;
+}
+#endif
+
 }  // namespace rf

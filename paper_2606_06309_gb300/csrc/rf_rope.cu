@@ -102,6 +102,7 @@ __global__ void __launch_bounds__(kRopeThreads)
   const int to_other = through ? 0 : p.pairs * static_cast<int>(sizeof(T));
   const int end_t = p.half[0], end_h = end_t + p.half[1];      // the axes' pairs end here
 
+  cudaGridDependencySynchronize();  // what was launched before is done (launch_early)
   const int A = p.active ? min(max(p.counts[0], 0), p.F) : p.F;
   const uint32_t rows = static_cast<uint32_t>(A) * p.N, step = gridDim.y * slots;
   for (uint32_t r = blockIdx.y * slots + slot; r < rows; r += step) {
@@ -165,8 +166,11 @@ rf_status launch_rope(RopeParams p, int sm_count, cudaStream_t stream) {
   // eight blocks of 256 threads fill an SM; four times that many even out the blocks' ends
   const int64_t most = std::max<int64_t>(1, static_cast<int64_t>(sm_count) * 32 / groups);
   const dim3 grid(groups, static_cast<unsigned>(std::min(blocks, most)));
-  rope_kernel<T, E, HALF><<<grid, kRopeThreads, 0, stream>>>(p);
-  return launch_status("rope_kernel launch");
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(kRopeThreads);
+  cfg.stream = stream;
+  return launch_early(cfg, 1, "rope_kernel launch", rope_kernel<T, E, HALF>, p);
 }
 
 template <typename T>
