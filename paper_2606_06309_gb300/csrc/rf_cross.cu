@@ -32,7 +32,7 @@
 // from all of them, in the order of the ranges.
 //
 // Measured (device time, calls one after another):
-//   75,600 tokens, 40 heads of 128, 512 states: 541 us, 1.47 PFLOP/s on one set of inputs (613 us with
+//   75,600 tokens, 40 heads of 128, 512 states: 541 us, 1.47 PFLOP/s on one set of inputs (597 us with
 //     inputs that change from call to call, when the power limit lowers the clock).  An item of 4 K/V
 //     tiles takes 13,200 cycles: 9,200 in its steps, of which the products are 8,200, and 4,000 from
 //     the last product to the next item's first P.
