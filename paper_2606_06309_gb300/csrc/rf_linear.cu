@@ -28,6 +28,7 @@
 #include <atomic>
 #include <cmath>
 
+#include "rf_deal.h"
 #include "rf_ops.h"
 #include "rf_rows.cuh"
 #include "rf_stage.cuh"
@@ -358,11 +359,17 @@ __device__ __forceinline__ void load_rows(const RowBoxes& x, const BoxList<CAP>&
     if (who == of - 1) load(maps.whole, 0, x.tok);
     return;
   }
+  Deal mine{who, of};
 #pragma unroll 1
-  for (int i = who; i < x.n_many; i += of) load(maps.many, list.row[i], list.tok[i]);
+  while (mine.more(x.n_many)) {
+    const int i = mine.take();
+    load(maps.many, list.row[i], list.tok[i]);
+  }
 #pragma unroll 1
-  for (int i = CAP - 1 - who; i >= CAP - x.n_unit; i -= of)
+  while (mine.more(x.n_many + x.n_unit)) {
+    const int i = CAP - 1 - (mine.take() - x.n_many);
     load(maps.unit, list.row[i], list.tok[i]);
+  }
 }
 
 // ---------------------------------------------------------------------------------------
@@ -695,8 +702,9 @@ __global__ void __launch_bounds__(kSplitThreads, 1)
 
   const RowBoxes x = *boxes;
   // the boxes of a tile across frames are dealt to all warps but the MMA warp: one warp would take
-  // a hundred cycles for each (33 frames of one token, 1536 -> 6144: 29 us, this way 16)
-  const int loaders = x.n_many + x.n_unit > 2 ? kSplitThreads / 32 - 1 : 1;
+  // a hundred cycles for each (33 frames of one token, 1536 -> 6144: 29 us, this way 16); a warp
+  // without a box stays out, as nothing would keep the ring from passing it
+  const int loaders = loading_warps(x.n_many + x.n_unit, kSplitThreads / 32 - 1);
   const int who = warp == 0 ? 0 : warp - 1;
   if (warp != 1 && who < loaders) {
     const bool lead = elect_one();
