@@ -50,13 +50,17 @@ class ActiveBlock:
     """Buffers and tables of one block over `core`'s frames, whose N tokens are a grid gh x gw.
 
     dims: rotated elements of a head per axis (time, height, width).  positions: the axes' positions,
-    0, 1, 2, ... where None.  core's key/value cache is this layer's."""
+    0, 1, 2, ... where None.  core's key/value cache is this layer's.  Weights are bf16, the step
+    core's type."""
 
     def __init__(self, core: StepCore, gh: int, gw: int, weights: BlockWeights, dims, heads_kv: int,
                  positions=None, base: float = 10000.0, pairing: str = "interleaved",
                  act: str = "gelu_tanh"):
         if gh * gw != core.N:
             raise ValueError(f"a grid of {gh} x {gw} is not {core.N} tokens")
+        if weights.qkv[0].dtype is not torch.bfloat16:  # the step core reads queries, keys, values so
+            raise ValueError(f"weights of {weights.qkv[0].dtype}: the step core's attention is of "
+                             "torch.bfloat16")
         self.core, self.gh, self.gw, self.w = core, gh, gw, weights
         self.dims, self.heads_kv, self.pairing, self.act = tuple(dims), heads_kv, pairing, act
         T, H, d = core.F * core.N, core.H, core.d
