@@ -12,6 +12,12 @@ The step core's attention with the operators around it, on one stream with no ho
 
 The hidden states are [F*N, D] for all frames; only the active frames' rows are read and written.
 Normalisations stay the model's: each of the three is a callable on the hidden states.
+
+A model's blocks run over one StepCore (plan, lists, workspace), each with a cache of its own:
+
+    blocks = [ActiveBlock(core, gh, gw, w, dims, heads_kv, own_cache=True) for w in layers]
+    core.compact(s)                     # once per step
+    for block in blocks: block.run(s, x, scale, ...)
 """
 from __future__ import annotations
 
@@ -46,16 +52,36 @@ def _on(stream):
     return torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream)
 
 
+def _one_layer(core: StepCore, block, s: int):
+    """Refuse core's cache where it lost this block's keys: this block and then another one stored theirs
+    of the step before, and this one now wants them back for frames that are skipped."""
+    Kc = core.Kc
+    if Kc.is_inference():  # counts no versions
+        return
+    cache = (Kc.data_ptr(), Kc._version)  # replaced or written by the caller: another layer's now
+    last_cache, last_s, writers = getattr(core, "_cache_writers", (None, None, []))
+    if cache == last_cache and s == last_s:
+        core._cache_writers = (cache, s, [w for w in writers if w != id(block)] + [id(block)])
+        return
+    if cache == last_cache and id(block) in writers[:-1] and not core.plan.host["mask"][s].all():
+        raise ValueError("ActiveBlock: another block has stored its keys in the step core's cache: "
+                         "blocks that share a step core each need own_cache=True")
+    core._cache_writers = (cache, s, [id(block)])
+
+
 class ActiveBlock:
     """Buffers and tables of one block over `core`'s frames, whose N tokens are a grid gh x gw.
 
     dims: rotated elements of a head per axis (time, height, width).  positions: the axes' positions,
-    0, 1, 2, ... where None.  core's key/value cache is this layer's.  Weights are bf16, the step
-    core's type."""
+    0, 1, 2, ... where None.  Weights are bf16, the step core's type.
+
+    own_cache: a rolling key/value cache of this block's own, zeros at first (set_kv_cache), so that
+    several blocks can share core, which may then have none.  Otherwise core's cache is this
+    layer's, and no other's."""
 
     def __init__(self, core: StepCore, gh: int, gw: int, weights: BlockWeights, dims, heads_kv: int,
                  positions=None, base: float = 10000.0, pairing: str = "interleaved",
-                 act: str = "gelu_tanh"):
+                 act: str = "gelu_tanh", own_cache: bool = False):
         if gh * gw != core.N:
             raise ValueError(f"a grid of {gh} x {gw} is not {core.N} tokens")
         if weights.qkv[0].dtype is not torch.bfloat16:  # the step core reads queries, keys, values so
@@ -71,8 +97,16 @@ class ActiveBlock:
         self.qkv = torch.zeros(T, 3, H, d, dtype=wt.dtype, device=wt.device)
         self.rows = torch.zeros(T, H, d, dtype=wt.dtype, device=wt.device)  # attention's results
         self.ffn = torch.zeros(T, weights.up[0].shape[0], dtype=wt.dtype, device=wt.device)
+        self.cache = None      # own keys and values, [2, F, N, H d] each
+        if own_cache:
+            self.cache = tuple(torch.zeros(2, core.F, core.N, H * d, dtype=wt.dtype, device=wt.device)
+                               for _ in range(2))
         self.enc = None        # [L, 2, Hkv, d]
         self.enc_mask = self.enc_range = None
+
+    def set_kv_cache(self, K0: torch.Tensor, V0: torch.Tensor):
+        """StepCore.set_kv_cache for this layer's cache."""
+        self.core.set_kv_cache(K0, V0, self.cache)
 
     def encode(self, states: torch.Tensor, mask=None, ranges=None, stream=None):
         """Keys and values of an encoder's states [L, De], kept until the next call: once per prompt.
@@ -101,10 +135,14 @@ class ActiveBlock:
         lin = dict(on, status=c.status)
         n1, n2, n3 = (n or (lambda h: h) for n in norms)
         q, k, v = self.qkv.unbind(1)
+        if self.cache is None and c.Kc is not None:
+            _one_layer(c, self, s)
 
         rf_linear(self.qkv.view(T, -1), n1(x), w.qkv[0], F, N, bias=w.qkv[1], **lin)
         rf_rope(q, q, k, k, F, self.gh, self.gw, self.dims, self.tables, pairing=self.pairing, **on)
-        if c.Kc is not None:
+        if self.cache is not None:
+            c.project_kv(s, k, v, cache=self.cache)
+        elif c.Kc is not None:
             c.project_kv(s, k, v)
         c.attn(self.rows, q, k, v, scale)
         rf_linear(x, self.rows.view(T, H * d), w.out[0], F, N, bias=w.out[1], gate=gates[0],

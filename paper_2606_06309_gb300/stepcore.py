@@ -91,11 +91,12 @@ class StepCore:
         self.z2[0].copy_(z0)
         self.z2[1].copy_(z0)
 
-    def set_kv_cache(self, K0: torch.Tensor, V0: torch.Tensor):
+    def set_kv_cache(self, K0: torch.Tensor, V0: torch.Tensor, cache=None):
         """Both cache slots of every frame hold the keys and values K0, V0 ([F*N, H, d]): a frame
-        projected before its second update gets them back (alpha weights two equal states)."""
+        projected before its second update gets them back (alpha weights two equal states).
+        cache: another layer's pair of caches in place of the step core's own."""
         D = self.H * self.d
-        for c, X in ((self.Kc, K0), (self.Vc, V0)):
+        for c, X in zip(cache or (self.Kc, self.Vc), (K0, V0)):
             x = X.reshape(self.F, self.N, D)
             c[0].copy_(x)
             c[1].copy_(x)
@@ -118,8 +119,10 @@ class StepCore:
         rf_project(self.ctx, self.z2, _row(self.plan.cur_slot, s), _row(self.plan.alpha, s),
                    _row(self.plan.beta, s), self.F, self.E, stream)
 
-    def project_kv(self, s: int, K, V, stream=None):
-        rf_project_kv(K, V, K.stride(0), self.Kc, self.Vc, _row(self.plan.cur_slot, s),
+    def project_kv(self, s: int, K, V, stream=None, cache=None):
+        """cache: another layer's pair of caches in place of the step core's own."""
+        Kc, Vc = cache or (self.Kc, self.Vc)
+        rf_project_kv(K, V, K.stride(0), Kc, Vc, _row(self.plan.cur_slot, s),
                       _row(self.plan.alpha, s), _row(self.plan.beta, s), self.active,
                       self.skipped, self.counts, self.F, self.N, self.H * self.d, stream)
 
