@@ -28,7 +28,7 @@ from typing import Callable, Optional, Tuple
 import numpy as np
 import torch
 
-from . import rf_cross_attn, rf_linear, rf_rope, rf_rope_table
+from . import _stream, rf_cross_attn, rf_linear, rf_rope, rf_rope_table
 from .stepcore import StepCore
 
 Linear = Tuple[torch.Tensor, Optional[torch.Tensor]]  # weight [out, in], bias [out] or None
@@ -50,6 +50,23 @@ def _on(stream):
     if stream is None:
         return nullcontext()
     return torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream)
+
+
+class _Enqueued:
+    """The work on the current stream so far, for other streams to wait for.  Work recorded in a graph
+    has no place among theirs, and a stream being captured cannot wait for what is outside: there
+    the order is the caller's."""
+
+    def __init__(self):
+        self.stream, self.event = _stream(None), None
+        if not torch.cuda.is_current_stream_capturing():
+            self.event = torch.cuda.Event()
+            self.event.record()
+
+    def wait(self, at: int):
+        """at: the current stream's handle."""
+        if at != self.stream and self.event is not None and not torch.cuda.is_current_stream_capturing():
+            torch.cuda.current_stream().wait_event(self.event)
 
 
 def _one_layer(core: StepCore, block, s: int):
@@ -77,7 +94,12 @@ class ActiveBlock:
 
     own_cache: a rolling key/value cache of this block's own, zeros at first (set_kv_cache), so that
     several blocks can share core, which may then have none.  Otherwise core's cache is this
-    layer's, and no other's."""
+    layer's, and no other's.
+
+    encode and run may be given different streams: run waits for the encoder's states and for the
+    block's making, and states are kept until the runs that read them are done.  What else a call
+    reads is the caller's to order, and a block is kept while runs on other streams than it was
+    made on are under way."""
 
     def __init__(self, core: StepCore, gh: int, gw: int, weights: BlockWeights, dims, heads_kv: int,
                  positions=None, base: float = 10000.0, pairing: str = "interleaved",
@@ -103,6 +125,10 @@ class ActiveBlock:
                                for _ in range(2))
         self.enc = None        # [L, 2, Hkv, d]
         self.enc_mask = self.enc_range = None
+        self._made, self._encoded = _Enqueued() if wt.is_cuda else None, None
+        self._enc_homes = ()   # streams that the states and what is kept with them were allocated on
+        self._enc_read = {}    # stream -> event behind its last run that read them
+        self._enc_old = []     # earlier states still being read, with such events
 
     def set_kv_cache(self, K0: torch.Tensor, V0: torch.Tensor):
         """StepCore.set_kv_cache for this layer's cache."""
@@ -113,10 +139,19 @@ class ActiveBlock:
         mask [L]: zero = padding; ranges int32 [F, 2]: the states each frame sees."""
         L = states.shape[0]
         w, b = self.w.cross_kv
+        capturing = torch.cuda.is_current_stream_capturing
+        homes = () if mask is None and ranges is None else (_stream(None),)
+        quiet = capturing()  # nothing may be asked of events outside a capture
         with _on(stream):
-            self.enc = torch.empty(L, 2, self.heads_kv, self.core.d, dtype=w.dtype, device=w.device)
-            rf_linear(self.enc.view(L, -1), states, w, 1, L, bias=b, status=self.core.status)
-        self.enc_mask, self.enc_range = mask, ranges
+            enc = torch.empty(L, 2, self.heads_kv, self.core.d, dtype=w.dtype, device=w.device)
+            rf_linear(enc.view(L, -1), states, w, 1, L, bias=b, status=self.core.status)
+            encoded, quiet = _Enqueued(), quiet or capturing()
+        if not quiet:
+            self._enc_old = [o for o in self._enc_old if not all(e.query() for e in o[-1])]
+        if self._enc_read:
+            self._enc_old.append((self.enc, self.enc_mask, self.enc_range, list(self._enc_read.values())))
+        self.enc, self.enc_mask, self.enc_range = enc, mask, ranges
+        self._encoded, self._enc_homes, self._enc_read = encoded, (encoded.stream, *homes), {}
 
     def run(self, s: int, x: torch.Tensor, scale: float, norms=(None, None, None), gates=(None, None),
             stream=None):
@@ -126,7 +161,17 @@ class ActiveBlock:
 
         core.compact(s) has been called for the step (once, for all blocks)."""
         with _on(stream):
-            self._run(s, x, scale, norms, gates)
+            at = _stream(None)
+            for before in (self._made, self._encoded):
+                if before is not None:
+                    before.wait(at)
+            try:
+                self._run(s, x, scale, norms, gates)
+            finally:
+                if any(h != at for h in self._enc_homes) and not torch.cuda.is_current_stream_capturing():
+                    if at not in self._enc_read:
+                        self._enc_read[at] = torch.cuda.Event()
+                    self._enc_read[at].record()
 
     def _run(self, s, x, scale, norms, gates):
         c, w = self.core, self.w
