@@ -15,7 +15,10 @@ Normalisations stay the model's: each of the three is a callable on the hidden s
 
 A model's blocks run over one StepCore (plan, lists, workspace), each with a cache of its own:
 
-    blocks = [ActiveBlock(core, gh, gw, w, dims, heads_kv, own_cache=True) for w in layers]
+    blocks = []
+    for w in layers:
+        blocks.append(ActiveBlock(core, gh, gw, w, dims, heads_kv, own_cache=True,
+                                  buffers=blocks[0] if blocks else None))
     core.compact(s)                     # once per step
     for block in blocks: block.run(s, x, scale, ...)
 """
@@ -96,6 +99,10 @@ class ActiveBlock:
     several blocks can share core, which may then have none.  Otherwise core's cache is this
     layer's, and no other's.
 
+    buffers: another block whose buffers (not its cache) this one uses too, as it runs before or after
+    that one on the same stream: 75,600 tokens, D = 5120, feed-forward 13,824 take 5.2 GB.  Without a
+    cache, its own or core's, a block's buffers hold its skipped frames' keys and cannot be shared.
+
     encode and run may be given different streams: run waits for the encoder's states and for the
     block's making, and states are kept until the runs that read them are done.  What else a call
     reads is the caller's to order, and a block is kept while runs on other streams than it was
@@ -103,7 +110,8 @@ class ActiveBlock:
 
     def __init__(self, core: StepCore, gh: int, gw: int, weights: BlockWeights, dims, heads_kv: int,
                  positions=None, base: float = 10000.0, pairing: str = "interleaved",
-                 act: str = "gelu_tanh", own_cache: bool = False):
+                 act: str = "gelu_tanh", own_cache: bool = False,
+                 buffers: Optional["ActiveBlock"] = None):
         if gh * gw != core.N:
             raise ValueError(f"a grid of {gh} x {gw} is not {core.N} tokens")
         if weights.qkv[0].dtype is not torch.bfloat16:  # the step core reads queries, keys, values so
@@ -116,9 +124,24 @@ class ActiveBlock:
         pos = positions or [np.arange(n) for n in (core.F, gh, gw)]
         self.tables = [torch.from_numpy(rf_rope_table(p, dim, base)).to(wt.device) if dim else None
                        for p, dim in zip(pos, self.dims)]
-        self.qkv = torch.zeros(T, 3, H, d, dtype=wt.dtype, device=wt.device)
-        self.rows = torch.zeros(T, H, d, dtype=wt.dtype, device=wt.device)  # attention's results
-        self.ffn = torch.zeros(T, weights.up[0].shape[0], dtype=wt.dtype, device=wt.device)
+
+        def zeros(name, *shape):
+            if buffers is None:
+                return torch.zeros(shape, dtype=wt.dtype, device=wt.device)
+            t = getattr(buffers, name)
+            if t.shape != shape or t.device != wt.device:
+                raise ValueError(f"{name} is {tuple(t.shape)} on {t.device} in the block whose buffers are "
+                                 f"to be shared, not {shape} on {wt.device}")
+            return t
+
+        if buffers is not None:
+            if (not own_cache and core.Kc is None) or (buffers.cache is None and buffers.core.Kc is None):
+                raise ValueError("a block without a cache has its skipped frames' keys in its buffers")
+            if buffers._made is not None:
+                buffers._made.wait(_stream(None))
+        self.qkv = zeros("qkv", T, 3, H, d)
+        self.rows = zeros("rows", T, H, d)  # attention's results
+        self.ffn = zeros("ffn", T, weights.up[0].shape[0])
         self.cache = None      # own keys and values, [2, F, N, H d] each
         if own_cache:
             self.cache = tuple(torch.zeros(2, core.F, core.N, H * d, dtype=wt.dtype, device=wt.device)
