@@ -62,12 +62,30 @@ __device__ __forceinline__ float ex2_neg_log2e(float x) {
 __device__ __forceinline__ float times_sigmoid(float x, float s) {
   return __fdividef(x, 1.f + ex2_neg_log2e(s));
 }
+// x Phi(x).  The tail Phi(-|x|) = e^(-x^2 / 2) times a function that falls from 1/2 to 0.03 over the
+// numbers where it is not yet lost; that one is t Q(t) with t = 1 / (1 + 0.3 |x|) and Q of degree 7,
+// fitted for the least largest relative error, 1.3e-7.  So the digits of negative x stay, which
+// 1 + erf(x / sqrt 2) loses (4% of the value at -5), up to the rounding of x^2: 8e-6 at -12.  Fewer
+// instructions, too: 6240 rows 1536 -> 6144 81 us, with erff 92, with erfcf 143.
+__device__ __forceinline__ float gelu(float x) {
+  const float t = __fdividef(1.f, fmaf(0.3f, fabsf(x), 1.f));
+  float q = 0.035931736f;
+  q = fmaf(q, t, -0.158276007f);
+  q = fmaf(q, t, 0.208206624f);
+  q = fmaf(q, t, -0.0553938560f);
+  q = fmaf(q, t, 0.129469201f);
+  q = fmaf(q, t, 0.0996374935f);
+  q = fmaf(q, t, 0.120798357f);
+  q = fmaf(q, t, 0.119626388f);
+  const float tail = t * q * ex2_approx(-0.72134752f * (x * x));
+  return x * (x < 0.f ? tail : 1.f - tail);
+}
 template <int N>
 __device__ __forceinline__ void activate(int act, float (&v)[N]) {
   switch (act) {
     case RF_ACT_GELU:
 #pragma unroll
-      for (int i = 0; i < N; ++i) v[i] = 0.5f * v[i] * (1.f + erff(v[i] * 0.70710678118654752f));
+      for (int i = 0; i < N; ++i) v[i] = gelu(v[i]);
       break;
     case RF_ACT_GELU_TANH:  // 0.5 (1 + tanh u) = sigmoid(2 u)
 #pragma unroll
