@@ -55,12 +55,19 @@ struct Epilogue {
   int vec_cols;         // bias and gate alone
 };
 
-__device__ __forceinline__ float ex2_neg_log2e(float x) {
-  return ex2_approx(-1.4426950408889634f * x);
+// 1 / x for x of 2^-126 to 2^126, to a unit in the last place; 0 from there on
+__device__ __forceinline__ float rcp_approx(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
 }
-// x * sigmoid(s): 1 + e^-s overflows to infinity for very negative s, and the quotient is then 0
-__device__ __forceinline__ float times_sigmoid(float x, float s) {
-  return __fdividef(x, 1.f + ex2_neg_log2e(s));
+// x * sigmoid(s) = x / (1 + h^2) with h = e^(-s / 2) = 2^t.  Both sides of the quotient are scaled by 2^-22:
+// the denominator then stays in the range of floats where the value does (SiLU to -100; unscaled the
+// quotient is 0 from -87.3 down, where the value is -1e-36).
+__device__ __forceinline__ float times_sigmoid(float x, float t) {
+  constexpr float kScale = 0x1p-22f;
+  const float h = ex2_approx(t);
+  return x * kScale * rcp_approx(fmaf(h * kScale, h, kScale));
 }
 // x Phi(x).  The tail Phi(-|x|) = e^(-x^2 / 2) times a function that falls from 1/2 to 0.03 over the
 // numbers where it is not yet lost; that one is t Q(t) with t = 1 / (1 + 0.3 |x|) and Q of degree 7,
@@ -87,14 +94,14 @@ __device__ __forceinline__ void activate(int act, float (&v)[N]) {
 #pragma unroll
       for (int i = 0; i < N; ++i) v[i] = gelu(v[i]);
       break;
-    case RF_ACT_GELU_TANH:  // 0.5 (1 + tanh u) = sigmoid(2 u)
+    case RF_ACT_GELU_TANH:  // 0.5 (1 + tanh u) = sigmoid(2 u), u = sqrt(2 / pi) (v + 0.044715 v^3); t = -u log2 e
 #pragma unroll
       for (int i = 0; i < N; ++i)
-        v[i] = times_sigmoid(v[i], 1.5957691216057308f * (v[i] + 0.044715f * v[i] * v[i] * v[i]));
+        v[i] = times_sigmoid(v[i], v[i] * fmaf(-0.051471619f, v[i] * v[i], -1.15110411f));
       break;
     case RF_ACT_SILU:
 #pragma unroll
-      for (int i = 0; i < N; ++i) v[i] = times_sigmoid(v[i], v[i]);
+      for (int i = 0; i < N; ++i) v[i] = times_sigmoid(v[i], -0.72134752f * v[i]);
       break;
     default:
       break;

@@ -5,6 +5,11 @@ exactly, and the result is the activation of a known number, in 32 bits.  Relati
   gelu       z^2 / 2 in the exponent is off by less than 2.5 2^-24 of itself, which is within (z^2 + |z|) 2^-23
              of the value; the rest is an exponential (2^-22), a quotient (2^-22) and some twelve
              products and sums (2^-24 each) or a function evaluated as well as that: 2^-20 in all
+  silu       with |s| the exponent (log2 e |s| is rounded to 32 bits, which costs |s| 2^-23 of e^s), s = z: an
+             exponential in two factors of 2^-22 each, a quotient (2^-22) and three products (2^-24
+             each): |z| 2^-23 + 2^-20
+  gelu_tanh  s = 2 sqrt(2/pi) (z + 0.044715 z^3) itself from four operations and three constants, each
+             off by at most 2^-24, so |s| (2^-23 + 7 2^-24) + 2^-20 <= |s| 2^-21 + 2^-20
 and 2^-126 absolute: numbers below the smallest normal one may be lost.
 """
 import math
@@ -17,18 +22,24 @@ from ops_check import DEV, DTYPES
 
 def _act(z, act):
     """In 64 bits, without cancellation in the tails; and the relative bound."""
+    if act == "silu":
+        return z * torch.sigmoid(z), z.abs() * 2.0 ** -23 + 2.0 ** -20
+    if act == "gelu_tanh":  # (1 + tanh u) / 2 is the sigmoid of 2 u
+        s = 2 * math.sqrt(2 / math.pi) * (z + 0.044715 * z ** 3)
+        return z * torch.sigmoid(s), s.abs() * 2.0 ** -21 + 2.0 ** -20
     return (0.5 * z * torch.erfc(-z / math.sqrt(2.0)),
             (z * z + z.abs()) * 2.0 ** -23 + 2.0 ** -20)
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("act", ["gelu"])
+@pytest.mark.parametrize("act", ["gelu", "gelu_tanh", "silu"])
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
 @pytest.mark.parametrize("rows,d_out", [(1, 777), (200, 128), (600, 5120), (600, 5123)])
 def test_activation(cuda_lib, rows, d_out, dtype, act):
     dt = DTYPES[dtype]
+    top = 100.0 if act == "silu" else 12.0
     g = torch.Generator().manual_seed(rows)
-    x = ((torch.rand(rows, 1, generator=g) * 2 - 1) * 12.0).to(dt)
+    x = ((torch.rand(rows, 1, generator=g) * 2 - 1) * top).to(dt)
     w = (2.0 ** -torch.randint(0, 6, (d_out, 1), generator=g).float()).to(dt)
     w[::7] *= -1
     X, W = (torch.zeros(t.shape[0], 8, dtype=dt, device=DEV) for t in (x, w))
