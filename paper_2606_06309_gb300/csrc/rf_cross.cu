@@ -45,6 +45,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <type_traits>
 
@@ -1201,7 +1202,7 @@ template <int D, bool F16, int KEYS>
 rf_status launch(const Maps& m, const CrossParams& p, int grid, const DeviceInfo& di,
                  cudaStream_t s) {
   constexpr int smem = Cfg<D>::kSmem;
-  static bool done[64] = {};
+  static std::atomic<bool> done[64] = {};
   if (smem > di.max_smem_optin) return fail(RF_ERR_UNSUPPORTED, "rf_cross_attn: shared memory");
   if (!done[di.device]) {
     if (cudaError_t e = cudaFuncSetAttribute(cross_kernel<D, F16, KEYS>,

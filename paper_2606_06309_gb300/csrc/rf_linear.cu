@@ -830,7 +830,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1)
 // Host side
 // ---------------------------------------------------------------------------------------
 template <typename K>
-rf_status set_smem(K kernel, int bytes, const DeviceInfo& di, bool (&done)[64]) {
+rf_status set_smem(K kernel, int bytes, const DeviceInfo& di, std::atomic<bool> (&done)[64]) {
   if (bytes > di.max_smem_optin) return fail(RF_ERR_UNSUPPORTED, "rf_linear: shared memory");
   if (!done[di.device]) {
     if (cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
@@ -901,7 +901,7 @@ rf_status make_maps(Maps* t, const LinearParams& p, const void* d_X, int64_t x_s
 
 rf_status launch_pair(const Maps& t, const LinearParams& p, int64_t tiles, const DeviceInfo& di,
                       cudaStream_t s) {
-  static bool done[64] = {};
+  static std::atomic<bool> done[64] = {};
   if (rf_status st = set_smem(pair_kernel, PairCfg::kSmem, di, done)) return st;
   // pairs that run together: where a GPC has an odd number of free SMs it is fewer than half of
   // them, and a pair that waits for the others to finish would double the time
@@ -929,7 +929,7 @@ rf_status launch_pair(const Maps& t, const LinearParams& p, int64_t tiles, const
 
 rf_status launch_split(const Maps& t, const LinearParams& p, int64_t tiles, const DeviceInfo& di,
                        cudaStream_t s) {
-  static bool done[64] = {};
+  static std::atomic<bool> done[64] = {};
   if (rf_status st = set_smem(split_kernel, kSplitSmem, di, done)) return st;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(static_cast<unsigned>(tiles * p.cluster));
