@@ -311,6 +311,18 @@ __device__ __forceinline__ int row_of(const CrossParams& p, const Work& w, const
   return q < p.rows.N ? p.rows.frame(a) * p.rows.N + q : -1;
 }
 
+// Whether a tile's row is one: row_of(...) >= 0, without the active list.
+__device__ __forceinline__ bool is_row(const CrossParams& p, const Work& w, const Item& t, int tile,
+                                       int row) {
+  if (p.packed) {
+    const int al = p.by_frame_rows.div(row);
+    return al < p.tile_frames && (p.kv_range || tile * p.tile_frames + al < w.A);
+  }
+  const int r = tile * w.rows + row;
+  if (p.kv_range) return r < p.rows.N;
+  return row < w.rows && r < w.A * p.rows.Np && r - p.rows.by_Np.div(r) * p.rows.Np < p.rows.N;
+}
+
 // The first of the 128 consecutive tokens of one head that a tile's rows are, or -1: rows of
 // several frames or heads, or fewer than 128.
 __device__ __forceinline__ int whole_tile(const CrossParams& p, const Work& w, const Item& t, int tile) {
@@ -778,7 +790,8 @@ __device__ __forceinline__ uint4 pack8(const float* o, float scale) {
 // item, with P left in tensor memory for the MMA warp.  False: a wait gave up.
 template <int D, bool F16, int KEYS>
 __device__ __forceinline__ bool softmax_item(const CrossParams& p, const Work& w, const Item& t,
-                                             int X, uint32_t tS, uint32_t tO, uint32_t bar_s, int& s_cnt, float& m_out,
+                                             int X, bool has_row, uint32_t tS, uint32_t tO,
+                                             uint32_t bar_s, int& s_cnt, float& m_out,
                                              float& l_out, volatile int* abort) {
   const float sl2 = p.scale_log2;
   const bool gather = gathers<KEYS>(w);
@@ -823,7 +836,8 @@ __device__ __forceinline__ bool softmax_item(const CrossParams& p, const Work& w
     const float mx = fmaxf(fmaxf(fmaxf(mx8[0], mx8[1]), fmaxf(mx8[2], mx8[3])),
                            fmaxf(fmaxf(mx8[4], mx8[5]), fmaxf(mx8[6], mx8[7])));
     const float m_new = fmaxf(m, mx * sl2);
-    const bool rescale = __any_sync(0xffffffffu, m_new > m + kRescaleLog2);
+    // (what is in the tile past its rows has no say: tokens of other frames, or an earlier tile's)
+    const bool rescale = __any_sync(0xffffffffu, has_row && m_new > m + kRescaleLog2);
     float fac = 1.f;
     if (rescale) {
       // a row that has seen no key yet has m = m_new = -inf: factor 1, not 2^(-inf + inf)
@@ -892,22 +906,29 @@ __device__ __forceinline__ bool softmax_group(const CUtensorMap* tmO, const Cros
   int64_t at = -1;  // byte offset of this thread's row in O
   int s_cnt = 0, o_cnt = 0;
   Item next;
-  if (w.first < w.items) next = get_item<KEYS>(p, w, w.first, rank);
+  bool next_row = false;
+  auto find = [&](int i) {  // the next item
+    if (i >= w.items) return;
+    next = get_item<KEYS>(p, w, i, rank);
+    next_row = is_row(p, w, next, 2 * next.pair + X, row);
+  };
+  find(w.first);
 #pragma unroll 1
   for (int i = w.first, turn = 0; i < w.items;) {
     const Item t = next;
+    const bool valid = next_row;
     i += w.step[turn];
     turn ^= 1;
     const int tile = 2 * t.pair + X;
     if (tile >= w.tiles) {
-      if (i < w.items) next = get_item<KEYS>(p, w, i, rank);
+      find(i);
       continue;
     }
     float m = -INFINITY, l = 0.f;
     bool ok = t.j0 >= t.j1 ||
-              softmax_item<D, F16, KEYS>(p, w, t, X, tS, tO, bar(C::kSFull + X), s_cnt, m, l, abort);
+              softmax_item<D, F16, KEYS>(p, w, t, X, valid, tS, tO, bar(C::kSFull + X), s_cnt, m, l, abort);
     // found while the last P V runs: behind it every cycle counts
-    if (i < w.items) next = get_item<KEYS>(p, w, i, rank);
+    find(i);
     const int first = whole_tile(p, w, t, tile);
     // no key: zeros, not 0 * accumulator, which may hold anything
     const bool none = l == 0.f;
