@@ -457,8 +457,8 @@ rf_status rf_cross_attn(void* d_O, float* d_lse, const void* d_Q, const void* d_
  *               (0: one gate for all frames)
  *   d_R         [F*N][d_out] of out_dtype, or NULL; may be d_Y itself (same stride)
  *   d_status    as for rf_attn, or NULL
- * X and W rows on 16-byte boundaries (RF_ERR_MISALIGNED): d_in itself may be any number, as may
- * d_out.  Outputs, bias, gate and residual need only their own elements' alignment, and are moved in
+ * X and W rows on 16-byte boundaries (RF_ERR_MISALIGNED; a single row's stride may be any): d_in itself
+ * may be any number, as may d_out.  Outputs, bias, gate and residual need only their own elements' alignment, and are moved in
  * vectors where all of them are 16-byte aligned.  Requires an sm_103 device.
  */
 rf_status rf_linear(void* d_Y, int64_t y_row_stride, int out_dtype, const void* d_X,

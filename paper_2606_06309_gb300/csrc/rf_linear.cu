@@ -965,6 +965,9 @@ extern "C" rf_status rf_linear(void* d_Y, int64_t y_row_stride, int out_dtype, c
     return fail(RF_ERR_INVALID_ARG, "rf_linear: active list and counts come together");
   if (d_R == d_Y && r_row_stride != y_row_stride && static_cast<int64_t>(F) * N > 1)
     return fail(RF_ERR_INVALID_ARG, "rf_linear: in place with two strides");
+  // (a row by itself has no stride that matters: the tensor map gets one on a boundary)
+  if (static_cast<int64_t>(F) * N == 1) x_row_stride = (x_row_stride + 7) / 8 * 8;
+  if (d_out == 1) w_row_stride = (w_row_stride + 7) / 8 * 8;
   if (!aligned16(d_X) || !aligned16(d_W) || x_row_stride % 8 || w_row_stride % 8)
     return fail(RF_ERR_MISALIGNED, "rf_linear: X and W rows on 16-byte boundaries");
   const int es_out = dtype_bytes(out_dtype);
