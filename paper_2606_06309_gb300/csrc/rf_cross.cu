@@ -32,15 +32,15 @@
 // from all of them, in the order of the ranges.
 //
 // Measured (device time, calls one after another):
-//   75,600 tokens, 40 heads of 128, 512 states: 541 us, 1.47 PFLOP/s on one set of inputs (597 us with
+//   75,600 tokens, 40 heads of 128, 512 states: 541 us, 1.47 PFLOP/s on one set of inputs (609 us with
 //     inputs that change from call to call, when the power limit lowers the clock).  An item of 4 K/V
 //     tiles takes 13,200 cycles: 9,200 in its steps, of which the products are 8,200, and 4,000 from
 //     the last product to the next item's first P.
-//   6,240 of 20,280 tokens, 12 heads, 512 states: 20.8 us: 300 items, two for nearly every SM, and the
+//   6,240 of 20,280 tokens, 12 heads, 512 states: 20.1 us: 300 items, two for nearly every SM, and the
 //     launch's start and end.
-//   16 sequences of one token, 12 heads, 32,000 states in 16 ranges: 46 us, 4.3 TB/s of K and V: the
+//   16 sequences of one token, 12 heads, 32,000 states in 16 ranges: 44.5 us, 4.4 TB/s of K and V: the
 //     longest sequence's tiles on the SMs that share it.
-//   20 of 33 frames of 1003 tokens, 24 heads on 6 of 64, windows of 1500 states with masked ones: 70 us.
+//   20 of 33 frames of 1003 tokens, 24 heads on 6 of 64, windows of 1500 states with masked ones: 68 us.
 //     Items of two or three K/V tiles: half of the time is the change from item to item.
 #include <cuda_runtime.h>
 

@@ -14,12 +14,14 @@
 // Measured (device time, calls one after another):
 //   75,600 rows 5120 -> 5120, residual and gate: bounded by the tensor cores, 1.84 PFLOP/s while
 //     the clock holds (2.16 ms; 2.57 ms, 1.54 PFLOP/s, when the power limit lowers it).
-//   6,240 of 20,280 rows 1536 -> 6144, bias and GELU: 82 us, 1.44 PFLOP/s: 600 tiles are 7.9 for
-//     each of the 76 pairs, a tile's products take 12,300 cycles, and the last tile's activation,
-//     5 us, has none to hide behind.
+//   6,240 of 20,280 rows 1536 -> 6144, bias and tanh-GELU: 82 us, 1.44 PFLOP/s (87 to 90 with inputs
+//     that change from call to call).  As one frame, or in frames of whole tiles, 72 us, and without the
+//     activation 66, eight rounds of the 76 pairs: 6 us are the last tiles' activation, which has no
+//     products to hide behind, and 10 to 12 the 72 of 600 tiles that lie across frames of 1560 tokens
+//     and are loaded in boxes.
 //   1 row 1536 -> 9216: 9.4 us, of which reading W's 28 MB takes 4.2: launch, tensor memory,
 //     barriers and one cluster's exchange are the rest.
-//   333 rows 1000 -> 777: 10.8 us, the same fixed costs.
+//   333 rows 1000 -> 777: 10.9 us, the same fixed costs.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -370,8 +372,10 @@ __device__ __forceinline__ int row_token(const LinearParams& p, int r, int& fram
 struct RowMaps {
   const CUtensorMap *whole, *many, *unit;
 };
-// Issue the copies of one k block of a tile's rows (the bytes are announced before; one thread).
-// Boxes are dealt to `of` threads; a whole tile's is the last one's.
+// Issue the copies of one k block of a tile's rows (one thread of each of the `of` warps they are dealt
+// to; a whole tile's box is the last one's).  The barrier's one arrival carries the bytes of all of
+// them and holds its phase open: copies of other warps, and of a pair's second CTA, may land before
+// it, and count below zero until then.  So the arrival is never parted from the count of bytes.
 template <bool PAIR, int CAP>
 __device__ __forceinline__ void load_rows(const RowBoxes& x, const BoxList<CAP>& list,
                                           const RowMaps& maps, uint32_t dst, uint32_t bar, int k0,

@@ -29,9 +29,9 @@ constexpr int tile_rows(int unit, int most) { return most / unit * unit; }
 
 // How a tile of rows is loaded: in one TMA box where its rows lie in one frame, else in boxes of
 // kBoxRows and of `unit` rows, listed in shared memory {first token, first row of the tile}: the
-// larger ones from the front of the list, the others from its end.  One elected thread issues them
-// all, each from a fixed tensor map: a box issued by its own lane under a branch, or with the map
-// chosen per box, held a product's 512-cycle step up to three times its length.
+// larger ones from the front of the list, the others from its end.  One elected thread of a warp issues
+// that warp's share of them, each from a fixed tensor map: a box issued by its own lane under a branch,
+// or with the map chosen per box, held a product's 512-cycle step up to three times its length.
 constexpr int kBoxRows = 32;
 template <int CAP>  // boxes at most; a tile has at most 256 rows
 struct BoxList {
