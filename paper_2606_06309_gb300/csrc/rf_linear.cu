@@ -63,13 +63,13 @@ __device__ __forceinline__ float rcp_approx(float x) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-// x * sigmoid(s) = x / (1 + h^2) with h = e^(-s / 2) = 2^t.  Both sides of the quotient are scaled by 2^-22:
-// the denominator then stays in the range of floats where the value does (SiLU to -100; unscaled the
-// quotient is 0 from -87.3 down, where the value is -1e-36).
+// x * sigmoid(s) = x / (1 + h^2) with h = e^(-s / 2) = 2^t.  The denominator is scaled by 2^-22 and its
+// reciprocal back, so that it stays in the range of floats where the value does (SiLU to -100; unscaled
+// the quotient is 0 from -87.3 down, where the value is -1e-36).
 __device__ __forceinline__ float times_sigmoid(float x, float t) {
   constexpr float kScale = 0x1p-22f;
   const float h = ex2_approx(t);
-  return x * kScale * rcp_approx(fmaf(h * kScale, h, kScale));
+  return x * (kScale * rcp_approx(fmaf(h * kScale, h, kScale)));  // (x 2^-22 could lose digits)
 }
 // x Phi(x).  The tail Phi(-|x|) = e^(-x^2 / 2) times a function that falls from 1/2 to 0.03 over the
 // numbers where it is not yet lost; that one is t Q(t) with t = 1 / (1 + 0.3 |x|) and Q of degree 7,

@@ -71,3 +71,22 @@ def test_activation_of_infinities(cuda_lib, act):
     y = Y.cpu()[:, 0]
     assert y[0] == math.inf and torch.isnan(y[1])
     assert y[2] == x[2, 0].float() and y[3] == 0.0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("act", ["gelu", "gelu_tanh", "silu"])
+def test_activation_of_tiny_numbers(cuda_lib, act):
+    """Next to 0 each is z / 2, to 2^-20 of it, down to the smallest normal results."""
+    e = torch.arange(-124, -20)
+    z = torch.cat([(1 + 37 / 128) * 2.0 ** e, -(1 + 91 / 128) * 2.0 ** e])[:, None].to(torch.bfloat16)
+    for rows in (z, z.repeat(3, 1)):  # both kernels
+        n = rows.shape[0]
+        d_out = 8 if n <= 256 else 5120
+        X = torch.zeros(n, 8, dtype=torch.bfloat16, device=DEV)
+        W = torch.zeros(d_out, 8, dtype=torch.bfloat16, device=DEV)
+        X[:, :1], W[:, :1] = rows.to(DEV), 1.0
+        Y = torch.empty(n, d_out, device=DEV)
+        cuda_lib.rf_linear(Y, X[:, :1], W[:, :1], 1, n, act=act)
+        y, x = Y.cpu().double(), rows.double()
+        want, _ = _act(x, act)
+        assert ((y - want).abs() <= 2.0 ** -20 * want.abs()).all()
