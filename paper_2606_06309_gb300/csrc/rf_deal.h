@@ -1,4 +1,4 @@
-// rf_deal.h -- a tile's boxes of rows dealt to the warps that load them.
+// rf_deal.h -- a tile's boxes of rows dealt to the warps that load them, and the frame its rows are of.
 #pragma once
 #include "rf_div.h"
 
@@ -23,5 +23,19 @@ struct Deal {
     return i;
   }
 };
+
+// The active frame that rows [r0, r0 + n) are of, those below `end` that is, and whether it is one.  Rows from
+// `end` on are in no frame, but the padding of the last one, and a pair's second half may have no others: it
+// gets the last row's frame, so that what is read by the frame's number is there.  by: rows of a frame.
+struct RowsFrame {
+  int a;
+  bool one;
+};
+template <typename Div>
+RF_HOST_DEVICE RowsFrame rows_frame(int r0, int n, int end, const Div& by) {
+  const int last = (r0 + n < end ? r0 + n : end) - 1;
+  const int a = by.div(r0 < last ? r0 : last);
+  return {a, a == by.div(last)};
+}
 
 }  // namespace rf

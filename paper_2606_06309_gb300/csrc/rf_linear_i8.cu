@@ -433,11 +433,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads8, 1)
       const float* gate = p.epi.gate;
       bool one_gate = p.epi.gate_stride == 0;
       if (gate && !one_gate) {  // the tile's rows are of one frame?
-        const int r1 = min(r0 + half, R) - 1;
-        const FastDiv& by = p.rows.active ? p.rows.by_Np : p.by_N;
-        const int a = by.div(min(r0, r1));
-        one_gate = a == by.div(r1);
-        if (one_gate) gate += p.rows.frame(a) * p.epi.gate_stride;
+        // (without a list the rows are the tokens, and those that pad them are of no frame)
+        const RowsFrame rf = p.rows.active ? rows_frame(r0, half, R, p.rows.by_Np)
+                                           : rows_frame(r0, half, p.rows.T, p.by_N);
+        one_gate = rf.one;
+        if (one_gate) gate += p.rows.frame(rf.a) * p.epi.gate_stride;
       }
       if (threadIdx.x - 128 < kTileCols) fetch_col(p.epi, tc, n * q.bn, threadIdx.x - 128, one_gate ? gate : nullptr);
       __syncwarp();
