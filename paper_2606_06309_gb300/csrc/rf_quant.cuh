@@ -12,7 +12,7 @@ namespace rf {
 // quotient rounds to a half: t in [2^i, 2^(i+1)) is a quotient of whole numbers with a denominator below
 // 2^(20-i), so it differs from a half by 2^(i-20) or more, and t's rounding is 2^(i-24).  Of 32-bit rows one
 // may, and is compared exactly: p + pe is c most, c = h + 1/2, and 127 y - p, of numbers that near to each
-// other, has no rounding.
+// other, has no rounding.  Neither overflows: y and most are RowScale's, scaled to 2^28 at most.
 __device__ __forceinline__ int exact_digit(float y, float k, float most) {
   const float h = floorf(y * k), c = h + 0.5f;
   const float p = c * most, pe = fmaf(c, most, -p), q = fmaf(127.f, y, -p);
@@ -29,12 +29,13 @@ __device__ __forceinline__ float largest(float most, float a, float b) {
 
 // The factor and scale of a row whose largest value's bits (without the sign) are most_bits: NaN above
 // infinity above the others.  A row with one of those gets the scale NaN and digits 0, so its products are
-// NaN.  Rows too small for 127 / most are multiplied by 2^100 first.
+// NaN.  Rows too small for 127 / most are multiplied by 2^100 first; ones so large that 127 most could pass
+// the largest float, by 2^-100 (what that takes below the normal numbers has the digit 0 either way).
 struct RowScale {
   float k, k_lo, scale, most, up;
   __device__ __forceinline__ explicit RowScale(uint32_t most_bits) {
     most = __uint_as_float(most_bits);
-    up = most < 0x1p-100f ? 0x1p100f : 1.f;
+    up = most < 0x1p-100f ? 0x1p100f : most > 0x1p100f ? 0x1p-100f : 1.f;
     const bool ok = most_bits < 0x7F800000u;
     scale = ok ? most / 127.f : __uint_as_float(0x7FC00000u);
     most *= up;
