@@ -32,6 +32,13 @@ struct Epilogue {
   int vec_cols;         // bias, gate and w_scale alone
 };
 
+// A token's scale as two factors, one for before the column's and one for after it: a sum below 2^31 times the
+// first stays below 2^95, so that nothing overflows but a product of all three that does.  The second is 1 for all
+// but rows of numbers above 2^70.
+constexpr float kLargeScale = 0x1p64f;
+__device__ __forceinline__ float scale_first(float xs) { return fabsf(xs) > kLargeScale ? 1.f : xs; }
+__device__ __forceinline__ float scale_then(float xs) { return fabsf(xs) > kLargeScale ? xs : 1.f; }
+
 __device__ __forceinline__ float load_elem(const void* p, int64_t i, int dtype) {
   if (dtype == RF_FP32) return static_cast<const float*>(p)[i];
   if (dtype == RF_FP16) return __half2float(static_cast<const __half*>(p)[i]);
@@ -389,7 +396,7 @@ __device__ __forceinline__ void finish_tokens(const Epilogue& e, const int2* tok
       for (int u = 0; u < kTok; ++u) {
         const float xs = t[u].x >= 0 ? e.x_scale[t[u].x] : 0.f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[4 * u + i] = v[4 * u + i] * xs * ws[i] + bias[i];
+        for (int i = 0; i < 4; ++i) v[4 * u + i] = v[4 * u + i] * scale_first(xs) * ws[i] * scale_then(xs) + bias[i];
       }
     activate(e.act, v);
 #pragma unroll

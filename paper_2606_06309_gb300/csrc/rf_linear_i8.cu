@@ -111,8 +111,11 @@ __device__ __forceinline__ void each4(const float* from, float (&v)[32], uint64_
 __device__ __forceinline__ void finish_scaled(const Epilogue& e, const TileCols& c, int at, int frame, int n,
                                               float xs, bool one_gate, float (&v)[32]) {
 #pragma unroll
-  for (int i = 0; i < 32; i += 2) f2_unpack(fmul2(f2_pack(v[i], v[i + 1]), f2_pack(xs, xs)), v[i], v[i + 1]);
+  for (int i = 0; i < 32; i += 2) f2_unpack(fmul2(f2_pack(v[i], v[i + 1]), f2_both(scale_first(xs))), v[i], v[i + 1]);
   each4(c.scale + at, v, fmul2);
+  if (fabsf(xs) > kLargeScale)
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] *= xs;
   if (e.bias) each4(c.bias + at, v, fadd2);
   activate(e.act, v);
   if (!e.gate) return;
@@ -820,7 +823,8 @@ __global__ void __launch_bounds__(kDotThreads) dot8_kernel(const __grid_constant
       f = frame[r];
     }
   if (t < 0 || n >= e.n_out) return;
-  float v[1] = {static_cast<float>(mine) * e.x_scale[t] * e.w_scale[n]};
+  const float xs = e.x_scale[t];
+  float v[1] = {static_cast<float>(mine) * scale_first(xs) * e.w_scale[n] * scale_then(xs)};
   if (e.bias) v[0] += load_elem(e.bias, n, e.in_dtype);
   activate(e.act, v);
   if (e.gate) v[0] *= e.gate[f * e.gate_stride + n];
