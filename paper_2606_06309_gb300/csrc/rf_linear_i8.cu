@@ -502,7 +502,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads8, 1)
         seal();
         __syncwarp();
         if (lane == 0) {
-          mbar_arrive_cta(in);
+          mbar_arrive_shared(in);
           mbar_arrive(bar(C::kBarEmpty + s));
         }
         s += 2;

@@ -45,12 +45,15 @@ __device__ __forceinline__ void mbar_arrive_remote(uint32_t bar) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar)
                : "memory");
 }
-// The same, ordering this thread's accesses within its own CTA only.  For arrivals that announce what the
-// tensor cores read of this CTA's own shared and tensor memory, behind fence_proxy_async or
-// tcgen05.wait::st, which have completed it: no thread of the other CTA reads it.  (The cluster's
-// release waits for all of the warp's accesses in flight: eight warps on a 384-cycle step 1000.)
-__device__ __forceinline__ void mbar_arrive_cta(uint32_t bar) {
-  asm volatile("mbarrier.arrive.release.cta.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+// The same, ordering accesses of this CTA's own shared memory only (of any of its threads that this one has
+// synchronised with): for arrivals that announce what the tensor cores read there, or in tensor memory behind
+// tc_fence_before.  mbar_arrive_remote waits for all of the warp's accesses in flight, of global memory too: eight
+// warps took a 384-cycle step to 1000 with it, and one warp that did it for them 2.1 ms to 3.2.
+__device__ __forceinline__ void mbar_arrive_shared(uint32_t bar) {
+  asm volatile(
+      "fence.release.sync_restrict::shared::cta.cluster;\n\t"
+      "mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar)
+      : "memory");
 }
 __device__ __forceinline__ bool mbar_try_wait_cluster(uint32_t bar, uint32_t parity) {
   uint32_t ok;
