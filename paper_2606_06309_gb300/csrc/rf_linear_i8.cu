@@ -579,12 +579,13 @@ constexpr int kS8Full = 0, kS8Empty = kSplitMaxStages8, kS8Acc = 2 * kSplitMaxSt
 constexpr int kS8OffBar = kSplitRing8, kS8OffMisc = kS8OffBar + kS8Bars * 8, kS8OffTok = kS8OffMisc + 24,
               kSplitSmem8 = kS8OffTok + 256 * 8 + 1024;
 
-// 16 digits of a row from k on; zeros past K, and where there is no row.
+// 16 digits of a row from k on; zeros past K, and where there is no row.  (An ordinary load: the launch before may
+// have made W or X while this grid was resident already, which .nc does not allow.)
 __device__ __forceinline__ uint4 digits16(const int8_t* row, int k, int K) {
   uint4 v = make_uint4(0, 0, 0, 0);
   if (!row || k >= K) return v;
   if (k + 16 <= K) {
-    asm volatile("ld.global.nc.L1::no_allocate.L2::128B.v4.u32 {%0, %1, %2, %3}, [%4];"
+    asm volatile("ld.global.L1::no_allocate.L2::128B.v4.u32 {%0, %1, %2, %3}, [%4];"
                  : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
                  : "l"(row + k));
     return v;

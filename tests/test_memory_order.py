@@ -1,5 +1,5 @@
 """What the kernels' sources must not do, as no run shows it reliably: order memory between CTAs with less than the
-cluster's scope."""
+cluster's scope, or read through the read-only path what a launch before them may still be writing."""
 import glob
 import os
 import re
@@ -39,3 +39,12 @@ def test_remote_arrivals_take_mapped_addresses():
         mapped = set(re.findall(r"(\w+) = map_to_rank\(", text))
         for call in re.findall(r"\bmbar_arrive(?:_expect_tx)?\((\w+)", text):
             assert call not in mapped, (name, call)
+
+
+def test_no_read_only_loads_of_what_a_launch_before_may_write():
+    """Grids of rf_linear_i8 are resident before the launch that makes their digits and scales has ended: no loads
+    that take memory for read-only while the kernel lives."""
+    text = _code()["rf_linear_i8.cu"]
+    assert "cudaGridDependencySynchronize" in text
+    for name in ("rf_linear_i8.cu", "rf_quant.cu", "rf_norm.cu", "rf_epilogue.cuh", "rf_vec.cuh", "rf_stage.cuh"):
+        assert not re.search(r"ld\.global[.\w:]*\.nc|__ldg\(", _code()[name]), name
