@@ -960,9 +960,16 @@ void shape(NormParams& p, int E, int slots) {
   p.chunks = (p.N + p.chunk_rows - 1) / p.chunk_rows;
 }
 
+// What all calls take: tokens, and pieces with their number in a launch's grid.
+bool too_many_tokens(int F, int N) { return static_cast<int64_t>(F) * N > 0x7FFFFFFF - 65536; }
+bool too_many_pieces(const NormParams& p) {
+  return static_cast<int64_t>(p.F) * p.chunks * p.tiles > 0x7FFFFFFF - 65536;
+}
+
 // Workspace for any alignment: the pieces' sums, for the gradients all channels' too, and the joined ones.
+// -1 where rows of all alignments have too many pieces.
 int64_t norm_bytes(int F, int N, int C, int G, bool grad) {
-  int64_t most = 0;
+  int64_t most = -1;
   for (int E : {1, 4, 8}) {
     if (C % E) continue;
     NormParams p{};
@@ -972,6 +979,7 @@ int64_t norm_bytes(int F, int N, int C, int G, bool grad) {
     p.G = G;
     p.cpg = C / G;
     shape(p, E, slots_of(grad ? kGrad : kRows));
+    if (too_many_pieces(p)) continue;
     const int64_t pieces = static_cast<int64_t>(F) * p.chunks;
     most = std::max(most, 8 * (pieces * (static_cast<int64_t>(p.tiles) * p.tile_groups + (grad ? C : 0)) + static_cast<int64_t>(F) * G));
   }
@@ -1000,6 +1008,7 @@ template <typename T, int E, int MODE>
 rf_status launch(NormParams& p, const DeviceInfo& di, cudaStream_t st, const char* what) {
   using L = Layout<T, E, MODE>;
   shape(p, E, slots_of(MODE));
+  if (too_many_pieces(p)) return fail(RF_ERR_INVALID_ARG, "rf_group_norm: too many frames");
   p.by_cpg = FastDiv(static_cast<uint32_t>(p.cpg));
   p.by_tx = FastDiv(static_cast<uint32_t>(p.tx));
   p.by_ty = FastDiv(static_cast<uint32_t>(p.ty));
@@ -1010,7 +1019,6 @@ rf_status launch(NormParams& p, const DeviceInfo& di, cudaStream_t st, const cha
   p.by_segs = FastDiv(static_cast<uint32_t>(p.group_segs));
   p.w_vec = aligned16(p.weight) && aligned16(p.bias);
   const int64_t pieces = static_cast<int64_t>(p.F) * p.chunks * p.tiles;
-  if (pieces > 0x7FFFFFFF - 65536) return fail(RF_ERR_INVALID_ARG, "rf_group_norm: too many frames");
   p.done = p.part + pieces * p.tile_groups;
   p.channels = p.done + static_cast<int64_t>(p.F) * p.G;
   static std::atomic<bool> done[3][64] = {};
@@ -1076,8 +1084,7 @@ rf_status check_norm(const char* fn, int dtype, int F, int N, int C, int G, int 
                      const int32_t* d_counts, const void* d_workspace, int64_t bytes, bool grad) {
   if (!dtype_bytes(dtype)) return fail(RF_ERR_UNSUPPORTED, fn);
   if (F < 1 || N < 1 || C < 1) return fail(RF_ERR_INVALID_ARG, fn);
-  if (static_cast<int64_t>(F) * N > 0x7FFFFFFF - 65536)
-    return fail(RF_ERR_INVALID_ARG, "group norm: too many tokens");
+  if (too_many_tokens(F, N)) return fail(RF_ERR_INVALID_ARG, "group norm: too many tokens");
   if (C > kMaxC) return fail(RF_ERR_INVALID_ARG, "group norm: more than 65536 channels");
   if (G < 1 || C % G) return fail(RF_ERR_INVALID_ARG, "group norm: channels are not whole groups");
   if (w_dtype != dtype && w_dtype != RF_FP32)
@@ -1089,7 +1096,9 @@ rf_status check_norm(const char* fn, int dtype, int F, int N, int C, int G, int 
       reinterpret_cast<uintptr_t>(d_weight) % dtype_bytes(w_dtype) ||
       reinterpret_cast<uintptr_t>(d_bias) % dtype_bytes(w_dtype))
     return fail(RF_ERR_MISALIGNED, "group norm: pointer not on its elements' boundary");
-  if (bytes < norm_bytes(F, N, C, G, grad))
+  const int64_t need = norm_bytes(F, N, C, G, grad);
+  if (need < 0) return fail(RF_ERR_INVALID_ARG, "group norm: too many frames");
+  if (bytes < need)
     return fail(RF_ERR_INVALID_ARG, "group norm: workspace below rf_group_norm_workspace_bytes");
   return RF_OK;
 }
@@ -1100,7 +1109,8 @@ rf_status check_norm(const char* fn, int dtype, int F, int N, int C, int G, int 
 using namespace rf;
 
 extern "C" int64_t rf_group_norm_workspace_bytes(int F, int N, int C, int G, int dtype) {
-  if (F < 1 || N < 1 || C < 1 || G < 1 || C % G || C > kMaxC || !dtype_bytes(dtype)) return -1;
+  if (F < 1 || N < 1 || C < 1 || G < 1 || C % G || C > kMaxC || !dtype_bytes(dtype) || too_many_tokens(F, N))
+    return -1;
   return norm_bytes(F, N, C, G, true);
 }
 
