@@ -989,8 +989,6 @@ int64_t norm_bytes(int F, int N, int C, int G, bool grad) {
 template <typename K, typename... A>
 rf_status run(K kernel, int64_t grid, int64_t smem, const DeviceInfo& di, cudaStream_t st, const char* what,
               std::atomic<bool> (&done)[64], const A&... args) {
-  if (smem + 1024 > di.max_smem_optin)
-    return fail(RF_ERR_UNSUPPORTED, "rf_group_norm: too many channels for rows of 8 bits");
   if (smem + 1024 > 48 * 1024 && !done[di.device]) {  // (with what a kernel declares)
     if (cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, di.max_smem_optin - 1024))
       return fail(RF_ERR_CUDA, "cudaFuncSetAttribute(rf_group_norm)", e);
@@ -1035,6 +1033,8 @@ rf_status launch(NormParams& p, const DeviceInfo& di, cudaStream_t st, const cha
     smem8 = p.C * (E == 8 ? 14ll : 12ll) + kDigitVecs<E> * kThreads * 16;
     p.ring = sizeof(T) * E == 16 && p.segs == 1 && smem8 + 1024 <= di.max_smem_optin;
     if (!p.ring) smem8 = p.C * 12ll;
+    if (smem8 + 1024 > di.max_smem_optin)  // (before the first launch: a call that is refused writes nothing)
+      return fail(RF_ERR_UNSUPPORTED, "rf_group_norm: too many channels for rows of 8 bits");
     // whole waves of blocks, with 64 rows of a block and up where every frame is active
     p.blocks = std::max<int64_t>(p.F, 2 * 152 * std::max<int64_t>(1, rows / (2 * 152 * 64)));
   } else {

@@ -47,3 +47,19 @@ def test_more_pieces_than_a_grid_has(cuda_lib):
     got = cuda_lib.load().rf_group_norm(P, 65536, None, 2 * P, 65536, 0, 1, 1 << 30, 65536, 1, None, None, 0, 1e-5, 0, None,
                                         256, HUGE, None, None, None)
     assert got == 1
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("C", [19400, 65536])
+def test_a_refused_call_writes_nothing(cuda_lib, C, dtype):
+    """Rows of 8 bits with more channels than shared memory has factors for: digits, scales and statistics stay."""
+    F, N, G = 2, 100, 8
+    X = torch.ones(F * N, C, dtype=dtype, device="cuda")
+    Y, s = torch.full((F * N, C), 77, dtype=torch.int8, device="cuda"), torch.full((F * N,), 7.0, device="cuda")
+    st = torch.full((F, G, 2), 7.0, device="cuda")
+    ws = torch.zeros(rf.rf_group_norm_workspace_bytes(F, N, C, G, dtype), dtype=torch.uint8, device="cuda")
+    with pytest.raises(rf.RFError):
+        rf.rf_group_norm(Y, X, F, N, G, stats=st, scale=s, workspace=ws)
+    torch.cuda.synchronize()
+    assert (Y == 77).all() and (s == 7.0).all() and (st == 7.0).all() and not ws.any()
