@@ -1,5 +1,6 @@
-// rf_epilogue.cuh -- what rf_linear and rf_linear_i8 share: sums of products on their way out (scales, bias,
-// activation, gate, residual), and the rows of a tile on their way in.
+// rf_epilogue.cuh -- sums of products on their way out (scales, bias, activation, gate, residual) and the rows of a
+// tile on their way in, for rf_linear and rf_linear_i8.  Both use all of it, but for finish_tile and what it
+// calls: those are rf_linear's, and rf_linear_i8's pairs have a form of their own.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>

@@ -4,7 +4,7 @@
 //     Y[t, n] = R[t, n] + g[n] * act(s[t] u[n] sum_k X[t, k] W[n, k] + b[n])     t: tokens of active frames
 //
 // The tensor cores of sm_103a have no product of 8-bit integers (tcgen05's kind::i8 is refused for this
-// target).  A byte is exact in fp16, a product of two in 22 bits, so digits are expanded to fp16 on
+// target).  A byte is exact in fp16, a product of two in 15 bits, so digits are expanded to fp16 on
 // their way to the tensor cores and summed in fp32: exactly while sums stay below 2^24.  Memory and L2
 // see bytes only.
 //
@@ -14,13 +14,14 @@
 //   dot8_kernel   up to eight rows: whole-number sums (dp4a), no tensor core
 //
 // Measured (device time, calls one after another):
-//   75,600 rows 5120 -> 5120: 2.04 to 2.08 ms, 1.9 PFLOP/s while the clock holds, of the tensor cores' 2.4 at
+//   75,600 rows 5120 -> 5120: 2.13 to 2.18 ms, 1.85 PFLOP/s while the clock holds, of the tensor cores' 2.4 at
 //     that clock: the expanding warps' instructions (two thirds of the issue slots) and the hand-overs; with
-//     residual and gate 2.28 to 2.42.  (rf_linear of 16-bit rows: 1.80 to 1.93 and 2.2 to 2.5.)
-//   6,240 of 20,280 rows 1536 -> 6144, bias and tanh-GELU: 107 us.  As one frame without activation 96:
-//     eleven rounds of the 76 pairs, each with an epilogue as long as its products.
-//   1 row 1536 -> 9216: 3.4 us, of which W's 14 MB take 2.1.
-//   333 rows 1000 -> 777: 12 to 14 us: launch, tensor memory, and digits that come in three dependent steps
+//     residual 2.30 to 2.41.  (rf_linear of 16-bit rows: 1.87 to 1.96, with residual and gate 2.2 to 2.5.)
+//   6,240 of 20,280 rows 1536 -> 6144, bias and tanh-GELU: 113 to 136 us.  As one frame without activation 92 to
+//     98: eleven rounds of the 76 pairs, some 16,500 cycles a tile, of which 24 steps at the rate of long rows are
+//     11,200; what the others go to is not known.  (rf_linear: 82 and 65 to 73.)
+//   1 row 1536 -> 9216: 3.3 us, of which W's 14 MB take 2.1.
+//   333 rows 1000 -> 777: 12 us: launch, tensor memory, and digits that come in three dependent steps
 //     (global memory, registers, shared memory).
 #include <cuda_runtime.h>
 
@@ -129,7 +130,7 @@ __device__ __forceinline__ void finish_scaled(const Epilogue& e, const TileCols&
   }
 }
 
-// finish_tile with scales: a warp's 32 rows of an accumulator (tensor memory columns from `acc`; a row per
+// As rf_linear's finish_tile, with scales, and other registers and waits: a warp's 32 rows of an accumulator (tensor memory columns from `acc`; a row per
 // lane, its token or -1), columns n0 .. n0 + cols - 1 of the result, the tile's from `col` on, 128 bytes of them at a time through the
 // warp's stage.  ready() is called when the accumulator is wanted, read() when it has been read; false from
 // ready() ends it.
@@ -899,7 +900,8 @@ rf_status launch_pair(I8Params& q, int64_t rows, const DeviceInfo& di, cudaStrea
 
 // Tokens per tile and CTAs per cluster of a split launch: the pair with the least to do for the busiest
 // SM, in cycles, as rf_linear's plan; a step of 64 digits takes the warps about a cycle for each four
-// of the 64 x (128 + tokens).
+// of the 64 x (128 + tokens).  It ranks the plans of one product, and is no measure of their time where W is
+// long: 16 rows 5120 -> 13824 take 54.9 us, over three times what it says.
 struct SplitPlan {
   int tokens, cluster;
 };
@@ -1044,15 +1046,16 @@ extern "C" rf_status rf_linear_i8(void* d_Y, int64_t y_row_stride, int dtype, co
   p.tile_rows = tile_rows(unit, 128);
   const int64_t pair_tiles = (rows + 2 * p.tile_rows - 1) / (2 * p.tile_rows) * ((d_out + kBN8 - 1) / kBN8);
   // Pairs of CTAs once their tiles occupy a third of the 76 pairs (us, pair against split; K -> columns):
-  //   tiles 15:  600 rows  320 ->  960 10.0 /  7.9    27:  128 rows 5120 ->  5120 26.2 / 31.4
-  //         16:  256 rows 1536 -> 3000 16.8 / 15.0    40:  300 rows 1000 ->  3840 12.6 / 15.5
-  //         16:  512 rows 1536 -> 1536 13.9 / 15.2    48: 2048 rows  256 ->  1024  9.7 / 11.0
-  //         24: 1024 rows  128 -> 1024  9.0 /  7.0    64: 4096 rows   64 ->   640  9.5 / 12.5
+  //   tiles 15:  600 rows  320 ->  960  9.3 /  7.4    27:  128 rows 5120 ->  5120 27.0 / 31.0
+  //         16:  256 rows 1536 -> 3000 15.9 / 14.5    40:  300 rows 1000 ->  3840 12.3 / 15.3
+  //         16:  512 rows 1536 -> 1536 13.9 / 14.6    48: 2048 rows  256 ->  1024  9.4 / 10.8
+  //         24: 1024 rows  128 -> 1024  8.7 /  6.8    64: 4096 rows   64 ->   640  9.3 / 12.5
   // A row of tiles costs the same whatever its rows, so for few of them it has to be longer, and K too:
-  //         48:   64 rows 1536 -> 9216 14.2 / 12.6    72:   16 rows 1536 -> 13824 14.8 / 16.5
-  //         72:   32 rows  320 -> 13824 11.2 / 7.5    72:   16 rows 5120 -> 13824 26.7 / 52.4
-  // Up to four rows it is W's bytes: dot products (4 rows 5120 -> 13824 12.6; 8 rows 32.9, pairs 26.7; 5 rows
-  // 1536 -> 1536 7.6).
+  //         48:   64 rows 1536 -> 9216 14.5 / 12.5    72:   16 rows 1536 -> 13824 14.9 / 15.6
+  //         72:   32 rows  320 -> 13824 10.5 / 7.3    72:   16 rows 5120 -> 13824 27.8 / 54.9
+  // (Between those, 100 rows 1536 -> 9216 take 14.3 / 15.0 and go the longer way.)
+  // Up to four rows it is W's bytes: dot products (4 rows 5120 -> 13824 12.3; 8 rows 32.6, pairs 29.0; 5 rows
+  // 1536 -> 1536 7.1).
   const bool pair = rows > 256 ? pair_tiles >= 25
                                : pair_tiles >= (rows >= 128 ? 25 : 64) && p.kblocks >= 16;
   if (rows == 1) return run_dot<1, 2>(q, s);

@@ -17,10 +17,11 @@
 // grid barrier behind the rows' stores, and the joining in every block.  75,600 rows of 5120 took 533 us.)
 // Where frames fit a block per tile, one launch (whole_kernel).
 //
-// Measured (device, fp16 and bf16): 75,600 rows of 5120 with SiLU 369 us, 2.3 GB in three passes at 6.3 TB/s; 4 of 13
-// frames of 1560 rows of 1536 17.5 us; one image of 399,360 x 128 with SiLU 58 us, two reads and a write at 5.3 TB/s;
+// Measured (device, fp16 and bf16): 75,600 rows of 5120 with SiLU 364 to 369 us: two reads and a write, 2.3 GB, would be 6.3 TB/s; 4 of 13
+// frames of 1560 rows of 1536 17.5 us; one image of 399,360 x 128 with SiLU 58 us, two reads and a write, which would be 5.3 TB/s;
 // gradients of 75,600 rows of 1536 225 us, 1.16 GB in five passes: the activation's slope and the products, twice each, at 60%
 // of the issue slots.  Bound by HBM where rows are many, by three launches of 5 us in all where they are few.
+// (How much of the second read comes from L2 is not measured: under the profiler each launch begins with cold caches.)
 //
 // The moments of a thread's rows are (mean, sum of squares about it), four (of single elements, sixteen) rows at a time, joined pairwise
 // (Chan, Golub and LeVeque, "Updating formulae and a pairwise algorithm for computing sample variances",
@@ -46,6 +47,7 @@ constexpr int kTileVecs = 128;              // vectors of a tile at most (of sin
 constexpr int kMaxC = 65536;                // channels
 
 enum Mode { kRows, kDigits, kGrad };
+// (152 SMs, sm_103a's: the workspace's size goes by these, and is asked for where there may be no device.)
 constexpr int slots_of(int mode) { return (mode == kGrad ? 2 : 3) * 152; }
 constexpr int blocks_of(int mode) { return mode == kGrad ? 2 : 3; }  // of an SM
 
